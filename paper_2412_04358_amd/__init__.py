@@ -2,6 +2,8 @@
 
 `approx_topk` / `exact_topk` call the hand-written HIP library through its C ABI; the
 library is loaded on first use and a missing build raises, there is no CPU fallback.
+What a decoder needs beside the selection - attention over a shared prefix, verification of
+drafted tokens, a cache's pages - is in decode.py.
 """
 from .binding import (  # noqa: F401
     ATK_BF16,
@@ -24,4 +26,19 @@ from .binding import (  # noqa: F401
     set_plan_override,
     strerror,
     worst_case_recall,
+)
+from .decode import (  # noqa: F401
+    ATK_F16,
+    ATK_STATUS_BAD_LEN,
+    ATK_STATUS_BAD_PAGE,
+    ATK_STATUS_BAD_SEQ,
+    ATK_STATUS_NO_PAGES,
+    PageTables,
+    append_tokens,
+    compact_pages,
+    copy_pages,
+    fork_sequences,
+    free_sequences,
+    shared_prefix_attention,
+    verify_drafts,
 )

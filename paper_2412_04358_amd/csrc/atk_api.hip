@@ -8,6 +8,7 @@
 #include <mutex>
 
 #include "atk_common.h"
+#include "atk_decode_common.h"
 #include "atk_exact.h"
 #include "atk_select.h"
 
@@ -19,6 +20,7 @@ static int hip_fail(hipError_t e) {
     g_last_hip_error = (int)e;
     return ATK_ERR_HIP;
 }
+int set_hip_error(hipError_t e) { return hip_fail(e); }
 
 static int64_t pow2_ceil(int64_t v) {
     int64_t p = 1;
@@ -1036,6 +1038,7 @@ const char *atk_strerror(int code) {
         case ATK_ERR_HIP: return "a HIP runtime call failed";
         case ATK_ERR_ALIGN: return "a pointer is not aligned to its element size";
         case ATK_ERR_WORKSPACE: return "the call needs more scratch than the allocation-free entry point holds (ATK_NOALLOC_SCRATCH_BYTES)";
+        case ATK_ERR_ARGS: return "an argument of a decoding call is out of the range that atk_decode.h states";
     }
     return "unknown error code";
 }

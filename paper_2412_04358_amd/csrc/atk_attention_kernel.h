@@ -1,0 +1,498 @@
+// Attention over a paged cache whose first keys all sequences of a batch share: one range of keys against a block of queries.
+//
+// Softmax over keys in any number of ranges: a range keeps m = max s, l = sum 2^(c (s - m)), o = sum 2^(c (s - m)) v (s = q.k, c = scale * log2(e)), and
+// ranges join by M = max m, l = sum 2^(c (m_i - M)) l_i, o likewise.  So a range can be any workgroup's: the shared keys are cut for all rows
+// of all sequences together, a sequence's own keys for its rows, and attn_join_kernel joins what a row has.
+//
+// A wavefront takes 32 keys at a time and keeps everything in registers, without LDS between the products:
+//   S^T = K Q^T by 16x16 matrix instructions: K is read as it lies (a lane has 16 bytes of one key), and a lane ends up with one query
+//   (lane % 16) and eight keys, 4 * (lane / 16) + 0..3 of both halves of the 32.  Maximum and sum of a query are over its own registers and two
+//   exchanges.
+//   O^T = V^T P^T: P^T's operand is wanted as (query, eight keys) in a lane: what the lane already has, when these keys are taken in its order.  V's is
+//   (d, the same eight keys): the lane reads DP/16 elements of each of the eight keys (a row of V over 16 lanes, whole lines) and
+//   pairs them up with one v_perm for two elements; element i of a lane's piece goes to product i, so 16 lanes' pieces make the d's of a product
+//   DP/16 apart, and a lane's results are contiguous in d again.
+#pragma once
+
+#include "atk_decode_common.h"
+
+namespace atk {
+
+constexpr float kNoMax = -__builtin_inff();
+constexpr int kAttnWaves = 4;      // of a workgroup: they take turns at the 32-key tiles of its range and join through LDS
+constexpr int kTileKeys = 32;
+constexpr float kLazyMax = 8.0f;   // the maximum that weights are taken relative to follows the true one when that is 2^8 above it: 2^8 times the largest weight is
+                                   // far from f32's and bf16's range, and rescaling is rare
+
+struct AttnDev {
+    const void *q, *k, *v;
+    void *out;
+    float *lse;
+    const int32_t *table, *lens, *seqs;
+    int32_t *status;
+    float *parts_o;    // [row][part][dim]
+    float2 *parts_ml;  // [row][part]
+    int64_t table_stride;
+    int64_t qs[3], os[3], ks[3], vs[3];
+    int batch, tokens, heads, kv_heads, group, dim;
+    int rows, row_pages, n_pages;
+    int prefix_len;
+    int prefix_splits, prefix_blocks, prefix_keys;  // ranges of the shared keys, row blocks, keys of a range (a multiple of a workgroup's tiles)
+    int own_splits, own_blocks;
+    int n_prefix;      // workgroups of the shared keys; those of own keys follow
+    int parts;         // prefix_splits + own_splits
+    FastDiv page;
+    float scale, scale2;  // scale2: scale * log2(e)
+};
+
+// Element types: a 16-byte piece of a row, its products, and a lane's weights as the second product takes them.
+template <int ELT>
+struct AttnElt;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+template <>
+struct AttnElt<ATK_BF16> {
+    static constexpr int kBytes = 2;
+    static constexpr float kBias = 0.0f;  // weights are 2^(s - m + kBias)
+    static constexpr uint32_t kExp = 0x7f807f80u;
+    static __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+    }
+};
+template <>
+struct AttnElt<ATK_F16> {
+    static constexpr int kBytes = 2;
+    // f16 has no exponents below -24: many weights of 2^-25 beside one of 1 would vanish, and their sum need not be small.  2^7 above them, and at most 2^15 with
+    // the lazy maximum, weights down to 2^-31 count.
+    static constexpr float kBias = 7.0f;
+    static constexpr uint32_t kExp = 0x7c007c00u;
+    static __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) {
+        typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
+    }
+};
+template <>
+struct AttnElt<ATK_F32> {
+    static constexpr int kBytes = 4;
+    static constexpr float kBias = 0.0f;
+    static constexpr uint32_t kExp = 0x7f800000u;
+    // a piece is four elements: four products of one k each per lane group
+    static __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
+        return c;
+    }
+};
+
+template <int ELT>
+__device__ __forceinline__ bool not_finite(uint32_t w) {
+    if (ELT == ATK_F32) return (w & 0x7f800000u) == 0x7f800000u;
+    constexpr uint32_t lo = AttnElt<ELT>::kExp & 0xffffu, hi = AttnElt<ELT>::kExp & 0xffff0000u;
+    return (w & lo) == lo || (w & hi) == hi;
+}
+
+// Eight rows of V as a lane has them: DVL elements each.
+template <int ELT, int DP>
+struct VRows {
+    static constexpr int kDvl = DP / 16;                                    // elements of a lane's piece of a row
+    static constexpr int kWords = kDvl * AttnElt<ELT>::kBytes / 4;          // 32-bit words of it
+    static constexpr int kVec = kWords % 4 == 0 ? 4 : 2;                    // words of a load
+    uint32_t w[8][kWords];
+
+    __device__ __forceinline__ void load(int j, const char *row, int n, int dim) {
+#pragma unroll
+        for (int x = 0; x < kWords; x += kVec) {
+            const int word = n * kWords + x;
+            if (DP * AttnElt<ELT>::kBytes / 4 == kVec || word * 4 < dim * AttnElt<ELT>::kBytes) {
+                if (kVec == 4) {
+                    u32x4 t = *(const u32x4 *)(row + word * 4);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) w[j][x + y] = t[y];
+                } else {
+                    u32x2 t = *(const u32x2 *)(row + word * 4);
+                    w[j][x] = t[0], w[j][x + 1] = t[1];
+                }
+            } else {
+#pragma unroll
+                for (int y = 0; y < kVec; ++y) w[j][x + y] = 0;
+            }
+        }
+    }
+    // the operand of product i in 16 bits: element i of all eight keys
+    __device__ __forceinline__ u32x4 operand(int i) const {
+        u32x4 r;
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+            r[p] = __builtin_amdgcn_perm(w[2 * p + 1][i / 2], w[2 * p][i / 2], (i & 1) ? 0x07060302u : 0x05040100u);
+        return r;
+    }
+    __device__ __forceinline__ bool any_not_finite() const {
+        bool bad = false;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int x = 0; x < kWords; ++x) bad |= not_finite<ELT>(w[j][x]);
+        return bad;
+    }
+};
+
+// A lane's eight weights as an operand.
+template <int ELT>
+struct Weights {
+    u32x4 w[ELT == ATK_F32 ? 2 : 1];
+    __device__ __forceinline__ void set(const f32x4 &a, const f32x4 &b) {
+        if constexpr (ELT == ATK_F32) {
+            w[0] = __builtin_bit_cast(u32x4, a), w[1] = __builtin_bit_cast(u32x4, b);
+        } else {
+            w[0] = u32x4{AttnElt<ELT>::pack(a[0], a[1]), AttnElt<ELT>::pack(a[2], a[3]), AttnElt<ELT>::pack(b[0], b[1]), AttnElt<ELT>::pack(b[2], b[3])};
+        }
+    }
+};
+
+template <int ELT, int DP>
+__device__ __forceinline__ f32x4 mma_pv(const VRows<ELT, DP> &v, int i, const Weights<ELT> &p, f32x4 c) {
+    if constexpr (ELT == ATK_F32) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v.w[j][i]), __uint_as_float(p.w[j / 4][j % 4]), c, 0, 0, 0);
+        return c;
+    } else {
+        return AttnElt<ELT>::mma(v.operand(i), p.w[0], c);
+    }
+}
+
+// Row r of the rows that read head h of a range: where its query lies, and how many keys it sees.
+struct AttnRow {
+    int b, t, head;
+};
+__device__ __forceinline__ AttnRow attn_row(const AttnDev &a, int h, int r, int own_b) {
+    AttnRow x;
+    const int g = r % a.group, bt = r / a.group;
+    x.head = h * a.group + g;
+    if (own_b >= 0) {
+        x.b = own_b, x.t = bt;
+    } else {
+        x.b = bt / a.tokens, x.t = bt - x.b * a.tokens;
+    }
+    return x;
+}
+// keys of sequence b (0 for a row number or a length that is out of range)
+__device__ __forceinline__ int seq_row(const AttnDev &a, int b, bool *bad) {
+    const int s = a.seqs ? a.seqs[b] : b;
+    if ((unsigned)s < (unsigned)a.rows) return s;
+    *bad = true;
+    return -1;
+}
+__device__ __forceinline__ int seq_len(const AttnDev &a, int row, bool *bad) {
+    if (row < 0) return 0;
+    const int len = a.lens[row];
+    const int64_t most = (int64_t)a.row_pages * a.page.d;
+    if (len >= 0 && len <= most) return len;
+    *bad = true;
+    return len < 0 ? 0 : (int)most;
+}
+
+template <int ELT, int DP, int RT>
+__device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int n_rows, int own_b, const int32_t *table_row, int ka, int kb, int part, char *lds) {
+    typedef AttnElt<ELT> E;
+    constexpr int kPiece = 16 / E::kBytes;            // elements of 16 bytes
+    constexpr int NC = DP / (4 * kPiece);             // 16-byte pieces of a row that a lane has
+    constexpr int NT = DP / 16;                       // products along d
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n = lane & 15, g = lane >> 4;
+
+    u32x4 q[RT][NC];
+    int lim[RT];
+    int min_lim = kb;
+    bool bad_len = false, bad_seq = false, bad_page = false;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = r0 + rt * 16 + n;
+        const bool real = r < n_rows;
+        const AttnRow x = attn_row(a, h, real ? r : 0, own_b);
+        const int len = seq_len(a, seq_row(a, x.b, &bad_seq), &bad_len);
+        // rows past the end are computed as if they saw all keys, and not written: they must not make tiles masked
+        lim[rt] = real ? min(kb, len - (a.tokens - 1 - x.t)) : kb;
+        min_lim = min(min_lim, lim[rt]);
+        const char *p = (const char *)a.q + (x.b * a.qs[0] + x.t * a.qs[1] + x.head * a.qs[2]) * E::kBytes;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int at = (c * 4 + g) * 16;
+            q[rt][c] = at < a.dim * E::kBytes ? *(const u32x4 *)(p + at) : u32x4{0, 0, 0, 0};
+        }
+    }
+    for (int w = 1; w < 16; w <<= 1) min_lim = min(min_lim, __shfl_xor(min_lim, w, 64));
+
+    float m[RT], l[RT];  // maximum, in units of s: c * s need not be finite where s is
+    bool far = false;    // ... and is not for some query of the wavefront
+    f32x4 acc[RT][NT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m[rt] = kNoMax, l[rt] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) acc[rt][i] = f32x4{0, 0, 0, 0};
+    }
+    const char *kh = (const char *)a.k + h * a.ks[2] * E::kBytes, *vh = (const char *)a.v + h * a.vs[2] * E::kBytes;
+
+    for (int k0 = ka + wave * kTileKeys; k0 < kb; k0 += kAttnWaves * kTileKeys) {
+        // lane j (and j + 32) looks key k0 + j up; keys past the end are read as the last one and masked
+        int page = table_row[a.page.div(min(k0 + (lane & 31), kb - 1))];
+        const bool good = (unsigned)page < (unsigned)a.n_pages;
+        bad_page |= !good;
+        if (!good) page = 0;
+        const uint32_t valid = (uint32_t)__ballot(good);
+
+        u32x4 kf[2][NC];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int key = min(k0 + x * 16 + n, kb - 1);
+            const char *row = kh + (__shfl(page, x * 16 + n, 64) * a.ks[0] + a.page.mod(key) * a.ks[1]) * E::kBytes;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int at = (c * 4 + g) * 16;
+                kf[x][c] = at < a.dim * E::kBytes ? *(const u32x4 *)(row + at) : u32x4{0, 0, 0, 0};
+            }
+        }
+        VRows<ELT, DP> v;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int at = (j / 4) * 16 + g * 4 + j % 4;
+            const int key = min(k0 + at, kb - 1);
+            const char *row = vh + (__shfl(page, at, 64) * a.vs[0] + a.page.mod(key) * a.vs[1]) * E::kBytes;
+            v.load(j, row, n, a.dim);
+        }
+        f32x4 s[RT][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                s[rt][x] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int c = 0; c < NC; ++c) s[rt][x] = E::mma(kf[x][c], q[rt][c], s[rt][x]);
+            }
+        const bool masked = k0 + kTileKeys > min_lim || valid != 0xffffffffu;
+        bool apart = false;  // a value that is not finite beside a mask: 0 * it would not be 0
+        if (masked) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int at = x * 16 + g * 4 + j;
+                        if (k0 + at >= lim[rt] || !(valid >> at & 1)) s[rt][x][j] = kNoMax;
+                    }
+            apart = __any(v.any_not_finite());
+        }
+        float top[RT];
+        bool raise = false;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float t = fmaxf(fmaxf(fmaxf(s[rt][0][0], s[rt][0][1]), fmaxf(s[rt][0][2], s[rt][0][3])), fmaxf(fmaxf(s[rt][1][0], s[rt][1][1]), fmaxf(s[rt][1][2], s[rt][1][3])));
+            t = fmaxf(t, __shfl_xor(t, 16, 64));
+            t = fmaxf(t, __shfl_xor(t, 32, 64));
+            top[rt] = t;
+            raise |= (t - m[rt]) * a.scale2 > kLazyMax;
+        }
+        if (__any(raise)) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const float to = fmaxf(m[rt], top[rt]);
+                const float f = __builtin_amdgcn_exp2f((m[rt] - to) * a.scale2);
+                if (m[rt] != kNoMax) {  // (else nothing is kept yet)
+                    l[rt] *= f;
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) acc[rt][i] *= f;
+                }
+                m[rt] = to;
+                far |= fabsf(to) < __builtin_inff() && !(fabsf(to * a.scale2) < __builtin_inff());
+            }
+            far = __any(far);
+        }
+        Weights<ELT> p[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const float zero = m[rt] == kNoMax ? 0.0f : m[rt];
+            const float ref = zero * a.scale2 - E::kBias;
+            float sum = 0.0f;
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float e = __builtin_amdgcn_exp2f(far ? fmaf(s[rt][x][j] - zero, a.scale2, E::kBias) : fmaf(s[rt][x][j], a.scale2, -ref));
+                    s[rt][x][j] = e;
+                    sum += e;
+                }
+            l[rt] += sum;
+            p[rt].set(s[rt][0], s[rt][1]);
+        }
+        if (!apart) {
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) acc[rt][i] = mma_pv<ELT, DP>(v, i, p[rt], acc[rt][i]);
+        } else {
+            // query by query, with the values it does not see at 0; a product's columns are queries of their own
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+                for (int c = 0; c < 16; ++c) {
+                    const int limit = __shfl(lim[rt], c, 64);
+                    VRows<ELT, DP> u = v;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int at = (j / 4) * 16 + g * 4 + j % 4;
+                        if (k0 + at >= limit || !(valid >> at & 1))
+#pragma unroll
+                            for (int x = 0; x < VRows<ELT, DP>::kWords; ++x) u.w[j][x] = 0;
+                    }
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) {
+                        const f32x4 t = mma_pv<ELT, DP>(u, i, p[rt], acc[rt][i]);
+                        if (n == c) acc[rt][i] = t;
+                    }
+                }
+        }
+    }
+    const int bad = (bad_page ? ATK_STATUS_BAD_PAGE : 0) | (bad_seq ? ATK_STATUS_BAD_SEQ : 0) | (bad_len ? ATK_STATUS_BAD_LEN : 0);
+    if (bad && a.status) atomicOr(a.status, bad);
+
+    // the wavefronts' ranges join in LDS, in their order
+    float *ls_m = (float *)lds, *ls_l = ls_m + kAttnWaves * RT * 16, *ls_o = ls_l + kAttnWaves * RT * 16;
+    constexpr int kPitch = DP + 4;
+    float total[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        l[rt] += __shfl_xor(l[rt], 16, 64);
+        l[rt] += __shfl_xor(l[rt], 32, 64);
+        if (g == 0) ls_m[(wave * RT + rt) * 16 + n] = m[rt], ls_l[(wave * RT + rt) * 16 + n] = l[rt];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        float to = kNoMax;
+        for (int w = 0; w < kAttnWaves; ++w) to = fmaxf(to, ls_m[(w * RT + rt) * 16 + n]);
+        total[rt] = 0.0f;
+        for (int w = 0; w < kAttnWaves; ++w) {
+            const float mw = ls_m[(w * RT + rt) * 16 + n];
+            total[rt] += ls_l[(w * RT + rt) * 16 + n] * (mw == kNoMax ? 1.0f : __builtin_amdgcn_exp2f((mw - to) * a.scale2));
+        }
+        if (m[rt] != kNoMax) {
+            const float f = __builtin_amdgcn_exp2f((m[rt] - to) * a.scale2);
+#pragma unroll
+            for (int i = 0; i < NT; ++i) acc[rt][i] *= f;
+        }
+        m[rt] = to;
+    }
+    for (int w = 0; w < kAttnWaves; ++w) {
+        if (wave == w) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float *o = ls_o + (rt * 16 + n) * kPitch + (g * 4 + j) * NT + i;
+                        if (w > 0) acc[rt][i][j] += *o;
+                        if (w < kAttnWaves - 1) *o = acc[rt][i][j];
+                    }
+        }
+        __syncthreads();
+    }
+    if (wave != kAttnWaves - 1) return;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = r0 + rt * 16 + n;
+        if (r >= n_rows) continue;
+        const AttnRow x = attn_row(a, h, r, own_b);
+        const int64_t row = ((int64_t)x.b * a.tokens + x.t) * a.heads + x.head;
+        if (g == 0) a.parts_ml[row * a.parts + part] = float2{m[rt], total[rt]};
+        float *o = a.parts_o + (row * a.parts + part) * a.dim;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < NT; i += 4) {
+                const int d = (g * 4 + j) * NT + i;
+                if (d < a.dim) *(f32x4 *)(o + d) = f32x4{acc[rt][i][j], acc[rt][i + 1][j], acc[rt][i + 2][j], acc[rt][i + 3][j]};
+            }
+    }
+}
+
+template <int DP, int RT>
+constexpr int attn_lds_bytes() { return 2 * kAttnWaves * RT * 16 * 4 + RT * 16 * (DP + 4) * 4; }
+
+template <int ELT, int DP, int RT>
+__global__ __launch_bounds__(kAttnWaves * 64) void attn_range_kernel(const AttnDev a) {
+    __shared__ __align__(16) char lds[attn_lds_bytes<DP, RT>()];
+    const int id = blockIdx.x;
+    bool bad = false;
+    if (id < a.n_prefix) {
+        // heads side by side: with eight of them, each XCD's L2 holds one head's keys
+        const int h = id % a.kv_heads, x = id / a.kv_heads;
+        const int block = x % a.prefix_blocks, split = x / a.prefix_blocks;
+        const int row = seq_row(a, 0, &bad);
+        const int ka = split * a.prefix_keys, kb = row < 0 ? ka : min(a.prefix_len, ka + a.prefix_keys);
+        attn_range<ELT, DP, RT>(a, h, block * RT * 16, a.batch * a.tokens * a.group, -1, a.table + row * a.table_stride, ka, kb, split, lds);
+    } else {
+        const int y = id - a.n_prefix;
+        const int h = y % a.kv_heads;
+        int x = y / a.kv_heads;
+        const int block = x % a.own_blocks;
+        x /= a.own_blocks;
+        const int b = x % a.batch, split = x / a.batch;
+        const int row = seq_row(a, b, &bad), len = seq_len(a, row, &bad);
+        const int keys = max(0, len - a.prefix_len);
+        constexpr int kStep = kAttnWaves * kTileKeys;
+        const int per = (int)(((int64_t)keys + a.own_splits * kStep - 1) / (a.own_splits * kStep)) * kStep;
+        const int64_t from = a.prefix_len + (int64_t)split * per;
+        const int ka = (int)min((int64_t)len, from), kb = (int)min((int64_t)len, from + per);
+        attn_range<ELT, DP, 1>(a, h, block * 16, a.tokens * a.group, b, a.table + row * a.table_stride, ka, max(ka, kb), a.prefix_splits + split, lds);
+    }
+}
+
+hipError_t launch_attn_bf16(const AttnDev &a, int dp, int rt, int64_t grid, hipStream_t stream);
+hipError_t launch_attn_f16(const AttnDev &a, int dp, int rt, int64_t grid, hipStream_t stream);
+hipError_t launch_attn_f32(const AttnDev &a, int dp, int rt, int64_t grid, hipStream_t stream);
+
+// 16-row tiles of a workgroup's rows that the kernel is built for: registers hold Q, K, V and O of RT tiles, up to 512 words of a lane
+constexpr int attn_max_rt(int elt, int dp) {
+    return elt == ATK_F32 ? (dp <= 128 ? 2 : 1) : (dp <= 128 ? 4 : 2);
+}
+
+template <int ELT, int DP>
+hipError_t launch_attn_dp(const AttnDev &a, int rt, int64_t grid, hipStream_t stream) {
+    const dim3 threads(kAttnWaves * 64);
+    if constexpr (attn_max_rt(ELT, DP) >= 4)
+        if (rt == 4) {
+            hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 4>), dim3((uint32_t)grid), threads, 0, stream, a);
+            return hipGetLastError();
+        }
+    if constexpr (attn_max_rt(ELT, DP) >= 2)
+        if (rt == 2) {
+            hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 2>), dim3((uint32_t)grid), threads, 0, stream, a);
+            return hipGetLastError();
+        }
+    hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 1>), dim3((uint32_t)grid), threads, 0, stream, a);
+    return hipGetLastError();
+}
+template <int ELT>
+hipError_t launch_attn(const AttnDev &a, int dp, int rt, int64_t grid, hipStream_t stream) {
+    if (dp == 64) return launch_attn_dp<ELT, 64>(a, rt, grid, stream);
+    if (dp == 128) return launch_attn_dp<ELT, 128>(a, rt, grid, stream);
+    if (dp == 192) return launch_attn_dp<ELT, 192>(a, rt, grid, stream);
+    return launch_attn_dp<ELT, 256>(a, rt, grid, stream);
+}
+
+}  // namespace atk
