@@ -61,7 +61,7 @@ static hipError_t launch_join(const AttnDev &a, int dp, hipStream_t stream) {
 }
 
 struct AttnPlan {
-    int dp, rt, prefix_splits, prefix_blocks, prefix_keys, own_splits, own_blocks;
+    int dp, rt, waves, prefix_splits, prefix_blocks, prefix_keys, own_splits, own_blocks;
     int64_t grid, rows, parts, o_bytes, bytes;
 };
 
@@ -97,23 +97,31 @@ static int plan_attention(const atk_attention_args *p, AttnPlan *pl) {
     const int group = (int)(p->heads / p->kv_heads);
     pl->dp = p->dim <= 64 ? 64 : p->dim <= 128 ? 128 : p->dim <= 192 ? 192 : 256;
     const int64_t rows = p->batch * p->tokens * group, own_rows = p->tokens * group;
-    pl->rt = 1;
-    while (pl->rt < attn_max_rt(p->dtype, pl->dp) && rows > 16 * pl->rt) pl->rt *= 2;
-    constexpr int64_t kStep = kAttnWaves * kTileKeys, kWanted = 2 * kNumCU;
-    pl->prefix_blocks = (int)attn_ceil(rows, 16 * pl->rt);
+    // how the shared keys meet the rows: up to two 16-row tiles in every wavefront, or 32 rows a wavefront and keys by way of LDS
+    pl->rt = rows <= 16 || p->prefix_len == 0 ? 1 : 2, pl->waves = kAttnWaves;
+    int64_t block = 16 * pl->rt, step = kAttnWaves * kTileKeys;
+    int64_t wanted = 2 * kNumCU;
+    if (rows > 32 && p->dtype != ATK_F32 && p->prefix_len > 0) {
+        pl->rt = 0, pl->waves = rows <= 128 ? 4 : attn_max_waves(pl->dp);
+        block = 32 * pl->waves, step = kBlockKeys;
+        wanted = pl->waves == 8 ? kNumCU : 2 * kNumCU;
+    } else if (pl->rt > attn_max_rt(p->dtype, pl->dp)) {
+        pl->rt = 1, block = 16;
+    }
+    pl->prefix_blocks = (int)attn_ceil(rows, block);
     const int64_t base = pl->prefix_blocks * p->kv_heads;
     pl->prefix_splits = 0, pl->prefix_keys = 0;
     if (p->prefix_len > 0) {
-        const int64_t steps = attn_ceil(p->prefix_len, kStep);
-        const int64_t splits = std::min(steps, std::max<int64_t>(1, kWanted / base));
-        pl->prefix_keys = (int)(attn_ceil(steps, splits) * kStep);
+        const int64_t steps = attn_ceil(p->prefix_len, step);
+        const int64_t splits = std::min(steps, std::max<int64_t>(1, wanted / base));
+        pl->prefix_keys = (int)(attn_ceil(steps, splits) * step);
         pl->prefix_splits = (int)attn_ceil(p->prefix_len, pl->prefix_keys);
     }
     // a sequence's own keys: as many as its row could hold, the device knows how many there are
     const int64_t own = p->row_pages * p->page_size - p->prefix_len;
     pl->own_blocks = (int)attn_ceil(own_rows, 16);
     const int64_t own_base = p->batch * p->kv_heads * pl->own_blocks;
-    pl->own_splits = own > 0 ? (int)std::min(attn_ceil(own, kStep), std::max<int64_t>(1, kWanted / own_base)) : 0;
+    pl->own_splits = own > 0 ? (int)std::min(attn_ceil(own, pl->waves * kTileKeys), std::max<int64_t>(1, wanted / own_base)) : 0;
     pl->rows = p->batch * p->tokens * p->heads;
     pl->parts = pl->prefix_splits + pl->own_splits;
     pl->grid = base * pl->prefix_splits + own_base * pl->own_splits;
@@ -161,9 +169,9 @@ int atk_shared_prefix_attention(const atk_attention_args *p, void *work, int64_t
     a.scale = (float)p->scale;
     a.scale2 = (float)(p->scale * 1.4426950408889634);
     hipStream_t s = (hipStream_t)stream;
-    hipError_t e = p->dtype == ATK_F32    ? launch_attn_f32(a, pl.dp, pl.rt, pl.grid, s)
-                   : p->dtype == ATK_BF16 ? launch_attn_bf16(a, pl.dp, pl.rt, pl.grid, s)
-                                          : launch_attn_f16(a, pl.dp, pl.rt, pl.grid, s);
+    hipError_t e = p->dtype == ATK_F32    ? launch_attn_f32(a, pl.dp, pl.rt, pl.waves, pl.grid, s)
+                   : p->dtype == ATK_BF16 ? launch_attn_bf16(a, pl.dp, pl.rt, pl.waves, pl.grid, s)
+                                          : launch_attn_f16(a, pl.dp, pl.rt, pl.waves, pl.grid, s);
     if (e == hipSuccess)
         e = p->dtype == ATK_F32    ? launch_join<ATK_F32>(a, pl.dp, s)
             : p->dtype == ATK_BF16 ? launch_join<ATK_BF16>(a, pl.dp, s)

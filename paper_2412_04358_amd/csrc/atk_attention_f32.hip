@@ -1,6 +1,6 @@
-// Instances of attn_range_kernel for f32.
+// Instances of the attention kernels for f32.
 #include "atk_attention_kernel.h"
 
 namespace atk {
-hipError_t launch_attn_f32(const AttnDev &a, int dp, int rt, int64_t grid, hipStream_t stream) { return launch_attn<ATK_F32>(a, dp, rt, grid, stream); }
+hipError_t launch_attn_f32(const AttnDev &a, int dp, int rt, int waves, int64_t grid, hipStream_t stream) { return launch_attn<ATK_F32>(a, dp, rt, waves, grid, stream); }
 }  // namespace atk

@@ -19,7 +19,7 @@
 namespace atk {
 
 constexpr float kNoMax = -__builtin_inff();
-constexpr int kAttnWaves = 4;      // of a workgroup: they take turns at the 32-key tiles of its range and join through LDS
+constexpr int kAttnWaves = 4;      // of a workgroup of attn_range_kernel: they take turns at the 32-key tiles of its range and join through LDS
 constexpr int kTileKeys = 32;
 constexpr float kLazyMax = 8.0f;   // the maximum that weights are taken relative to follows the true one when that is 2^8 above it: 2^8 times the largest weight is
                                    // far from f32's and bf16's range, and rescaling is rare
@@ -205,7 +205,7 @@ __device__ __forceinline__ int seq_len(const AttnDev &a, int row, bool *bad) {
     return len < 0 ? 0 : (int)most;
 }
 
-template <int ELT, int DP, int RT>
+template <int ELT, int DP, int RT, int NW>
 __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int n_rows, int own_b, const int32_t *table_row, int ka, int kb, int part, char *lds) {
     typedef AttnElt<ELT> E;
     constexpr int kPiece = 16 / E::kBytes;            // elements of 16 bytes
@@ -247,7 +247,7 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
     }
     const char *kh = (const char *)a.k + h * a.ks[2] * E::kBytes, *vh = (const char *)a.v + h * a.vs[2] * E::kBytes;
 
-    for (int k0 = ka + wave * kTileKeys; k0 < kb; k0 += kAttnWaves * kTileKeys) {
+    for (int k0 = ka + wave * kTileKeys; k0 < kb; k0 += NW * kTileKeys) {
         // lane j (and j + 32) looks key k0 + j up; keys past the end are read as the last one and masked
         int page = table_row[a.page.div(min(k0 + (lane & 31), kb - 1))];
         const bool good = (unsigned)page < (unsigned)a.n_pages;
@@ -370,7 +370,7 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
     if (bad && a.status) atomicOr(a.status, bad);
 
     // the wavefronts' ranges join in LDS, in their order
-    float *ls_m = (float *)lds, *ls_l = ls_m + kAttnWaves * RT * 16, *ls_o = ls_l + kAttnWaves * RT * 16;
+    float *ls_m = (float *)lds, *ls_l = ls_m + NW * RT * 16, *ls_o = ls_l + NW * RT * 16;
     constexpr int kPitch = DP + 4;
     float total[RT];
 #pragma unroll
@@ -383,9 +383,9 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         float to = kNoMax;
-        for (int w = 0; w < kAttnWaves; ++w) to = fmaxf(to, ls_m[(w * RT + rt) * 16 + n]);
+        for (int w = 0; w < NW; ++w) to = fmaxf(to, ls_m[(w * RT + rt) * 16 + n]);
         total[rt] = 0.0f;
-        for (int w = 0; w < kAttnWaves; ++w) {
+        for (int w = 0; w < NW; ++w) {
             const float mw = ls_m[(w * RT + rt) * 16 + n];
             total[rt] += ls_l[(w * RT + rt) * 16 + n] * (mw == kNoMax ? 1.0f : __builtin_amdgcn_exp2f((mw - to) * a.scale2));
         }
@@ -396,7 +396,7 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
         }
         m[rt] = to;
     }
-    for (int w = 0; w < kAttnWaves; ++w) {
+    for (int w = 0; w < NW; ++w) {
         if (wave == w) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
@@ -406,12 +406,12 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
                     for (int j = 0; j < 4; ++j) {
                         float *o = ls_o + (rt * 16 + n) * kPitch + (g * 4 + j) * NT + i;
                         if (w > 0) acc[rt][i][j] += *o;
-                        if (w < kAttnWaves - 1) *o = acc[rt][i][j];
+                        if (w < NW - 1) *o = acc[rt][i][j];
                     }
         }
         __syncthreads();
     }
-    if (wave != kAttnWaves - 1) return;
+    if (wave != NW - 1) return;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const int r = r0 + rt * 16 + n;
@@ -430,69 +430,348 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
     }
 }
 
-template <int DP, int RT>
-constexpr int attn_lds_bytes() { return 2 * kAttnWaves * RT * 16 * 4 + RT * 16 * (DP + 4) * 4; }
 
+// ------------------------------------------------------------------------------------ many rows on shared keys, 16-bit types
+//
+// With more rows than a tile or two the shared keys are bound by the matrix units and the exponentials, so a key's data should come to a wavefront once for
+// 32 rows and to a CU once for all of its rows: a workgroup's NW wavefronts have 32 rows each, and 64 keys at a time pass through LDS, in two
+// buffers - the next tile is written to the other one while this one is worked on, from loads that were given out a tile earlier.
+//   S^T = K Q^T and O^T = V^T P^T by 32x32x16 matrix instructions, half the operands' reads of 16x16x32 for a product.  A lane has one query (lane % 32) and of
+//   each 32 keys those with 8 * i + 4 * (lane / 32) + 0..3; step s of the second product takes i = 2 s and 2 s + 1.
+//   V lies in LDS by d, a lane's eight keys of a step side by side: transposed in registers on the way in (a lane has loaded two d's of eight keys), so that
+//   both operands are single 16-byte reads.  Rows in LDS are 16 bytes longer than their data: lanes a row apart meet in different banks.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <int ELT>
+__device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c) {
+    if constexpr (ELT == ATK_BF16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+constexpr int kBlockKeys = 64;
+template <int DP>
+struct BlockLds {
+    static constexpr int kK = DP * 2 + 16;                 // bytes of a key's row of K
+    static constexpr int kV = kBlockKeys * 2 + 16;         // bytes of a d's row of V
+    static constexpr int kBuffer = kBlockKeys * kK + DP * kV;
+    static constexpr int kBytes = 2 * kBuffer;
+};
+
+// Rows r0 .. r0 + 32 * NW - 1 of head h against keys ka .. kb - 1, all of which every one of these rows sees.
+template <int ELT, int DP, int NW>
+__device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int n_rows, const int32_t *table_row, int ka, int kb, int part, char *lds) {
+    typedef AttnElt<ELT> E;
+    typedef BlockLds<DP> L;
+    constexpr int NS = DP / 16;                            // steps of the first product
+    constexpr int ND = DP / 32;                            // tiles of d
+    constexpr int KC = kBlockKeys * DP / 8 / (NW * 64);    // 16-byte pieces of K that a thread brings in
+    constexpr int PL = DP / 2;                             // lanes of a row of V, two d's each
+    constexpr bool kOneGroup = PL % 64 == 0;               // a wavefront's load is of one group of eight keys
+    constexpr bool kSpare = 8 * PL < NW * 64;              // ... the last wavefronts bring in none of V
+    constexpr int VC = kSpare ? 1 : 8 * PL / (NW * 64);    // ... loads of eight keys of a thread
+    static_assert(KC >= 1, "every thread has its share");
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n = lane & 31, g = lane >> 5;
+    const char *kh = (const char *)a.k + h * a.ks[2] * 2, *vh = (const char *)a.v + h * a.vs[2] * 2;
+
+    // what a thread brings in: piece (wave * 64 + lane) + c * NW * 64 of K; group of eight keys and two d's of V
+    int k_key[KC], k_piece[KC], v_group[VC], v_d[VC];
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+        const int id = c * NW * 64 + threadIdx.x;
+        k_key[c] = id / (DP / 8), k_piece[c] = id % (DP / 8);
+    }
+#pragma unroll
+    for (int c = 0; c < VC; ++c) {
+        const int id = c * NW * 64 + threadIdx.x;
+        v_group[c] = id / PL, v_d[c] = id % PL * 2;
+    }
+    u32x4 kr[KC];
+    uint32_t vr[VC][8];
+    uint32_t valid_next = 0xffffffffu, valid_next2 = 0xffffffffu;  // of the keys of a tile's halves
+    bool bad_page = false;
+    auto look_up = [&](int k0) -> int {  // lane j: the page of key k0 + j; keys past the end are read as the last one
+        return k0 < kb ? table_row[a.page.div(min(k0 + lane, kb - 1))] : 0;
+    };
+    auto load = [&](int k0, int page) {
+        const int key = min(k0 + lane, kb - 1);
+        const bool good = (unsigned)page < (unsigned)a.n_pages;
+        bad_page |= !good;
+        const uint64_t votes = __ballot(good && k0 + lane < kb);
+        valid_next = (uint32_t)votes, valid_next2 = (uint32_t)(votes >> 32);
+        const int64_t p = good ? page : 0, slot = a.page.mod(key);
+        const int64_t ko = (p * a.ks[0] + slot * a.ks[1]) * 2, vo = (p * a.vs[0] + slot * a.vs[1]) * 2;
+        const int klo = (int)ko, khi = (int)(ko >> 32), vlo = (int)vo, vhi = (int)(vo >> 32);
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+            const int64_t at = (int64_t)(((uint64_t)(uint32_t)__shfl(khi, k_key[c], 64) << 32) | (uint32_t)__shfl(klo, k_key[c], 64));
+            kr[c] = k_piece[c] * 8 < a.dim ? *(const u32x4 *)(kh + at + k_piece[c] * 16) : u32x4{0, 0, 0, 0};
+        }
+        if (kSpare && wave * 64 >= 8 * PL) return;
+#pragma unroll
+        for (int c = 0; c < VC; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                // group (x, s, half): keys 32 x + 16 s + 8 (j / 4) + 4 half + j % 4
+                const int who = (v_group[c] >> 1) * 16 + (j >> 2) * 8 + (v_group[c] & 1) * 4 + (j & 3);
+                int lo, hi;
+                if constexpr (kOneGroup) {  // its addresses are scalars
+                    const int one = __builtin_amdgcn_readfirstlane(who);
+                    lo = __builtin_amdgcn_readlane(vlo, one), hi = __builtin_amdgcn_readlane(vhi, one);
+                } else {
+                    lo = __shfl(vlo, who, 64), hi = __shfl(vhi, who, 64);
+                }
+                const int64_t at = (int64_t)(((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo);
+                vr[c][j] = v_d[c] < a.dim ? *(const uint32_t *)(vh + at + v_d[c] * 2) : 0u;
+            }
+    };
+    auto store = [&](char *buffer) {
+#pragma unroll
+        for (int c = 0; c < KC; ++c) *(u32x4 *)(buffer + k_key[c] * L::kK + k_piece[c] * 16) = kr[c];
+        if (kSpare && wave * 64 >= 8 * PL) return;
+        char *v = buffer + kBlockKeys * L::kK;
+#pragma unroll
+        for (int c = 0; c < VC; ++c) {
+            u32x4 even, odd;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                even[j] = __builtin_amdgcn_perm(vr[c][2 * j + 1], vr[c][2 * j], 0x05040100u);
+                odd[j] = __builtin_amdgcn_perm(vr[c][2 * j + 1], vr[c][2 * j], 0x07060302u);
+            }
+            *(u32x4 *)(v + v_d[c] * L::kV + v_group[c] * 16) = even;
+            *(u32x4 *)(v + (v_d[c] + 1) * L::kV + v_group[c] * 16) = odd;
+        }
+    };
+
+    const int r = r0 + wave * 32 + n;
+    const bool real = r < n_rows;
+    const AttnRow x = attn_row(a, h, real ? r : 0, -1);
+    u32x4 q[NS];
+    {
+        const char *p = (const char *)a.q + (x.b * a.qs[0] + x.t * a.qs[1] + x.head * a.qs[2]) * 2;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const int at = (s * 2 + g) * 16;
+            q[s] = at < a.dim * 2 ? *(const u32x4 *)(p + at) : u32x4{0, 0, 0, 0};
+        }
+    }
+    float m = kNoMax, l = 0.0f;
+    bool far = false;
+    f32x16 acc[ND];
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
+
+    load(ka, look_up(ka));
+    int page = look_up(ka + kBlockKeys);
+    uint32_t valid[2];
+    int at = 0;
+    store(lds);
+    valid[0] = valid_next, valid[1] = valid_next2;
+    load(ka + kBlockKeys, page);
+    page = look_up(ka + 2 * kBlockKeys);
+    __syncthreads();
+    for (int k0 = ka; k0 < kb; k0 += kBlockKeys) {
+        const char *kl = lds + at * L::kBuffer, *vl = kl + kBlockKeys * L::kK;
+        at ^= 1;
+        const uint32_t now[2] = {valid[0], valid[1]};
+        if (k0 + kBlockKeys < kb) {
+            store(lds + at * L::kBuffer);
+            valid[0] = valid_next, valid[1] = valid_next2;
+            load(k0 + 2 * kBlockKeys, page);
+            page = look_up(k0 + 3 * kBlockKeys);
+        }
+        f32x16 s[2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[y][j] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NS; ++i) s[y] = mma32<ELT>(*(const u32x4 *)(kl + (y * 32 + n) * L::kK + (i * 2 + g) * 16), q[i], s[y]);
+        }
+        if ((now[0] & now[1]) != 0xffffffffu) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (!(now[y] >> (8 * (j >> 2) + 4 * g + (j & 3)) & 1)) s[y][j] = kNoMax;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, s[y][j]);
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        if (__any((top - m) * a.scale2 > kLazyMax)) {
+            const float to = fmaxf(m, top);
+            const float f = __builtin_amdgcn_exp2f((m - to) * a.scale2);
+            if (m != kNoMax) {
+                l *= f;
+#pragma unroll
+                for (int i = 0; i < ND; ++i) acc[i] *= f;
+            }
+            m = to;
+            far = __any(fabsf(to) < __builtin_inff() && !(fabsf(to * a.scale2) < __builtin_inff()));
+        }
+        const float zero = m == kNoMax ? 0.0f : m;
+        const float ref = zero * a.scale2 - E::kBias;
+        float sum = 0.0f;
+        if (far) {  // (as below behind the subtraction: 2^(0 * x + y))
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[y][j] = __builtin_amdgcn_exp2f(fmaf(s[y][j] - zero, a.scale2, E::kBias));
+        } else {
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[y][j] = __builtin_amdgcn_exp2f(fmaf(s[y][j], a.scale2, -ref));
+        }
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sum += s[y][j];
+        l += sum;
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const u32x4 p = {E::pack(s[y][8 * t], s[y][8 * t + 1]), E::pack(s[y][8 * t + 2], s[y][8 * t + 3]), E::pack(s[y][8 * t + 4], s[y][8 * t + 5]),
+                                 E::pack(s[y][8 * t + 6], s[y][8 * t + 7])};
+#pragma unroll
+                for (int i = 0; i < ND; ++i) acc[i] = mma32<ELT>(*(const u32x4 *)(vl + (i * 32 + n) * L::kV + (y * 4 + t * 2 + g) * 16), p, acc[i]);
+            }
+        __syncthreads();
+    }
+    if (bad_page && a.status) atomicOr(a.status, ATK_STATUS_BAD_PAGE);
+    l += __shfl_xor(l, 32, 64);
+    if (!real) return;
+    const int64_t row = ((int64_t)x.b * a.tokens + x.t) * a.heads + x.head;
+    if (g == 0) a.parts_ml[row * a.parts + part] = float2{m, l};
+    float *o = a.parts_o + (row * a.parts + part) * a.dim;
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int d = i * 32 + j * 8 + g * 4;
+            if (d < a.dim) *(f32x4 *)(o + d) = f32x4{acc[i][4 * j], acc[i][4 * j + 1], acc[i][4 * j + 2], acc[i][4 * j + 3]};
+        }
+}
+
+// Own keys of a sequence: workgroup y of those.
+template <int ELT, int DP, int NW>
+__device__ __forceinline__ void attn_own(const AttnDev &a, int y, char *lds) {
+    bool bad = false;  // (told by attn_range)
+    const int h = y % a.kv_heads;
+    int x = y / a.kv_heads;
+    const int block = x % a.own_blocks;
+    x /= a.own_blocks;
+    const int b = x % a.batch, split = x / a.batch;
+    const int row = seq_row(a, b, &bad), len = seq_len(a, row, &bad);
+    const int keys = max(0, len - a.prefix_len);
+    constexpr int kStep = NW * kTileKeys;
+    const int per = (int)(((int64_t)keys + a.own_splits * kStep - 1) / (a.own_splits * kStep)) * kStep;
+    const int64_t from = a.prefix_len + (int64_t)split * per;
+    const int ka = (int)min((int64_t)len, from), kb = (int)min((int64_t)len, from + per);
+    attn_range<ELT, DP, 1, NW>(a, h, block * 16, a.tokens * a.group, b, a.table + row * a.table_stride, ka, max(ka, kb), a.prefix_splits + split, lds);
+}
+
+template <int DP, int RT, int NW>
+constexpr int attn_lds_bytes() { return 2 * NW * RT * 16 * 4 + RT * 16 * (DP + 4) * 4; }
+
+// Few rows on the shared keys: the wavefronts of a workgroup share its keys out.
 template <int ELT, int DP, int RT>
 __global__ __launch_bounds__(kAttnWaves * 64) void attn_range_kernel(const AttnDev a) {
-    __shared__ __align__(16) char lds[attn_lds_bytes<DP, RT>()];
+    __shared__ __align__(16) char lds[attn_lds_bytes<DP, RT, kAttnWaves>()];
     const int id = blockIdx.x;
+    if (id >= a.n_prefix) {
+        attn_own<ELT, DP, kAttnWaves>(a, id - a.n_prefix, lds);
+        return;
+    }
+    // heads side by side: with eight of them, each XCD's L2 holds one head's keys
     bool bad = false;
-    if (id < a.n_prefix) {
-        // heads side by side: with eight of them, each XCD's L2 holds one head's keys
-        const int h = id % a.kv_heads, x = id / a.kv_heads;
-        const int block = x % a.prefix_blocks, split = x / a.prefix_blocks;
-        const int row = seq_row(a, 0, &bad);
-        const int ka = split * a.prefix_keys, kb = row < 0 ? ka : min(a.prefix_len, ka + a.prefix_keys);
-        attn_range<ELT, DP, RT>(a, h, block * RT * 16, a.batch * a.tokens * a.group, -1, a.table + row * a.table_stride, ka, kb, split, lds);
+    const int h = id % a.kv_heads, x = id / a.kv_heads;
+    const int block = x % a.prefix_blocks, split = x / a.prefix_blocks;
+    const int row = seq_row(a, 0, &bad);
+    const int ka = split * a.prefix_keys, kb = row < 0 ? ka : min(a.prefix_len, ka + a.prefix_keys);
+    attn_range<ELT, DP, RT, kAttnWaves>(a, h, block * RT * 16, a.batch * a.tokens * a.group, -1, a.table + row * a.table_stride, ka, kb, split, lds);
+}
+
+// Many: its wavefronts share its rows out.
+template <int ELT, int DP, int NW>
+__global__ __launch_bounds__(NW * 64, DP <= 128 ? 2 : 1) void attn_block_kernel(const AttnDev a) {
+    constexpr int kRangeBytes = attn_lds_bytes<DP, 1, NW>();
+    __shared__ __align__(16) char lds[BlockLds<DP>::kBytes > kRangeBytes ? BlockLds<DP>::kBytes : kRangeBytes];
+    const int id = blockIdx.x;
+    if (id >= a.n_prefix) {
+        attn_own<ELT, DP, NW>(a, id - a.n_prefix, lds);
+        return;
+    }
+    bool bad = false;
+    const int h = id % a.kv_heads, x = id / a.kv_heads;
+    const int block = x % a.prefix_blocks, split = x / a.prefix_blocks;
+    const int row = seq_row(a, 0, &bad), n_rows = a.batch * a.tokens * a.group, r0 = block * NW * 32;
+    const int ka = split * a.prefix_keys, kb = row < 0 ? ka : min(a.prefix_len, ka + a.prefix_keys);
+    const int32_t *table = a.table + row * a.table_stride;
+    // a row that sees only a part of these keys (a sequence that ends before them): tile by tile, with masks
+    bool all = true;
+    for (int r = r0 + threadIdx.x; r < min(n_rows, r0 + NW * 32); r += NW * 64) {
+        const AttnRow w = attn_row(a, h, r, -1);
+        if (seq_len(a, seq_row(a, w.b, &bad), &bad) - (a.tokens - 1 - w.t) < kb) all = false;
+    }
+    if (__syncthreads_and(all)) {
+        attn_block<ELT, DP, NW>(a, h, r0, n_rows, table, ka, kb, split, lds);
     } else {
-        const int y = id - a.n_prefix;
-        const int h = y % a.kv_heads;
-        int x = y / a.kv_heads;
-        const int block = x % a.own_blocks;
-        x /= a.own_blocks;
-        const int b = x % a.batch, split = x / a.batch;
-        const int row = seq_row(a, b, &bad), len = seq_len(a, row, &bad);
-        const int keys = max(0, len - a.prefix_len);
-        constexpr int kStep = kAttnWaves * kTileKeys;
-        const int per = (int)(((int64_t)keys + a.own_splits * kStep - 1) / (a.own_splits * kStep)) * kStep;
-        const int64_t from = a.prefix_len + (int64_t)split * per;
-        const int ka = (int)min((int64_t)len, from), kb = (int)min((int64_t)len, from + per);
-        attn_range<ELT, DP, 1>(a, h, block * 16, a.tokens * a.group, b, a.table + row * a.table_stride, ka, max(ka, kb), a.prefix_splits + split, lds);
+        for (int t = 0; t < NW * 2; ++t) {
+            __syncthreads();
+            attn_range<ELT, DP, 1, NW>(a, h, r0 + t * 16, n_rows, -1, table, ka, kb, split, lds);
+        }
     }
 }
 
-hipError_t launch_attn_bf16(const AttnDev &a, int dp, int rt, int64_t grid, hipStream_t stream);
-hipError_t launch_attn_f16(const AttnDev &a, int dp, int rt, int64_t grid, hipStream_t stream);
-hipError_t launch_attn_f32(const AttnDev &a, int dp, int rt, int64_t grid, hipStream_t stream);
+// rt: 16-row tiles of a workgroup of attn_range_kernel; 0: attn_block_kernel, waves of 32 rows
+hipError_t launch_attn_bf16(const AttnDev &a, int dp, int rt, int waves, int64_t grid, hipStream_t stream);
+hipError_t launch_attn_f16(const AttnDev &a, int dp, int rt, int waves, int64_t grid, hipStream_t stream);
+hipError_t launch_attn_f32(const AttnDev &a, int dp, int rt, int waves, int64_t grid, hipStream_t stream);
 
-// 16-row tiles of a workgroup's rows that the kernel is built for: registers hold Q, K, V and O of RT tiles, up to 512 words of a lane
-constexpr int attn_max_rt(int elt, int dp) {
-    return elt == ATK_F32 ? (dp <= 128 ? 2 : 1) : (dp <= 128 ? 4 : 2);
-}
+// 16-row tiles of a workgroup's rows that attn_range_kernel is built for: registers hold Q, K, V and O of RT tiles, up to 512 words of a lane
+constexpr int attn_max_rt(int elt, int dp) { return dp > 128 ? 1 : 2; }
+// wavefronts of a workgroup of attn_block_kernel: eight at 256 words of a lane, or four at up to 512
+constexpr int attn_max_waves(int dp) { return dp > 128 ? 4 : 8; }
 
 template <int ELT, int DP>
-hipError_t launch_attn_dp(const AttnDev &a, int rt, int64_t grid, hipStream_t stream) {
-    const dim3 threads(kAttnWaves * 64);
-    if constexpr (attn_max_rt(ELT, DP) >= 4)
-        if (rt == 4) {
-            hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 4>), dim3((uint32_t)grid), threads, 0, stream, a);
+hipError_t launch_attn_dp(const AttnDev &a, int rt, int waves, int64_t grid, hipStream_t stream) {
+    const dim3 g((uint32_t)grid);
+    if constexpr (ELT != ATK_F32) {
+        if (rt == 0) {
+            if constexpr (attn_max_waves(DP) >= 8) {
+                if (waves == 8) {
+                    hipLaunchKernelGGL((attn_block_kernel<ELT, DP, 8>), g, dim3(512), 0, stream, a);
+                    return hipGetLastError();
+                }
+            }
+            hipLaunchKernelGGL((attn_block_kernel<ELT, DP, 4>), g, dim3(256), 0, stream, a);
             return hipGetLastError();
         }
-    if constexpr (attn_max_rt(ELT, DP) >= 2)
+    }
+    if constexpr (attn_max_rt(ELT, DP) >= 2) {
         if (rt == 2) {
-            hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 2>), dim3((uint32_t)grid), threads, 0, stream, a);
+            hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 2>), g, dim3(kAttnWaves * 64), 0, stream, a);
             return hipGetLastError();
         }
-    hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 1>), dim3((uint32_t)grid), threads, 0, stream, a);
+    }
+    hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 1>), g, dim3(kAttnWaves * 64), 0, stream, a);
     return hipGetLastError();
 }
 template <int ELT>
-hipError_t launch_attn(const AttnDev &a, int dp, int rt, int64_t grid, hipStream_t stream) {
-    if (dp == 64) return launch_attn_dp<ELT, 64>(a, rt, grid, stream);
-    if (dp == 128) return launch_attn_dp<ELT, 128>(a, rt, grid, stream);
-    if (dp == 192) return launch_attn_dp<ELT, 192>(a, rt, grid, stream);
-    return launch_attn_dp<ELT, 256>(a, rt, grid, stream);
+hipError_t launch_attn(const AttnDev &a, int dp, int rt, int waves, int64_t grid, hipStream_t stream) {
+    if (dp == 64) return launch_attn_dp<ELT, 64>(a, rt, waves, grid, stream);
+    if (dp == 128) return launch_attn_dp<ELT, 128>(a, rt, waves, grid, stream);
+    if (dp == 192) return launch_attn_dp<ELT, 192>(a, rt, waves, grid, stream);
+    return launch_attn_dp<ELT, 256>(a, rt, waves, grid, stream);
 }
 
 }  // namespace atk

@@ -93,6 +93,40 @@ def test_shapes(dtype, B, T, H, Hk, D, prefix, lens, ps):
     check(*args, prefix)
 
 
+@pytest.mark.parametrize("dtype", TYPES[:2], ids=str)
+@pytest.mark.parametrize("B,T,H,Hk,D,prefix,ps", [
+    (33, 1, 1, 1, 64, 1, 16), (40, 1, 2, 2, 128, 64, 16), (11, 3, 4, 4, 40, 65, 8), (9, 1, 8, 2, 128, 700, 24), (12, 5, 6, 2, 80, 129, 1), (20, 1, 16, 2, 96, 500, 64), (5, 2, 32, 2, 192, 333, 16),
+    (9, 4, 16, 1, 256, 200, 32), (3, 17, 24, 2, 136, 450, 16), (33, 2, 16, 4, 128, 2100, 16),
+], ids=str)
+def test_many_rows_on_the_prefix(dtype, B, T, H, Hk, D, prefix, ps):
+    args = make(B, T, H, Hk, D, prefix, [prefix + T + (7 * i) % 50 for i in range(B)], ps, dtype, seed=D + prefix)
+    clean, _ = check(*args, prefix)
+    # some sequences end inside the prefix, one before it: their row blocks go another way, and the others' results stay
+    lens = args[4].clone()
+    lens[B // 2], lens[B - 1] = prefix // 2, 0
+    out, _ = check(*args[:4], lens, prefix)
+    same = [b for b in range(B) if b not in (B // 2, B - 1)]
+    assert (out[same].float() - clean[same].float()).abs().max() <= 4 * HALF[dtype] * clean.float().abs().max()
+
+
+@pytest.mark.parametrize("dtype", TYPES[:2], ids=str)
+def test_many_rows_with_scores_at_the_ends(dtype):
+    q, k, v, table, lens = make(40, 1, 4, 2, 64, 300, [301] * 40, 16, dtype, seed=8, scale_q=20.0)
+    check(q, k, v, table, lens, 300, scale=1.0)
+    check(q, k, v, table, lens, 300, scale=1e-6)
+    q = q.abs()
+    one = k.clone()
+    one[table[0, 3].long(), 3] = float("-inf")
+    check(q, one, v, table, lens, 300)
+    k = torch.where(torch.isnan(k), k, torch.full_like(k, float("-inf")))
+    out, lse = check(q, k, v, table, lens, 300)
+    assert (out == 0).all() and (lse == float("-inf")).all()
+    one = k.clone()
+    one[table[0, 3].long(), 3] = float("nan")     # a key that all see
+    out, lse = check(q, one, v, table, lens, 300)
+    assert torch.isnan(out[:, :, 0]).all()
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 def test_rows_that_see_nothing(dtype):
     # empty sequences, sequences shorter than their new tokens, and ones that end inside the prefix
