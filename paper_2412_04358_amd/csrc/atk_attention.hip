@@ -62,7 +62,7 @@ static hipError_t launch_join(const AttnDev &a, int dp, hipStream_t stream) {
 
 struct AttnPlan {
     int dp, rt, waves, prefix_splits, prefix_blocks, prefix_keys, own_splits, own_blocks;
-    int64_t grid, rows, parts, o_bytes, bytes;
+    int64_t rows, parts, o_bytes, bytes;
 };
 
 static int64_t attn_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -95,13 +95,14 @@ static int check_attention(const atk_attention_args *p, bool pointers) {
 
 static int plan_attention(const atk_attention_args *p, AttnPlan *pl) {
     const int group = (int)(p->heads / p->kv_heads);
-    pl->dp = p->dim <= 64 ? 64 : p->dim <= 128 ? 128 : p->dim <= 192 ? 192 : 256;
+    pl->dp = p->dim <= 64 ? 64 : p->dim <= 128 ? 128 : 256;
     const int64_t rows = p->batch * p->tokens * group, own_rows = p->tokens * group;
     // how the shared keys meet the rows: up to two 16-row tiles in every wavefront, or 32 rows a wavefront and keys by way of LDS
     pl->rt = rows <= 16 || p->prefix_len == 0 ? 1 : 2, pl->waves = kAttnWaves;
     int64_t block = 16 * pl->rt, step = kAttnWaves * kTileKeys;
     int64_t wanted = 2 * kNumCU;
-    if (rows > 32 && p->dtype != ATK_F32 && p->prefix_len > 0) {
+    const int64_t small = INT64_C(1) << 28;  // (four tokens' offsets are 32 bits)
+    if (rows > 32 && p->dtype != ATK_F32 && p->prefix_len > 0 && p->page_size % 4 == 0 && p->k_stride[1] < small && p->v_stride[1] < small) {
         pl->rt = 0, pl->waves = rows <= 128 ? 4 : attn_max_waves(pl->dp);
         block = 32 * pl->waves, step = kBlockKeys;
         wanted = pl->waves == 8 ? kNumCU : 2 * kNumCU;
@@ -121,13 +122,13 @@ static int plan_attention(const atk_attention_args *p, AttnPlan *pl) {
     const int64_t own = p->row_pages * p->page_size - p->prefix_len;
     pl->own_blocks = (int)attn_ceil(own_rows, 16);
     const int64_t own_base = p->batch * p->kv_heads * pl->own_blocks;
-    pl->own_splits = own > 0 ? (int)std::min(attn_ceil(own, pl->waves * kTileKeys), std::max<int64_t>(1, wanted / own_base)) : 0;
+    pl->own_splits = own > 0 ? (int)std::min(attn_ceil(own, kAttnWaves * kTileKeys), std::max<int64_t>(1, 2 * kNumCU / own_base)) : 0;
     pl->rows = p->batch * p->tokens * p->heads;
     pl->parts = pl->prefix_splits + pl->own_splits;
-    pl->grid = base * pl->prefix_splits + own_base * pl->own_splits;
     pl->o_bytes = pl->rows * pl->parts * p->dim * 4;
     pl->bytes = pl->o_bytes + pl->rows * pl->parts * 8;
-    return pl->grid < (INT64_C(1) << 31) && own_base < (INT64_C(1) << 31) && base < (INT64_C(1) << 31) ? ATK_OK : ATK_ERR_ARGS;
+    const int64_t most = INT64_C(1) << 30;  // workgroups
+    return base * std::max(1, pl->prefix_splits) < most && own_base * std::max(1, pl->own_splits) < most ? ATK_OK : ATK_ERR_ARGS;
 }
 
 }  // namespace atk
@@ -164,14 +165,16 @@ int atk_shared_prefix_attention(const atk_attention_args *p, void *work, int64_t
     a.prefix_splits = pl.prefix_splits, a.prefix_blocks = pl.prefix_blocks, a.prefix_keys = pl.prefix_keys;
     a.own_splits = pl.own_splits, a.own_blocks = pl.own_blocks;
     a.n_prefix = pl.prefix_splits * pl.prefix_blocks * a.kv_heads;
+    a.prefix_grid = (a.n_prefix + 7) / 8 * 8;
+    a.n_own = a.batch * a.kv_heads * pl.own_blocks * pl.own_splits;
     a.parts = (int)pl.parts;
     a.page.set((uint32_t)p->page_size);
     a.scale = (float)p->scale;
     a.scale2 = (float)(p->scale * 1.4426950408889634);
     hipStream_t s = (hipStream_t)stream;
-    hipError_t e = p->dtype == ATK_F32    ? launch_attn_f32(a, pl.dp, pl.rt, pl.waves, pl.grid, s)
-                   : p->dtype == ATK_BF16 ? launch_attn_bf16(a, pl.dp, pl.rt, pl.waves, pl.grid, s)
-                                          : launch_attn_f16(a, pl.dp, pl.rt, pl.waves, pl.grid, s);
+    hipError_t e = p->dtype == ATK_F32    ? launch_attn_f32(a, pl.dp, pl.rt, pl.waves, s)
+                   : p->dtype == ATK_BF16 ? launch_attn_bf16(a, pl.dp, pl.rt, pl.waves, s)
+                                          : launch_attn_f16(a, pl.dp, pl.rt, pl.waves, s);
     if (e == hipSuccess)
         e = p->dtype == ATK_F32    ? launch_join<ATK_F32>(a, pl.dp, s)
             : p->dtype == ATK_BF16 ? launch_join<ATK_BF16>(a, pl.dp, s)

@@ -2,5 +2,5 @@
 #include "atk_attention_kernel.h"
 
 namespace atk {
-hipError_t launch_attn_f16(const AttnDev &a, int dp, int rt, int waves, int64_t grid, hipStream_t stream) { return launch_attn<ATK_F16>(a, dp, rt, waves, grid, stream); }
+hipError_t launch_attn_f16(const AttnDev &a, int dp, int rt, int waves, hipStream_t stream) { return launch_attn<ATK_F16>(a, dp, rt, waves, stream); }
 }  // namespace atk

@@ -14,6 +14,8 @@
 //   DP/16 apart, and a lane's results are contiguous in d again.
 #pragma once
 
+#include <type_traits>
+
 #include "atk_decode_common.h"
 
 namespace atk {
@@ -39,7 +41,7 @@ struct AttnDev {
     int prefix_len;
     int prefix_splits, prefix_blocks, prefix_keys;  // ranges of the shared keys, row blocks, keys of a range (a multiple of a workgroup's tiles)
     int own_splits, own_blocks;
-    int n_prefix;      // workgroups of the shared keys; those of own keys follow
+    int n_prefix, prefix_grid, n_own;  // units of the shared keys and workgroups for them, which come first; units of own keys
     int parts;         // prefix_splits + own_splits
     FastDiv page;
     float scale, scale2;  // scale2: scale * log2(e)
@@ -286,6 +288,7 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
         const bool masked = k0 + kTileKeys > min_lim || valid != 0xffffffffu;
         bool apart = false;  // a value that is not finite beside a mask: 0 * it would not be 0
         if (masked) {
+            asm volatile("");  // (a branch, no selections)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -438,6 +441,9 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
 // buffers - the next tile is written to the other one while this one is worked on, from loads that were given out a tile earlier.
 //   S^T = K Q^T and O^T = V^T P^T by 32x32x16 matrix instructions, half the operands' reads of 16x16x32 for a product.  A lane has one query (lane % 32) and of
 //   each 32 keys those with 8 * i + 4 * (lane / 32) + 0..3; step s of the second product takes i = 2 s and 2 s + 1.
+//   A tile is a phase of products (those of the tile before with V, this one's with K) and one of vector instructions (maximum, exponentials, packing, the next
+//   tiles' addresses and stores), and each SIMD has two wavefronts of the workgroup, one of each half: the second half is a phase late, so that one of the two has the matrix
+//   units while the other one has the vector unit.  In step they took 2.6 times as long.
 //   V lies in LDS by d, a lane's eight keys of a step side by side: transposed in registers on the way in (a lane has loaded two d's of eight keys), so that
 //   both operands are single 16-byte reads.  Rows in LDS are 16 bytes longer than their data: lanes a row apart meet in different banks.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -459,8 +465,8 @@ struct BlockLds {
     static constexpr int kBytes = 2 * kBuffer;
 };
 
-// Rows r0 .. r0 + 32 * NW - 1 of head h against keys ka .. kb - 1, all of which every one of these rows sees.
-template <int ELT, int DP, int NW>
+// Rows r0 .. r0 + 32 * NW - 1 of head h against keys ka .. kb - 1 (one at least), all of which every one of these rows sees.  FULL: dim == DP.
+template <int ELT, int DP, int NW, bool FULL>
 __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int n_rows, const int32_t *table_row, int ka, int kb, int part, char *lds) {
     typedef AttnElt<ELT> E;
     typedef BlockLds<DP> L;
@@ -468,70 +474,106 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
     constexpr int ND = DP / 32;                            // tiles of d
     constexpr int KC = kBlockKeys * DP / 8 / (NW * 64);    // 16-byte pieces of K that a thread brings in
     constexpr int PL = DP / 2;                             // lanes of a row of V, two d's each
-    constexpr bool kOneGroup = PL % 64 == 0;               // a wavefront's load is of one group of eight keys
     constexpr bool kSpare = 8 * PL < NW * 64;              // ... the last wavefronts bring in none of V
     constexpr int VC = kSpare ? 1 : 8 * PL / (NW * 64);    // ... loads of eight keys of a thread
-    static_assert(KC >= 1, "every thread has its share");
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr bool kHalves = DP == 64;                     // a wavefront's load is of eight keys of K, of four keys of two groups of V: one half each
+    static_assert(KC >= 1 && (DP == 64 || DP == 128 || DP == 256), "every thread has its share");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, g = lane >> 5;
     const char *kh = (const char *)a.k + h * a.ks[2] * 2, *vh = (const char *)a.v + h * a.vs[2] * 2;
+    const int tiles = (kb - ka + kBlockKeys - 1) / kBlockKeys;
 
-    // what a thread brings in: piece (wave * 64 + lane) + c * NW * 64 of K; group of eight keys and two d's of V
-    int k_key[KC], k_piece[KC], v_group[VC], v_d[VC];
-#pragma unroll
-    for (int c = 0; c < KC; ++c) {
-        const int id = c * NW * 64 + threadIdx.x;
-        k_key[c] = id / (DP / 8), k_piece[c] = id % (DP / 8);
-    }
-#pragma unroll
-    for (int c = 0; c < VC; ++c) {
-        const int id = c * NW * 64 + threadIdx.x;
-        v_group[c] = id / PL, v_d[c] = id % PL * 2;
-    }
+    // What comes in.  Four keys that begin at a multiple of four lie in one page (page_size % 4 == 0, and so ka), so a wavefront's loads have scalar
+    // addresses, each found by a lane of its own, and offsets that stay the same: with an address for each lane's key, exchanged between lanes, or with
+    // scalar arithmetic alone they took 1100 cycles of a wavefront and tile, as long as all of its products.
+    // Thread's piece c of K: key (c * NW * 64 + thread) / (DP / 8); of V: group of eight keys (x, s, half), 32 x + 16 s + 4 half + {0..3, 8..11}, and two d's.
+    constexpr int kRow = DP / 8;
+    const int k_lane_key = kRow < 64 ? lane / kRow : 0, k_piece = (kRow < 64 ? lane : threadIdx.x) % kRow;
+    auto k_key = [&](int c) { return (c * NW * 64 + wave * 64) / kRow; };          // of the wavefront's first lane
+    auto v_group = [&](int c) { return (c * NW * 64 + wave * 64) / PL; };
+    const int v_d = (kHalves ? lane % 32 : (int)threadIdx.x % PL) * 2;
+    const uint32_t k_step = (uint32_t)a.ks[1] * 2, v_step = (uint32_t)a.vs[1] * 2;
+    // (halves: lanes 32 to 63 have a base of their own, and keys from its beginning)
+    const uint32_t k_off = (uint32_t)(kHalves ? (lane % 32) / kRow : k_lane_key) * k_step + k_piece * 16;
+    const uint32_t v_off = v_d * 2;
+    const bool upper = kHalves && lane >= 32;
+    int bad_page = 0;
+    // Lane x (of each 16) looks after keys 4 x .. 4 x + 3 of a tile; tiles past the last are read as that one (brought in and not used: no branches), keys past
+    // the end as the last four.
+    auto key_of = [&](int t) { return min(ka + min(t, tiles - 1) * kBlockKeys + (lane & 15) * 4, (kb - 1) & ~3); };
+    auto page_of = [&](int t) { return table_row[a.page.div(key_of(t))]; };
+    auto base_of = [&](int t, int page, const int64_t *stride) {
+        if ((unsigned)page >= (unsigned)a.n_pages) bad_page = ATK_STATUS_BAD_PAGE, page = 0;
+        return ((int64_t)page * stride[0] + (int64_t)a.page.mod(key_of(t)) * stride[1]) * 2;
+    };
+    auto scalar_base = [&](int64_t bases, int key) {  // of the four keys at `key` of the tile
+        const uint32_t lo = __builtin_amdgcn_readlane((int)bases, key >> 2), hi = __builtin_amdgcn_readlane((int)(bases >> 32), key >> 2);
+        return (int64_t)((uint64_t)hi << 32 | lo);
+    };
+    const bool alike = a.ks[0] == a.vs[0] && a.ks[1] == a.vs[1];
+    auto k_group_key = [&](int x) {  // first key of the four keys of base x
+        return kHalves ? k_key(x / 2) + x % 2 * 4 : k_key(x) & ~3;
+    };
+    auto v_group_key = [&](int x) {
+        const int group = kHalves ? v_group(x / 4) + x % 2 : v_group(x / 2), second = kHalves ? x / 2 % 2 : x % 2;
+        return (group >> 1) * 16 + (group & 1) * 4 + second * 8;
+    };
     u32x4 kr[KC];
     uint32_t vr[VC][8];
-    uint32_t valid_next = 0xffffffffu, valid_next2 = 0xffffffffu;  // of the keys of a tile's halves
-    bool bad_page = false;
-    auto look_up = [&](int k0) -> int {  // lane j: the page of key k0 + j; keys past the end are read as the last one
-        return k0 < kb ? table_row[a.page.div(min(k0 + lane, kb - 1))] : 0;
-    };
-    auto load = [&](int k0, int page) {
-        const int key = min(k0 + lane, kb - 1);
-        const bool good = (unsigned)page < (unsigned)a.n_pages;
-        bad_page |= !good;
-        const uint64_t votes = __ballot(good && k0 + lane < kb);
-        valid_next = (uint32_t)votes, valid_next2 = (uint32_t)(votes >> 32);
-        const int64_t p = good ? page : 0, slot = a.page.mod(key);
-        const int64_t ko = (p * a.ks[0] + slot * a.ks[1]) * 2, vo = (p * a.vs[0] + slot * a.vs[1]) * 2;
-        const int klo = (int)ko, khi = (int)(ko >> 32), vlo = (int)vo, vhi = (int)(vo >> 32);
+    auto load_k = [&](int64_t bases) {
+        const bool in = FULL || k_piece * 8 < a.dim;
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
-            const int64_t at = (int64_t)(((uint64_t)(uint32_t)__shfl(khi, k_key[c], 64) << 32) | (uint32_t)__shfl(klo, k_key[c], 64));
-            kr[c] = k_piece[c] * 8 < a.dim ? *(const u32x4 *)(kh + at + k_piece[c] * 16) : u32x4{0, 0, 0, 0};
+            int64_t at;
+            uint32_t off = k_off;
+            if constexpr (kHalves) {
+                const int64_t lo = scalar_base(bases, k_group_key(2 * c)), hi = scalar_base(bases, k_group_key(2 * c + 1));
+                at = upper ? hi : lo;
+            } else {
+                at = scalar_base(bases, k_group_key(c));
+                if (DP == 256) off += (k_key(c) & 3) * k_step;
+            }
+            kr[c] = in ? *(const u32x4 *)(kh + at + off) : u32x4{0, 0, 0, 0};
         }
+    };
+    auto load_v = [&](int64_t bases) {
         if (kSpare && wave * 64 >= 8 * PL) return;
+        const bool in = FULL || v_d < a.dim;
 #pragma unroll
         for (int c = 0; c < VC; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                // group (x, s, half): keys 32 x + 16 s + 8 (j / 4) + 4 half + j % 4
-                const int who = (v_group[c] >> 1) * 16 + (j >> 2) * 8 + (v_group[c] & 1) * 4 + (j & 3);
-                int lo, hi;
-                if constexpr (kOneGroup) {  // its addresses are scalars
-                    const int one = __builtin_amdgcn_readfirstlane(who);
-                    lo = __builtin_amdgcn_readlane(vlo, one), hi = __builtin_amdgcn_readlane(vhi, one);
+            for (int y = 0; y < 2; ++y) {
+                int64_t at;
+                if constexpr (kHalves) {
+                    const int64_t lo = scalar_base(bases, v_group_key(4 * c + 2 * y)), hi = scalar_base(bases, v_group_key(4 * c + 2 * y + 1));
+                    at = upper ? hi : lo;
                 } else {
-                    lo = __shfl(vlo, who, 64), hi = __shfl(vhi, who, 64);
+                    at = scalar_base(bases, v_group_key(2 * c + y));
                 }
-                const int64_t at = (int64_t)(((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo);
-                vr[c][j] = v_d[c] < a.dim ? *(const uint32_t *)(vh + at + v_d[c] * 2) : 0u;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) vr[c][4 * y + j] = in ? *(const uint32_t *)(vh + at + (v_off + j * v_step)) : 0u;
             }
     };
-    auto store = [&](char *buffer) {
+    char *const k_lds = lds, *const v_lds = lds + 2 * kBlockKeys * L::kK;
+    auto store_k = [&](int t) {
+        char *k = k_lds + (t & 1) * kBlockKeys * L::kK + k_lane_key * L::kK + k_piece * 16;
 #pragma unroll
-        for (int c = 0; c < KC; ++c) *(u32x4 *)(buffer + k_key[c] * L::kK + k_piece[c] * 16) = kr[c];
+        for (int c = 0; c < KC; ++c) *(u32x4 *)(k + k_key(c) * L::kK) = kr[c];
+    };
+    auto store_v = [&](int t) {
         if (kSpare && wave * 64 >= 8 * PL) return;
-        char *v = buffer + kBlockKeys * L::kK;
+        const int left = kb - ka - t * kBlockKeys;
+        if (left < kBlockKeys && left > 0) {  // what lies behind the last key has weight 0, which NaN would not heed
+            asm volatile("");
+#pragma unroll
+            for (int c = 0; c < VC; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int group = v_group(c) + (upper ? 1 : 0);
+                    if ((group >> 1) * 16 + (group & 1) * 4 + (j >> 2) * 8 + (j & 3) >= left) vr[c][j] = 0;
+                }
+        }
+        char *v = v_lds + (t & 1) * DP * L::kV + v_d * L::kV + (upper ? 16 : 0);
 #pragma unroll
         for (int c = 0; c < VC; ++c) {
             u32x4 even, odd;
@@ -540,8 +582,8 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
                 even[j] = __builtin_amdgcn_perm(vr[c][2 * j + 1], vr[c][2 * j], 0x05040100u);
                 odd[j] = __builtin_amdgcn_perm(vr[c][2 * j + 1], vr[c][2 * j], 0x07060302u);
             }
-            *(u32x4 *)(v + v_d[c] * L::kV + v_group[c] * 16) = even;
-            *(u32x4 *)(v + (v_d[c] + 1) * L::kV + v_group[c] * 16) = odd;
+            *(u32x4 *)(v + v_group(c) * 16) = even;
+            *(u32x4 *)(v + L::kV + v_group(c) * 16) = odd;
         }
     };
 
@@ -565,46 +607,93 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
 #pragma unroll
         for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
 
-    load(ka, look_up(ka));
-    int page = look_up(ka + kBlockKeys);
-    uint32_t valid[2];
-    int at = 0;
-    store(lds);
-    valid[0] = valid_next, valid[1] = valid_next2;
-    load(ka + kBlockKeys, page);
-    page = look_up(ka + 2 * kBlockKeys);
-    __syncthreads();
-    for (int k0 = ka; k0 < kb; k0 += kBlockKeys) {
-        const char *kl = lds + at * L::kBuffer, *vl = kl + kBlockKeys * L::kK;
-        at ^= 1;
-        const uint32_t now[2] = {valid[0], valid[1]};
-        if (k0 + kBlockKeys < kb) {
-            store(lds + at * L::kBuffer);
-            valid[0] = valid_next, valid[1] = valid_next2;
-            load(k0 + 2 * kBlockKeys, page);
-            page = look_up(k0 + 3 * kBlockKeys);
+    // What the phases bring in for the next ones: K a tile ahead, V for this one; the second half of the wavefronts, a phase late, one tile more.
+    const int late = NW == 8 ? wave >> 2 : 0;
+    int page = page_of(0), page_next = page_of(1);
+    int64_t bases = base_of(0, page, a.ks), bases_v = base_of(0, page, a.vs);  // of the tile whose K, V is brought in next
+    load_k(bases);
+    store_k(0);
+    auto step = [&](int t) {  // from tile t's addresses to tile t + 1's; its page came in a step earlier
+        bases_v = alike ? bases : base_of(t, page, a.vs);
+        page = page_next;
+        bases = base_of(t + 1, page, a.ks);
+    };
+    step(0);
+    if (late) {
+        page_next = page_of(2);
+        load_v(bases_v);
+        store_v(0);
+        load_k(bases);
+        store_k(1);
+        step(1);
+    }
+    load_k(bases);       // tile 1 + late
+    load_v(bases_v);     // tile late
+    page_next = page_of(2 + late);
+    step(1 + late);
+    page_next = page_of(3 + late);
+    f32x16 s[2];
+    u32x4 p[2][2];
+    auto barrier = [&]() {
+        __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // Products of tile t with V and of tile t + 1 with K (either may be left out).  Reads from LDS run kAhead products in front: one takes four products' time.
+    constexpr int kFirst = 2 * NS, kSecond = 4 * ND, kAhead = 6;
+    auto products = [&](auto second, auto first, int t) {
+        constexpr bool kBoth = decltype(second)::value && decltype(first)::value;
+        const char *k = k_lds + ((t + 1) & 1) * kBlockKeys * L::kK, *v = v_lds + (t & 1) * DP * L::kV;
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+        if constexpr (decltype(second)::value) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int i = 0; i < ND; ++i) acc[i] = mma32<ELT>(*(const u32x4 *)(v + (i * 32 + n) * L::kV + (y * 4 + x * 2 + g) * 16), p[y][x], acc[i]);
         }
-        f32x16 s[2];
+        if constexpr (decltype(first)::value) {
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
+            for (int y = 0; y < 2; ++y)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) s[y][j] = 0.0f;
+                for (int j = 0; j < 16; ++j) s[y][j] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < NS; ++i) s[y] = mma32<ELT>(*(const u32x4 *)(kl + (y * 32 + n) * L::kK + (i * 2 + g) * 16), q[i], s[y]);
+            for (int i = 0; i < NS; ++i)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) s[y] = mma32<ELT>(*(const u32x4 *)(k + (y * 32 + n) * L::kK + (i * 2 + g) * 16), q[i], s[y]);
         }
-        if ((now[0] & now[1]) != 0xffffffffu) {
+        constexpr int kAll = kBoth ? kFirst + kSecond : decltype(first)::value ? kFirst : kSecond;
+        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);  // reads from LDS
+#pragma unroll
+        for (int i = 0; i < kAll - kAhead; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);     // a product
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x8, kAhead, 0);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    typedef std::true_type Yes;
+    typedef std::false_type No;
+    auto softmax = [&](int t) {
+        const int left = kb - ka - t * kBlockKeys;  // keys of the tile
+        if (left < kBlockKeys) {
+            asm volatile("");  // (a branch: as selections these instructions are every tile's)
 #pragma unroll
             for (int y = 0; y < 2; ++y)
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
-                    if (!(now[y] >> (8 * (j >> 2) + 4 * g + (j & 3)) & 1)) s[y][j] = kNoMax;
+                    if (y * 32 + 8 * (j >> 2) + 4 * g + (j & 3) >= left) s[y][j] = kNoMax;
         }
         float top = s[0][0];
 #pragma unroll
         for (int y = 0; y < 2; ++y)
 #pragma unroll
             for (int j = 0; j < 16; ++j) top = fmaxf(top, s[y][j]);
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
         if (__any((top - m) * a.scale2 > kLazyMax)) {
             const float to = fmaxf(m, top);
             const float f = __builtin_amdgcn_exp2f((m - to) * a.scale2);
@@ -618,35 +707,56 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
         }
         const float zero = m == kNoMax ? 0.0f : m;
         const float ref = zero * a.scale2 - E::kBias;
-        float sum = 0.0f;
-        if (far) {  // (as below behind the subtraction: 2^(0 * x + y))
+        if (far) {
 #pragma unroll
             for (int y = 0; y < 2; ++y)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) s[y][j] = __builtin_amdgcn_exp2f(fmaf(s[y][j] - zero, a.scale2, E::kBias));
+                for (int j = 0; j < 16; ++j) s[y][j] = fmaf(s[y][j] - zero, a.scale2, E::kBias);
         } else {
 #pragma unroll
             for (int y = 0; y < 2; ++y)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) s[y][j] = __builtin_amdgcn_exp2f(fmaf(s[y][j], a.scale2, -ref));
+                for (int j = 0; j < 16; ++j) s[y][j] = fmaf(s[y][j], a.scale2, -ref);
         }
+        float sum = 0.0f;
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+        for (int y = 0; y < 2; ++y) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) sum += s[y][j];
-        l += sum;
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const u32x4 p = {E::pack(s[y][8 * t], s[y][8 * t + 1]), E::pack(s[y][8 * t + 2], s[y][8 * t + 3]), E::pack(s[y][8 * t + 4], s[y][8 * t + 5]),
-                                 E::pack(s[y][8 * t + 6], s[y][8 * t + 7])};
-#pragma unroll
-                for (int i = 0; i < ND; ++i) acc[i] = mma32<ELT>(*(const u32x4 *)(vl + (i * 32 + n) * L::kV + (y * 4 + t * 2 + g) * 16), p, acc[i]);
+            for (int j = 0; j < 16; ++j) {
+                s[y][j] = __builtin_amdgcn_exp2f(s[y][j]);
+                sum += s[y][j];
             }
-        __syncthreads();
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                p[y][x] = u32x4{E::pack(s[y][8 * x], s[y][8 * x + 1]), E::pack(s[y][8 * x + 2], s[y][8 * x + 3]), E::pack(s[y][8 * x + 4], s[y][8 * x + 5]),
+                                E::pack(s[y][8 * x + 6], s[y][8 * x + 7])};
+        }
+        l += sum;
+    };
+    barrier();
+    if (late) barrier();
+    products(No{}, Yes{}, -1);
+    barrier();
+    for (int t = 0; t < tiles - 1; ++t) {
+        const int page_new = page_of(t + 4 + late);  // (in front of the data's loads: what waits for it does not wait for them)
+        softmax(t);
+        store_k(t + 1 + late);
+        store_v(t + late);
+        load_k(bases);
+        load_v(bases_v);
+        step(t + 2 + late);
+        page_next = page_new;
+        barrier();
+        products(Yes{}, Yes{}, t);
+        barrier();
     }
-    if (bad_page && a.status) atomicOr(a.status, ATK_STATUS_BAD_PAGE);
+    softmax(tiles - 1);
+    store_v(tiles - 1 + late);
+    barrier();
+    products(Yes{}, No{}, tiles - 1);
+    if (!late && NW == 8) barrier();
+    bad_page |= __any(bad_page) ? ATK_STATUS_BAD_PAGE : 0;
+    if (bad_page && a.status && lane == 0) atomicOr(a.status, bad_page);
     l += __shfl_xor(l, 32, 64);
     if (!real) return;
     const int64_t row = ((int64_t)x.b * a.tokens + x.t) * a.heads + x.head;
@@ -661,15 +771,24 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
         }
 }
 
+// Workgroup `id` of 8 * ceil(n / 8) in the order of units 0 .. n - 1 that gives each XCD (id % 8) units in a row; -1: none.  Units with the same keys, and the heads of the
+// same tokens, are neighbours, and so meet in one L2 (against an XCD for each head: level, and no less so with a number of heads that is not a multiple of eight).
+__device__ __forceinline__ int xcd_unit(int id, int n) {
+    const int per = (n + 7) / 8, u = (id & 7) * per + (id >> 3);
+    return (id >> 3) < per && u < n ? u : -1;
+}
+
 // Own keys of a sequence: workgroup y of those.
 template <int ELT, int DP, int NW>
 __device__ __forceinline__ void attn_own(const AttnDev &a, int y, char *lds) {
     bool bad = false;  // (told by attn_range)
-    const int h = y % a.kv_heads;
-    int x = y / a.kv_heads;
-    const int block = x % a.own_blocks;
-    x /= a.own_blocks;
-    const int b = x % a.batch, split = x / a.batch;
+    y = xcd_unit(y, a.n_own);
+    if (y < 0) return;
+    const int block = y % a.own_blocks;
+    int x = y / a.own_blocks;
+    const int h = x % a.kv_heads;
+    x /= a.kv_heads;
+    const int split = x % a.own_splits, b = x / a.own_splits;
     const int row = seq_row(a, b, &bad), len = seq_len(a, row, &bad);
     const int keys = max(0, len - a.prefix_len);
     constexpr int kStep = NW * kTileKeys;
@@ -687,32 +806,28 @@ template <int ELT, int DP, int RT>
 __global__ __launch_bounds__(kAttnWaves * 64) void attn_range_kernel(const AttnDev a) {
     __shared__ __align__(16) char lds[attn_lds_bytes<DP, RT, kAttnWaves>()];
     const int id = blockIdx.x;
-    if (id >= a.n_prefix) {
-        attn_own<ELT, DP, kAttnWaves>(a, id - a.n_prefix, lds);
+    if (id >= a.prefix_grid) {
+        attn_own<ELT, DP, kAttnWaves>(a, id - a.prefix_grid, lds);
         return;
     }
-    // heads side by side: with eight of them, each XCD's L2 holds one head's keys
+    const int u = xcd_unit(id, a.n_prefix);
+    if (u < 0) return;
     bool bad = false;
-    const int h = id % a.kv_heads, x = id / a.kv_heads;
-    const int block = x % a.prefix_blocks, split = x / a.prefix_blocks;
+    const int block = u % a.prefix_blocks, h = u / a.prefix_blocks % a.kv_heads, split = u / (a.prefix_blocks * a.kv_heads);
     const int row = seq_row(a, 0, &bad);
     const int ka = split * a.prefix_keys, kb = row < 0 ? ka : min(a.prefix_len, ka + a.prefix_keys);
     attn_range<ELT, DP, RT, kAttnWaves>(a, h, block * RT * 16, a.batch * a.tokens * a.group, -1, a.table + row * a.table_stride, ka, kb, split, lds);
 }
 
 // Many: its wavefronts share its rows out.
-template <int ELT, int DP, int NW>
+template <int ELT, int DP, int NW, bool FULL>
 __global__ __launch_bounds__(NW * 64, DP <= 128 ? 2 : 1) void attn_block_kernel(const AttnDev a) {
     constexpr int kRangeBytes = attn_lds_bytes<DP, 1, NW>();
     __shared__ __align__(16) char lds[BlockLds<DP>::kBytes > kRangeBytes ? BlockLds<DP>::kBytes : kRangeBytes];
-    const int id = blockIdx.x;
-    if (id >= a.n_prefix) {
-        attn_own<ELT, DP, NW>(a, id - a.n_prefix, lds);
-        return;
-    }
+    const int u = xcd_unit(blockIdx.x, a.n_prefix);
+    if (u < 0) return;
     bool bad = false;
-    const int h = id % a.kv_heads, x = id / a.kv_heads;
-    const int block = x % a.prefix_blocks, split = x / a.prefix_blocks;
+    const int block = u % a.prefix_blocks, h = u / a.prefix_blocks % a.kv_heads, split = u / (a.prefix_blocks * a.kv_heads);
     const int row = seq_row(a, 0, &bad), n_rows = a.batch * a.tokens * a.group, r0 = block * NW * 32;
     const int ka = split * a.prefix_keys, kb = row < 0 ? ka : min(a.prefix_len, ka + a.prefix_keys);
     const int32_t *table = a.table + row * a.table_stride;
@@ -722,8 +837,8 @@ __global__ __launch_bounds__(NW * 64, DP <= 128 ? 2 : 1) void attn_block_kernel(
         const AttnRow w = attn_row(a, h, r, -1);
         if (seq_len(a, seq_row(a, w.b, &bad), &bad) - (a.tokens - 1 - w.t) < kb) all = false;
     }
-    if (__syncthreads_and(all)) {
-        attn_block<ELT, DP, NW>(a, h, r0, n_rows, table, ka, kb, split, lds);
+    if (ka < kb && __syncthreads_and(all)) {
+        attn_block<ELT, DP, NW, FULL>(a, h, r0, n_rows, table, ka, kb, split, lds);
     } else {
         for (int t = 0; t < NW * 2; ++t) {
             __syncthreads();
@@ -732,10 +847,11 @@ __global__ __launch_bounds__(NW * 64, DP <= 128 ? 2 : 1) void attn_block_kernel(
     }
 }
 
-// rt: 16-row tiles of a workgroup of attn_range_kernel; 0: attn_block_kernel, waves of 32 rows
-hipError_t launch_attn_bf16(const AttnDev &a, int dp, int rt, int waves, int64_t grid, hipStream_t stream);
-hipError_t launch_attn_f16(const AttnDev &a, int dp, int rt, int waves, int64_t grid, hipStream_t stream);
-hipError_t launch_attn_f32(const AttnDev &a, int dp, int rt, int waves, int64_t grid, hipStream_t stream);
+// rt: 16-row tiles of a workgroup of attn_range_kernel; 0: attn_block_kernel on the shared keys, waves of 32 rows, and own keys in a launch of their own: they are bound by
+// memory, and one workgroup of attn_block_kernel takes all registers of a CU (in one launch 64 samples' 130 MB took 53 us, apart 24 + 22)
+hipError_t launch_attn_bf16(const AttnDev &a, int dp, int rt, int waves, hipStream_t stream);
+hipError_t launch_attn_f16(const AttnDev &a, int dp, int rt, int waves, hipStream_t stream);
+hipError_t launch_attn_f32(const AttnDev &a, int dp, int rt, int waves, hipStream_t stream);
 
 // 16-row tiles of a workgroup's rows that attn_range_kernel is built for: registers hold Q, K, V and O of RT tiles, up to 512 words of a lane
 constexpr int attn_max_rt(int elt, int dp) { return dp > 128 ? 1 : 2; }
@@ -743,35 +859,43 @@ constexpr int attn_max_rt(int elt, int dp) { return dp > 128 ? 1 : 2; }
 constexpr int attn_max_waves(int dp) { return dp > 128 ? 4 : 8; }
 
 template <int ELT, int DP>
-hipError_t launch_attn_dp(const AttnDev &a, int rt, int waves, int64_t grid, hipStream_t stream) {
-    const dim3 g((uint32_t)grid);
+hipError_t launch_attn_dp(AttnDev a, int rt, int waves, hipStream_t stream) {
     if constexpr (ELT != ATK_F32) {
         if (rt == 0) {
-            if constexpr (attn_max_waves(DP) >= 8) {
-                if (waves == 8) {
-                    hipLaunchKernelGGL((attn_block_kernel<ELT, DP, 8>), g, dim3(512), 0, stream, a);
-                    return hipGetLastError();
+            const dim3 g((uint32_t)a.prefix_grid);
+            const bool full = a.dim == DP;
+            if (waves == 8 && attn_max_waves(DP) >= 8) {
+                if constexpr (attn_max_waves(DP) >= 8) {
+                    if (full)
+                        hipLaunchKernelGGL((attn_block_kernel<ELT, DP, 8, true>), g, dim3(512), 0, stream, a);
+                    else
+                        hipLaunchKernelGGL((attn_block_kernel<ELT, DP, 8, false>), g, dim3(512), 0, stream, a);
                 }
+            } else if (full) {
+                hipLaunchKernelGGL((attn_block_kernel<ELT, DP, 4, true>), g, dim3(256), 0, stream, a);
+            } else {
+                hipLaunchKernelGGL((attn_block_kernel<ELT, DP, 4, false>), g, dim3(256), 0, stream, a);
             }
-            hipLaunchKernelGGL((attn_block_kernel<ELT, DP, 4>), g, dim3(256), 0, stream, a);
-            return hipGetLastError();
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess || a.n_own == 0) return e;
+            a.prefix_grid = 0;
         }
     }
+    const dim3 g((uint32_t)(a.prefix_grid + (a.n_own + 7) / 8 * 8)), threads(kAttnWaves * 64);
     if constexpr (attn_max_rt(ELT, DP) >= 2) {
         if (rt == 2) {
-            hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 2>), g, dim3(kAttnWaves * 64), 0, stream, a);
+            hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 2>), g, threads, 0, stream, a);
             return hipGetLastError();
         }
     }
-    hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 1>), g, dim3(kAttnWaves * 64), 0, stream, a);
+    hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 1>), g, threads, 0, stream, a);
     return hipGetLastError();
 }
 template <int ELT>
-hipError_t launch_attn(const AttnDev &a, int dp, int rt, int waves, int64_t grid, hipStream_t stream) {
-    if (dp == 64) return launch_attn_dp<ELT, 64>(a, rt, waves, grid, stream);
-    if (dp == 128) return launch_attn_dp<ELT, 128>(a, rt, waves, grid, stream);
-    if (dp == 192) return launch_attn_dp<ELT, 192>(a, rt, waves, grid, stream);
-    return launch_attn_dp<ELT, 256>(a, rt, waves, grid, stream);
+hipError_t launch_attn(const AttnDev &a, int dp, int rt, int waves, hipStream_t stream) {
+    if (dp == 64) return launch_attn_dp<ELT, 64>(a, rt, waves, stream);
+    if (dp == 128) return launch_attn_dp<ELT, 128>(a, rt, waves, stream);
+    return launch_attn_dp<ELT, 256>(a, rt, waves, stream);
 }
 
 }  // namespace atk
