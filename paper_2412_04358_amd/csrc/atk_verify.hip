@@ -2,7 +2,7 @@
 //
 // Only one row of the target's probabilities is needed whole, and after a rejection one of the draft's: those of the first rejected
 // token.  verify_sums_kernel finds it (a few gathers, done again by every workgroup of the request), and sums the weights of a part of that row;
-// verify_draw_kernel finds the part, then the element, at which the running sum passes the target.  Sums are f64: an index is what comes out, and the
+// verify_draw_kernel finds the part, then the thread's eight elements, then the element at which the running sum passes the goal.  Sums are f64: an index is what comes out, and the
 // running sum of 10^5 f32 would be off by more than the weights.
 #include "atk_decode_common.h"
 
@@ -35,11 +35,13 @@ struct VerifyRow {
     int64_t certain;     // element that a draft without probabilities had for sure, -1 if none
     int accepted;
 
-    __device__ __forceinline__ VerifyRow(const VerifyDev &a, int64_t b) {
+    // found: how many were accepted, where that is known
+    __device__ __forceinline__ VerifyRow(const VerifyDev &a, int64_t b, int found = -1) {
         const int lane = threadIdx.x & 63;
         const int n = a.n_drafts ? min(max(a.n_drafts[b], 0), a.drafts) : a.drafts;
         int first = n;
-        for (int i0 = 0; i0 < n && first == n; i0 += 64) {
+        if (found >= 0) first = found;
+        for (int i0 = 0; found < 0 && i0 < n && first == n; i0 += 64) {
             const int i = i0 + lane;
             bool no = false;
             if (i < n) {
@@ -67,121 +69,184 @@ struct VerifyRow {
     }
 };
 
+// A thread's eight elements of a tile of kTile, from v on; those past `to` weigh nothing.
+constexpr int kEach = 8, kTile = 256 * kEach;
+
+// (rows begin where their strides put them: 16-byte loads at the elements' own alignment)
+typedef uint32_t WordsOn4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t WordsOn2 __attribute__((ext_vector_type(4), aligned(2)));
+template <int ELT>
+__device__ __forceinline__ void probs8(const void *p, int64_t v, double *out) {
+    if constexpr (ELT == ATK_F32) {
+        const WordsOn4 a = *(const WordsOn4 *)((const float *)p + v), b = *(const WordsOn4 *)((const float *)p + v + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = (double)__uint_as_float(a[e]), out[4 + e] = (double)__uint_as_float(b[e]);
+    } else {
+        const WordsOn2 a = *(const WordsOn2 *)((const uint16_t *)p + v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t w = a[e];
+            if constexpr (ELT == ATK_BF16) {
+                out[2 * e] = (double)__uint_as_float(w << 16), out[2 * e + 1] = (double)__uint_as_float(w & 0xffff0000u);
+            } else {
+                out[2 * e] = (double)(float)__builtin_bit_cast(_Float16, (uint16_t)(w & 0xffffu));
+                out[2 * e + 1] = (double)(float)__builtin_bit_cast(_Float16, (uint16_t)(w >> 16));
+            }
+        }
+    }
+}
+
+// w[e]: what is left of the target's probability over the draft's, or (of_target) that itself; all[e]: that itself
+template <int ELT>
+__device__ __forceinline__ void weights8(const VerifyRow<ELT> &row, int64_t v, int64_t to, double *left, double *all) {
+    if (v + kEach <= to) {
+        probs8<ELT>(row.p, v, all);
+        if (row.q) {
+            probs8<ELT>(row.q, v, left);
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) left[e] = all[e] - left[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) left[e] = v + e == row.certain ? all[e] - 1.0 : all[e];
+        }
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) left[e] = left[e] > 0 ? left[e] : 0.0, all[e] = all[e] > 0 ? all[e] : 0.0;
+    } else {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            left[e] = all[e] = 0.0;
+            if (v + e < to) {
+                const double2 w = row.weights(v + e);
+                left[e] = w.x, all[e] = w.y;
+            }
+        }
+    }
+}
+
 __device__ __forceinline__ double wave_sum(double v) {
     for (int w = 1; w < 64; w <<= 1) v += __shfl_xor(v, w, 64);
     return v;
 }
 
+__device__ __forceinline__ void sum256(double *a, double *b) {
+    __shared__ double2 waves[4];
+    *a = wave_sum(*a), *b = wave_sum(*b);
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = double2{*a, *b};
+    __syncthreads();
+    *a = (waves[0].x + waves[1].x) + (waves[2].x + waves[3].x), *b = (waves[0].y + waves[1].y) + (waves[2].y + waves[3].y);
+}
+
 template <int ELT>
 __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyDev a) {
-    __shared__ double2 waves[4];
     const int64_t b = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     const VerifyRow<ELT> row(a, b);
     const int64_t from = part * a.part, to = min(a.vocab, from + a.part);
     double2 s = {0, 0};
-    for (int64_t v = from + threadIdx.x; v < to; v += 256) {
-        const double2 w = row.weights(v);
-        s.x += w.x, s.y += w.y;
+    for (int64_t v = from + threadIdx.x * kEach; v < to; v += kTile) {
+        double left[kEach], all[kEach];
+        weights8<ELT>(row, v, to, left, all);
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) s.x += left[e], s.y += all[e];
     }
-    s.x = wave_sum(s.x), s.y = wave_sum(s.y);
-    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) a.sums[blockIdx.x] = double2{(waves[0].x + waves[1].x) + (waves[2].x + waves[3].x), (waves[0].y + waves[1].y) + (waves[2].y + waves[3].y)};
+    sum256(&s.x, &s.y);
+    if (threadIdx.x == 0 && part == 0) a.accepted[b] = row.accepted;
+    if (threadIdx.x == 0) a.sums[blockIdx.x] = s;
 }
 
+// The first lane whose running sum of weights (from *run on) passes the goal, -1 if none, and *run is behind them all then; *before: a lane's running sum without its own;
+// *last: the last lane with a weight, if there is one - where rounding lets no running sum pass, it is the one.
+__device__ __forceinline__ int find64(double w, double goal, double *run, int *last, double *before) {
+    const int lane = threadIdx.x & 63;
+    double upto = w;
+    for (int o = 1; o < 64; o <<= 1) {
+        const double v = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += v;
+    }
+    *before = *run + (upto - w);
+    const uint64_t some = __ballot(w > 0), passes = __ballot(w > 0 && *before + w > goal);
+    if (some) *last = 63 - __builtin_clzll(some);
+    *run += __shfl(upto, 63, 64);
+    return passes ? __builtin_ctzll(passes) : -1;
+}
+
+// One wavefront a request: what is left to do is a chain of dependent steps, and four wavefronts that meet at barriers took 9 us where this takes 6.
 template <int ELT>
-__global__ __launch_bounds__(256) void verify_draw_kernel(const VerifyDev a) {
-    __shared__ double before[256];
-    __shared__ int found, fallback, chosen;
-    __shared__ double base;
+__global__ __launch_bounds__(64) void verify_draw_kernel(const VerifyDev a) {
+    const int lane = threadIdx.x;
     const int64_t b = blockIdx.x;
-    const VerifyRow<ELT> row(a, b);
-    bool of_target = false;
-    if (threadIdx.x == 0) {
-        const double2 *s = a.sums + b * a.parts;
-        double left = 0, all = 0;
-        for (int i = 0; i < a.parts; ++i) left += s[i].x, all += s[i].y;
-        of_target = !(left > 0);  // nothing left (or sums that are no numbers): p itself
-        const double goal = (double)a.r[b] * (of_target ? all : left);
-        // the first part whose running sum passes the goal; rounding may leave none: the last one with a weight
-        double run = 0, start = 0;
-        int pick = -1;
-        for (int i = 0; i < a.parts; ++i) {
-            const double w = of_target ? s[i].y : s[i].x;
-            if (!(w > 0)) continue;
-            pick = i, start = run;
-            run += w;
-            if (run > goal) break;
-        }
-        chosen = pick | (of_target ? 1 << 30 : 0);
-        if (pick < 0) chosen = -1;
-        base = start;
-        before[0] = goal;
-        found = 256, fallback = -1;
+    const double2 *s = a.sums + b * a.parts;
+    const double r = (double)a.r[b];
+    const double2 mine = lane < a.parts ? s[lane] : double2{0, 0};
+    const VerifyRow<ELT> row(a, b, a.accepted[b]);
+    double left = mine.x, all = mine.y;
+    for (int i = lane + 64; i < a.parts; i += 64) left += s[i].x, all += s[i].y;
+    left = wave_sum(left), all = wave_sum(all);
+    const bool of_target = !(left > 0);  // nothing left (or sums that are no numbers): p itself
+    const double goal = r * (of_target ? all : left);
+    // the part, ...
+    int pick = -1, token = -1;
+    double run = 0, start = 0, before;
+    for (int i0 = 0; i0 < a.parts; i0 += 64) {
+        const double2 x = i0 == 0 ? mine : i0 + lane < a.parts ? s[i0 + lane] : double2{0, 0};
+        int last = -1;
+        const int got = find64(of_target ? x.y : x.x, goal, &run, &last, &before);
+        const int who = got >= 0 ? got : last;
+        if (who >= 0) pick = i0 + who, start = __shfl(before, who, 64);
+        if (got >= 0) break;
     }
-    __syncthreads();
-    const int pick = chosen;
-    const double goal = before[0], start = base;
-    __syncthreads();
-    int token = -1;
     if (pick >= 0) {
-        of_target = pick >> 30;
-        const int64_t from = (pick & ((1 << 30) - 1)) * a.part, to = min(a.vocab, from + a.part);
-        const int64_t each = (to - from + 255) / 256;
-        const int64_t mine = min(to, from + threadIdx.x * each), end = min(to, mine + each);
-        double sum = 0;
-        for (int64_t v = mine; v < end; ++v) {
-            const double2 w = row.weights(v);
-            sum += of_target ? w.y : w.x;
-        }
-        // running sums in front of each thread's elements, in order
-        before[threadIdx.x] = sum;
-        __syncthreads();
-        if (threadIdx.x < 64) {
-            double t[4], run = 0;
+        // ... the lane's eight elements of a quarter of a tile, and the one among them
+        const int64_t from = (int64_t)pick * a.part, to = min(a.vocab, from + a.part);
+        constexpr int kQuarter = 64 * kEach;
+        run = start;
+        bool found = false;
+        for (int64_t v0 = from; v0 < to && !found; v0 += kTile) {
+            double w[4][kEach], sum[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) t[j] = before[threadIdx.x * 4 + j], run += t[j];
-            double upto = run;
-            for (int w = 1; w < 64; w <<= 1) {
-                const double o = __shfl_up(upto, w, 64);
-                if ((int)threadIdx.x >= w) upto += o;
-            }
-            double x = start + (upto - run);
+            for (int k = 0; k < 4; ++k) {
+                const int64_t v = v0 + k * kQuarter + lane * kEach;
+                double t[kEach];
+                weights8<ELT>(row, v, to, w[k], t);
+                sum[k] = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) before[threadIdx.x * 4 + j] = x, x += t[j];
-        }
-        __syncthreads();
-        const double x = before[threadIdx.x];
-        if (sum > 0) {
-            atomicMax(&fallback, (int)threadIdx.x);
-            if (x + sum > goal) atomicMin(&found, (int)threadIdx.x);
-        }
-        __syncthreads();
-        const int who = found < 256 ? found : fallback;
-        if ((int)threadIdx.x == who) {
-            double run = x;
-            for (int64_t v = mine; v < end; ++v) {
-                const double2 w2 = row.weights(v);
-                const double w = of_target ? w2.y : w2.x;
-                if (!(w > 0)) continue;
-                token = (int)v;
-                run += w;
-                if (run > goal) break;
+                for (int e = 0; e < kEach; ++e) {
+                    if (of_target) w[k][e] = t[e];
+                    sum[k] += w[k][e];
+                }
             }
-            chosen = token;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (found) continue;
+                int last = -1;
+                const int got = find64(sum[k], goal, &run, &last, &before);
+                const int who = got >= 0 ? got : last;
+                found = got >= 0;
+                if (who < 0) continue;
+                int at = -1;
+                bool done = false;
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) {
+                    if (done || !(w[k][e] > 0)) continue;
+                    at = e;
+                    before += w[k][e];
+                    done = before > goal;
+                }
+                token = (int)(v0 + k * kQuarter) + who * kEach + __shfl(at, who, 64);
+            }
         }
-        __syncthreads();
-        token = chosen;
     }
-    for (int i = threadIdx.x; i <= a.drafts; i += 256)
+    for (int i = lane; i <= a.drafts; i += 64)
         a.tokens[b * (a.drafts + 1) + i] = i < row.accepted ? a.draft_tokens[b * a.drafts + i] : i == row.accepted ? token : -1;
-    if (threadIdx.x == 0) a.accepted[b] = row.accepted;
 }
 
-// Parts of a row: enough for the chip's workgroups, of 2048 elements at least.
+// Elements of a part: a tile, or as many tiles as keep the parts of all requests at about eight workgroups a CU.
+static int64_t verify_part(int64_t batch, int64_t vocab) {
+    const int64_t tiles = (vocab + kTile - 1) / kTile, each = batch * tiles / (8 * kNumCU);
+    return kTile * std::max<int64_t>(1, std::min<int64_t>(4, each));
+}
 static int64_t verify_parts(int64_t batch, int64_t vocab) {
-    const int64_t wanted = std::max<int64_t>(1, 4 * kNumCU / batch);
-    return std::max<int64_t>(1, std::min(wanted, (vocab + 2047) / 2048));
+    const int64_t part = verify_part(batch, vocab);
+    return (vocab + part - 1) / part;
 }
 
 template <int ELT>
@@ -189,7 +254,7 @@ static hipError_t launch_verify(const VerifyDev &a, int64_t batch, hipStream_t s
     hipLaunchKernelGGL((verify_sums_kernel<ELT>), dim3((uint32_t)(batch * a.parts)), dim3(256), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((verify_draw_kernel<ELT>), dim3((uint32_t)batch), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((verify_draw_kernel<ELT>), dim3((uint32_t)batch), dim3(64), 0, s, a);
     return hipGetLastError();
 }
 
@@ -201,6 +266,7 @@ extern "C" {
 
 int64_t atk_verify_workspace_bytes(int64_t batch, int64_t drafts, int64_t vocab) {
     if (batch < 1 || batch > (1 << 24) || drafts < 0 || drafts > (1 << 20) || vocab < 1 || vocab >= (INT64_C(1) << 30)) return ATK_ERR_ARGS;
+    if (batch * verify_parts(batch, vocab) >= (INT64_C(1) << 31)) return ATK_ERR_ARGS;  // workgroups
     return batch * verify_parts(batch, vocab) * (int64_t)sizeof(double2);
 }
 
@@ -225,7 +291,7 @@ int atk_verify_drafts(const void *target_probs, const int64_t target_stride[2], 
         if (a.ts[i] < 0 || a.ds[i] < 0) return ATK_ERR_ARGS;
     }
     a.vocab = vocab, a.drafts = (int)drafts, a.parts = (int)verify_parts(batch, vocab);
-    a.part = (vocab + a.parts - 1) / a.parts;
+    a.part = verify_part(batch, vocab);
     const hipStream_t s = (hipStream_t)stream;
     const hipError_t e = dtype == ATK_F32 ? launch_verify<ATK_F32>(a, batch, s) : dtype == ATK_BF16 ? launch_verify<ATK_BF16>(a, batch, s) : launch_verify<ATK_F16>(a, batch, s);
     return e == hipSuccess ? ATK_OK : set_hip_error(e);
