@@ -22,11 +22,24 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const AttnDev a) {
     const int d = (lane % LPR) * 4;
     f32x4 o = {0, 0, 0, 0};
     if (d < a.dim) {
-        for (int p = lane / LPR; p < a.parts; p += 64 / LPR) {
-            const float2 x = ml[p];
-            if (x.y == 0.0f) continue;  // no visible key in it
-            const float f = x.x == kNoMax ? 1.0f : __builtin_amdgcn_exp2f((x.x - m) * a.scale2);
-            o += f * *(const f32x4 *)(a.parts_o + (row * a.parts + p) * a.dim + d);
+        // eight parts in flight: one after the other their loads were nearly all of the time (64 samples, 17 parts: 9.9 us against 5.2)
+        constexpr int kStep = 64 / LPR;
+        const float *from = a.parts_o + row * a.parts * a.dim + d;
+        for (int p0 = lane / LPR; p0 < a.parts; p0 += 8 * kStep) {
+            float2 x[8];
+            f32x4 v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int p = min(p0 + j * kStep, a.parts - 1);
+                x[j] = ml[p];
+                v[j] = *(const f32x4 *)(from + (int64_t)p * a.dim);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (p0 + j * kStep >= a.parts || x[j].y == 0.0f) continue;  // (no visible key in it: nothing was written)
+                const float f = x[j].x == kNoMax ? 1.0f : __builtin_amdgcn_exp2f((x[j].x - m) * a.scale2);
+                o += f * v[j];
+            }
         }
     }
 #pragma unroll
@@ -93,36 +106,63 @@ static int check_attention(const atk_attention_args *p, bool pointers) {
     return ATK_OK;
 }
 
+// The shared keys in (at most) that many ranges of whole steps.
+static void split_prefix(const atk_attention_args *p, AttnPlan *pl, int64_t step, int64_t splits) {
+    const int64_t steps = attn_ceil(p->prefix_len, step);
+    pl->prefix_keys = (int)(attn_ceil(steps, std::min(steps, splits)) * step);
+    pl->prefix_splits = (int)attn_ceil(p->prefix_len, pl->prefix_keys);
+}
+
+// attn_block_kernel: four or eight wavefronts a workgroup, and how many ranges.  More ranges fill more CUs, and every range costs each row a partial result that is written and read
+// again.  In microseconds, as measured with heads of 128: a workgroup takes 7 and for each tile of 64 keys 2.2 with eight wavefronts, 1.4 with four and 2.5 with two workgroups
+// of four on a CU; partial results 0.65 a megabyte.
+static void plan_blocks(const atk_attention_args *p, int64_t rows, AttnPlan *pl) {
+    const double wide = pl->dp == 64 ? 0.6 : pl->dp == 128 ? 1.0 : 2.0;
+    const int64_t steps = attn_ceil(p->prefix_len, kBlockKeys);
+    double best = 0;
+    int64_t best_splits = 1;
+    pl->waves = 4;
+    for (int waves = 4; waves <= attn_max_waves(pl->dp); waves *= 2) {
+        const int64_t blocks = attn_ceil(rows, 32 * waves), base = blocks * p->kv_heads;
+        for (int64_t splits = 1; splits <= std::min<int64_t>(steps, 512); ++splits) {
+            const int64_t tiles = attn_ceil(steps, splits), groups = base * attn_ceil(steps, tiles);
+            const bool full = waves == 8 || (groups > kNumCU && pl->dp <= 128);
+            const double rounds = (double)attn_ceil(groups, waves == 4 && full ? 2 * kNumCU : kNumCU);
+            const double mb = 1e-6 * 4 * (double)(rows * p->kv_heads * p->dim) * (double)attn_ceil(steps, tiles);
+            const double us = rounds * (7 + tiles * wide * (waves == 8 ? 2.2 : full ? 2.5 : 1.4)) + 0.65 * mb;
+            if (best == 0 || us < best) best = us, best_splits = splits, pl->waves = waves;
+        }
+    }
+    pl->prefix_blocks = (int)attn_ceil(rows, 32 * pl->waves);
+    split_prefix(p, pl, kBlockKeys, best_splits);
+}
+
 static int plan_attention(const atk_attention_args *p, AttnPlan *pl) {
     const int group = (int)(p->heads / p->kv_heads);
     pl->dp = p->dim <= 64 ? 64 : p->dim <= 128 ? 128 : 256;
     const int64_t rows = p->batch * p->tokens * group, own_rows = p->tokens * group;
-    // how the shared keys meet the rows: up to two 16-row tiles in every wavefront, or 32 rows a wavefront and keys by way of LDS
-    pl->rt = rows <= 16 || p->prefix_len == 0 ? 1 : 2, pl->waves = kAttnWaves;
-    int64_t block = 16 * pl->rt, step = kAttnWaves * kTileKeys;
-    int64_t wanted = 2 * kNumCU;
-    const int64_t small = INT64_C(1) << 28;  // (four tokens' offsets are 32 bits)
-    if (rows > 32 && p->dtype != ATK_F32 && p->prefix_len > 0 && p->page_size % 4 == 0 && p->k_stride[1] < small && p->v_stride[1] < small) {
-        pl->rt = 0, pl->waves = rows <= 128 ? 4 : attn_max_waves(pl->dp);
-        block = 32 * pl->waves, step = kBlockKeys;
-        wanted = pl->waves == 8 ? kNumCU : 2 * kNumCU;
-    } else if (pl->rt > attn_max_rt(p->dtype, pl->dp)) {
-        pl->rt = 1, block = 16;
-    }
-    pl->prefix_blocks = (int)attn_ceil(rows, block);
-    const int64_t base = pl->prefix_blocks * p->kv_heads;
-    pl->prefix_splits = 0, pl->prefix_keys = 0;
-    if (p->prefix_len > 0) {
-        const int64_t steps = attn_ceil(p->prefix_len, step);
-        const int64_t splits = std::min(steps, std::max<int64_t>(1, wanted / base));
-        pl->prefix_keys = (int)(attn_ceil(steps, splits) * step);
-        pl->prefix_splits = (int)attn_ceil(p->prefix_len, pl->prefix_keys);
-    }
-    // a sequence's own keys: as many as its row could hold, the device knows how many there are
-    const int64_t own = p->row_pages * p->page_size - p->prefix_len;
+    // a sequence's own keys: as many as its row could hold, the device knows how many there are; workgroups for about three a CU
+    const int64_t own = p->row_pages * p->page_size - p->prefix_len, step = kAttnWaves * kTileKeys;
     pl->own_blocks = (int)attn_ceil(own_rows, 16);
     const int64_t own_base = p->batch * p->kv_heads * pl->own_blocks;
-    pl->own_splits = own > 0 ? (int)std::min(attn_ceil(own, kAttnWaves * kTileKeys), std::max<int64_t>(1, 2 * kNumCU / own_base)) : 0;
+    pl->own_splits = own > 0 ? (int)std::min(attn_ceil(own, step), std::max<int64_t>(1, 3 * kNumCU / own_base)) : 0;
+    // how the shared keys meet the rows: up to two 16-row tiles in every wavefront, or 32 rows a wavefront and keys by way of LDS
+    // (attn_block_kernel's addresses: four tokens' offsets and a page's place in 16 bytes are 32 bits)
+    auto reaches = [&](const int64_t *stride) {
+        const int64_t most = INT64_C(1) << 34;
+        return stride[1] < (INT64_C(1) << 28) && stride[1] <= most / p->page_size && stride[0] <= most / p->n_pages;
+    };
+    pl->rt = rows <= 16 || p->prefix_len == 0 ? 1 : 2, pl->waves = kAttnWaves;
+    pl->prefix_splits = 0, pl->prefix_keys = 0;
+    if (rows > 32 && p->dtype != ATK_F32 && p->prefix_len > 0 && p->page_size % 4 == 0 && reaches(p->k_stride) && reaches(p->v_stride)) {
+        pl->rt = 0;
+        plan_blocks(p, rows, pl);
+    } else {
+        if (pl->rt > attn_max_rt(p->dtype, pl->dp)) pl->rt = 1;
+        pl->prefix_blocks = (int)attn_ceil(rows, 16 * pl->rt);
+        if (p->prefix_len > 0) split_prefix(p, pl, step, std::max<int64_t>(1, 2 * kNumCU / (pl->prefix_blocks * p->kv_heads)));
+    }
+    const int64_t base = pl->prefix_blocks * p->kv_heads;
     pl->rows = p->batch * p->tokens * p->heads;
     pl->parts = pl->prefix_splits + pl->own_splits;
     pl->o_bytes = pl->rows * pl->parts * p->dim * 4;
@@ -166,6 +206,7 @@ int atk_shared_prefix_attention(const atk_attention_args *p, void *work, int64_t
     a.own_splits = pl.own_splits, a.own_blocks = pl.own_blocks;
     a.n_prefix = pl.prefix_splits * pl.prefix_blocks * a.kv_heads;
     a.prefix_grid = (a.n_prefix + 7) / 8 * 8;
+    a.masked_grid = 0, a.block_rows = pl.rt == 0 ? 32 * pl.waves : 0;
     a.n_own = a.batch * a.kv_heads * pl.own_blocks * pl.own_splits;
     a.parts = (int)pl.parts;
     a.page.set((uint32_t)p->page_size);

@@ -42,6 +42,7 @@ struct AttnDev {
     int prefix_splits, prefix_blocks, prefix_keys;  // ranges of the shared keys, row blocks, keys of a range (a multiple of a workgroup's tiles)
     int own_splits, own_blocks;
     int n_prefix, prefix_grid, n_own;  // units of the shared keys and workgroups for them, which come first; units of own keys
+    int masked_grid, block_rows;       // workgroups that look for attn_block_kernel's units with masks; rows of such a unit
     int parts;         // prefix_splits + own_splits
     FastDiv page;
     float scale, scale2;  // scale2: scale * log2(e)
@@ -249,9 +250,12 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
     }
     const char *kh = (const char *)a.k + h * a.ks[2] * E::kBytes, *vh = (const char *)a.v + h * a.vs[2] * E::kBytes;
 
+    // lane j (and j + 32) looks key k0 + j up, a tile ahead; keys past the end are read as the last one and masked
+    auto page_of = [&](int k0) { return table_row[a.page.div(min(k0 + (lane & 31), kb - 1))]; };
+    int page_next = ka < kb ? page_of(ka + wave * kTileKeys) : 0;
     for (int k0 = ka + wave * kTileKeys; k0 < kb; k0 += NW * kTileKeys) {
-        // lane j (and j + 32) looks key k0 + j up; keys past the end are read as the last one and masked
-        int page = table_row[a.page.div(min(k0 + (lane & 31), kb - 1))];
+        int page = page_next;
+        page_next = page_of(min(k0 + NW * kTileKeys, kb - 1));
         const bool good = (unsigned)page < (unsigned)a.n_pages;
         bad_page |= !good;
         if (!good) page = 0;
@@ -437,16 +441,20 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
 // ------------------------------------------------------------------------------------ many rows on shared keys, 16-bit types
 //
 // With more rows than a tile or two the shared keys are bound by the matrix units and the exponentials, so a key's data should come to a wavefront once for
-// 32 rows and to a CU once for all of its rows: a workgroup's NW wavefronts have 32 rows each, and 64 keys at a time pass through LDS, in two
-// buffers - the next tile is written to the other one while this one is worked on, from loads that were given out a tile earlier.
+// 32 rows and to a CU once for all of its rows: a workgroup's NW wavefronts have 32 rows each, and 64 keys at a time pass through LDS.
 //   S^T = K Q^T and O^T = V^T P^T by 32x32x16 matrix instructions, half the operands' reads of 16x16x32 for a product.  A lane has one query (lane % 32) and of
-//   each 32 keys those with 8 * i + 4 * (lane / 32) + 0..3; step s of the second product takes i = 2 s and 2 s + 1.
+//   each 32 keys those with 8 * i + 4 * (lane / 32) + 0..3; step x of the second product takes i = 2 x and 2 x + 1.
 //   A tile is a phase of products (those of the tile before with V, this one's with K) and one of vector instructions (maximum, exponentials, packing, the next
-//   tiles' addresses and stores), and each SIMD has two wavefronts of the workgroup, one of each half: the second half is a phase late, so that one of the two has the matrix
-//   units while the other one has the vector unit.  In step they took 2.6 times as long.
-//   V lies in LDS by d, a lane's eight keys of a step side by side: transposed in registers on the way in (a lane has loaded two d's of eight keys), so that
-//   both operands are single 16-byte reads.  Rows in LDS are 16 bytes longer than their data: lanes a row apart meet in different banks.
+//   tiles' loads), and with eight wavefronts each SIMD has two of them, one of each half: the second half is a phase late, so that one of the two has the matrix
+//   units while the other one has the vector unit.  128 samples of 32 heads on 65536 keys: 139 us, 0.99 PFLOP/s where a large matrix product reaches 1.1; the matrix units are busy for
+//   55 % of the cycles, and the clock is down to 1.7 GHz, as it is under matrix products of such data alone.  With one meeting of the wavefronts a tile in place of two: 160 us.
+//   K and V come from memory into LDS without passing through registers, row by row, 1 KB an instruction, a tile ahead.  (By way of registers, with V transposed there, the loads' and
+//   stores' instructions were half of the vector phase: 128 samples' 65536 keys took 184 us, and take 139.)  V is transposed on the way out, by
+//   the transposing reads: 16 lanes get 16 d's of four keys.
+//   Rows lie in LDS without gaps, so a row's 16-byte pieces are permuted (piece ^ a few bits of the key) for lanes a row apart to meet in different banks; the lane that brings a
+//   piece in takes its place's piece from memory.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 template <int ELT>
 __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c) {
@@ -456,149 +464,145 @@ __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
+// 16 bytes of each lane from base + off to LDS at `lds` + 16 * lane.  (Nothing but vmcnt waits for it, and no wait that the compiler inserts, which by the builtin are for all of them
+// in front of every read from LDS.)
+__device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void load_to_lds(const char *address, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(address) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // until all but the last N are there
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
 constexpr int kBlockKeys = 64;
-template <int DP>
+template <int DP, int NW>
 struct BlockLds {
-    static constexpr int kK = DP * 2 + 16;                 // bytes of a key's row of K
-    static constexpr int kV = kBlockKeys * 2 + 16;         // bytes of a d's row of V
-    static constexpr int kBuffer = kBlockKeys * kK + DP * kV;
-    static constexpr int kBytes = 2 * kBuffer;
+    static constexpr int kRow = DP * 2;                    // bytes of a key's row
+    static constexpr int kTile = kBlockKeys * kRow;
+    static constexpr int kBuffers = NW == 8 ? 3 : 2;       // of K and of V: wavefronts a phase apart hold one longer
+    static constexpr int kRing = 64;                       // tiles whose addresses are at hand
+    static constexpr int kData = 2 * kBuffers * kTile;
+    static constexpr int kBytes = kData + 2 * kRing * 16 * 4;
 };
 
-// Rows r0 .. r0 + 32 * NW - 1 of head h against keys ka .. kb - 1 (one at least), all of which every one of these rows sees.  FULL: dim == DP.
+// Rows r0 .. r0 + 32 * NW - 1 of head h against keys ka .. kb - 1 (one at least), all of which every one of these rows has to see: nothing is written if one does not.
+// FULL: dim == DP.
 template <int ELT, int DP, int NW, bool FULL>
 __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int n_rows, const int32_t *table_row, int ka, int kb, int part, char *lds) {
     typedef AttnElt<ELT> E;
-    typedef BlockLds<DP> L;
+    typedef BlockLds<DP, NW> L;
     constexpr int NS = DP / 16;                            // steps of the first product
     constexpr int ND = DP / 32;                            // tiles of d
-    constexpr int KC = kBlockKeys * DP / 8 / (NW * 64);    // 16-byte pieces of K that a thread brings in
-    constexpr int PL = DP / 2;                             // lanes of a row of V, two d's each
-    constexpr bool kSpare = 8 * PL < NW * 64;              // ... the last wavefronts bring in none of V
-    constexpr int VC = kSpare ? 1 : 8 * PL / (NW * 64);    // ... loads of eight keys of a thread
-    constexpr bool kHalves = DP == 64;                     // a wavefront's load is of eight keys of K, of four keys of two groups of V: one half each
-    static_assert(KC >= 1 && (DP == 64 || DP == 128 || DP == 256), "every thread has its share");
+    constexpr int kPieces = DP / 8;                        // 16-byte pieces of a row
+    constexpr int kLoads = L::kTile / 1024 / NW;           // of K, and of V, of a wavefront and tile
+    constexpr int kLoadKeys = 64 / kPieces;                // keys of one
+    constexpr bool kHalves = kLoadKeys == 8;               // two times four keys
+    static_assert(kLoads >= 1 && (DP == 64 || DP == 128 || DP == 256), "every wavefront has its share");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, g = lane >> 5;
     const char *kh = (const char *)a.k + h * a.ks[2] * 2, *vh = (const char *)a.v + h * a.vs[2] * 2;
     const int tiles = (kb - ka + kBlockKeys - 1) / kBlockKeys;
 
-    // What comes in.  Four keys that begin at a multiple of four lie in one page (page_size % 4 == 0, and so ka), so a wavefront's loads have scalar
-    // addresses, each found by a lane of its own, and offsets that stay the same: with an address for each lane's key, exchanged between lanes, or with
-    // scalar arithmetic alone they took 1100 cycles of a wavefront and tile, as long as all of its products.
-    // Thread's piece c of K: key (c * NW * 64 + thread) / (DP / 8); of V: group of eight keys (x, s, half), 32 x + 16 s + 4 half + {0..3, 8..11}, and two d's.
-    constexpr int kRow = DP / 8;
-    const int k_lane_key = kRow < 64 ? lane / kRow : 0, k_piece = (kRow < 64 ? lane : threadIdx.x) % kRow;
-    auto k_key = [&](int c) { return (c * NW * 64 + wave * 64) / kRow; };          // of the wavefront's first lane
-    auto v_group = [&](int c) { return (c * NW * 64 + wave * 64) / PL; };
-    const int v_d = (kHalves ? lane % 32 : (int)threadIdx.x % PL) * 2;
-    const uint32_t k_step = (uint32_t)a.ks[1] * 2, v_step = (uint32_t)a.vs[1] * 2;
-    // (halves: lanes 32 to 63 have a base of their own, and keys from its beginning)
-    const uint32_t k_off = (uint32_t)(kHalves ? (lane % 32) / kRow : k_lane_key) * k_step + k_piece * 16;
-    const uint32_t v_off = v_d * 2;
-    const bool upper = kHalves && lane >= 32;
-    int bad_page = 0;
-    // Lane x (of each 16) looks after keys 4 x .. 4 x + 3 of a tile; tiles past the last are read as that one (brought in and not used: no branches), keys past
-    // the end as the last four.
-    auto key_of = [&](int t) { return min(ka + min(t, tiles - 1) * kBlockKeys + (lane & 15) * 4, (kb - 1) & ~3); };
-    auto page_of = [&](int t) { return table_row[a.page.div(key_of(t))]; };
-    auto base_of = [&](int t, int page, const int64_t *stride) {
-        if ((unsigned)page >= (unsigned)a.n_pages) bad_page = ATK_STATUS_BAD_PAGE, page = 0;
-        return ((int64_t)page * stride[0] + (int64_t)a.page.mod(key_of(t)) * stride[1]) * 2;
-    };
-    auto scalar_base = [&](int64_t bases, int key) {  // of the four keys at `key` of the tile
-        const uint32_t lo = __builtin_amdgcn_readlane((int)bases, key >> 2), hi = __builtin_amdgcn_readlane((int)(bases >> 32), key >> 2);
-        return (int64_t)((uint64_t)hi << 32 | lo);
-    };
-    const bool alike = a.ks[0] == a.vs[0] && a.ks[1] == a.vs[1];
-    auto k_group_key = [&](int x) {  // first key of the four keys of base x
-        return kHalves ? k_key(x / 2) + x % 2 * 4 : k_key(x) & ~3;
-    };
-    auto v_group_key = [&](int x) {
-        const int group = kHalves ? v_group(x / 4) + x % 2 : v_group(x / 2), second = kHalves ? x / 2 % 2 : x % 2;
-        return (group >> 1) * 16 + (group & 1) * 4 + second * 8;
-    };
-    u32x4 kr[KC];
-    uint32_t vr[VC][8];
-    auto load_k = [&](int64_t bases) {
-        const bool in = FULL || k_piece * 8 < a.dim;
-#pragma unroll
-        for (int c = 0; c < KC; ++c) {
-            int64_t at;
-            uint32_t off = k_off;
-            if constexpr (kHalves) {
-                const int64_t lo = scalar_base(bases, k_group_key(2 * c)), hi = scalar_base(bases, k_group_key(2 * c + 1));
-                at = upper ? hi : lo;
-            } else {
-                at = scalar_base(bases, k_group_key(c));
-                if (DP == 256) off += (k_key(c) & 3) * k_step;
-            }
-            kr[c] = in ? *(const u32x4 *)(kh + at + off) : u32x4{0, 0, 0, 0};
-        }
-    };
-    auto load_v = [&](int64_t bases) {
-        if (kSpare && wave * 64 >= 8 * PL) return;
-        const bool in = FULL || v_d < a.dim;
-#pragma unroll
-        for (int c = 0; c < VC; ++c)
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                int64_t at;
-                if constexpr (kHalves) {
-                    const int64_t lo = scalar_base(bases, v_group_key(4 * c + 2 * y)), hi = scalar_base(bases, v_group_key(4 * c + 2 * y + 1));
-                    at = upper ? hi : lo;
-                } else {
-                    at = scalar_base(bases, v_group_key(2 * c + y));
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) vr[c][4 * y + j] = in ? *(const uint32_t *)(vh + at + (v_off + j * v_step)) : 0u;
-            }
-    };
-    char *const k_lds = lds, *const v_lds = lds + 2 * kBlockKeys * L::kK;
-    auto store_k = [&](int t) {
-        char *k = k_lds + (t & 1) * kBlockKeys * L::kK + k_lane_key * L::kK + k_piece * 16;
-#pragma unroll
-        for (int c = 0; c < KC; ++c) *(u32x4 *)(k + k_key(c) * L::kK) = kr[c];
-    };
-    auto store_v = [&](int t) {
-        if (kSpare && wave * 64 >= 8 * PL) return;
-        const int left = kb - ka - t * kBlockKeys;
-        if (left < kBlockKeys && left > 0) {  // what lies behind the last key has weight 0, which NaN would not heed
-            asm volatile("");
-#pragma unroll
-            for (int c = 0; c < VC; ++c)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int group = v_group(c) + (upper ? 1 : 0);
-                    if ((group >> 1) * 16 + (group & 1) * 4 + (j >> 2) * 8 + (j & 3) >= left) vr[c][j] = 0;
-                }
-        }
-        char *v = v_lds + (t & 1) * DP * L::kV + v_d * L::kV + (upper ? 16 : 0);
-#pragma unroll
-        for (int c = 0; c < VC; ++c) {
-            u32x4 even, odd;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                even[j] = __builtin_amdgcn_perm(vr[c][2 * j + 1], vr[c][2 * j], 0x05040100u);
-                odd[j] = __builtin_amdgcn_perm(vr[c][2 * j + 1], vr[c][2 * j], 0x07060302u);
-            }
-            *(u32x4 *)(v + v_group(c) * 16) = even;
-            *(u32x4 *)(v + L::kV + v_group(c) * 16) = odd;
-        }
-    };
-
+    // the query of a lane
     const int r = r0 + wave * 32 + n;
     const bool real = r < n_rows;
     const AttnRow x = attn_row(a, h, real ? r : 0, -1);
+    bool bad = false;
+    const int sees = seq_len(a, seq_row(a, x.b, &bad), &bad) - (a.tokens - 1 - x.t);
+
+    // What comes in.  Four keys that begin at a multiple of four lie in one page (page_size % 4 == 0, and so ka): a load has the address of its four keys, a scalar that a
+    // wavefront finds in LDS, and offsets that stay the same.  Addresses are looked up by all threads together, for 64 tiles and then 32 at a time, in units of 16 bytes.  (Looked up
+    // by every wavefront for each tile, with 64-bit products, they took as long as the tile's exponentials: 128 samples' 65536 keys 152 us.)
+    // Load c of a wavefront brings keys first_key(c) + lane / kPieces, place lane % kPieces of the row.
+    auto first_key = [&](int c) { return (c * NW + wave) * kLoadKeys; };
+    const int in_load = lane / kPieces, place = lane % kPieces;
+    auto k_swizzle = [](int key) { return DP == 64 ? key & 7 : key & 15; };
+    auto v_swizzle = [](int key) { return DP == 64 ? (key & 2) << 1 : (key & 3) << 2; };  // (half a wavefront reads 64 bytes of four keys at once)
+    // (the same for all c but for K's with 256: loads are eight keys apart there)
+    const int k_piece = place ^ k_swizzle(first_key(0) + in_load), v_piece = place ^ v_swizzle(first_key(0) + in_load);
+    const uint32_t in_group = kHalves ? in_load & 3 : in_load;  // key of the four (from first_key(c) & 3 on)
+    const uint32_t k_step = (uint32_t)a.ks[1] * 2, v_step = (uint32_t)a.vs[1] * 2;
+    bool bad_page = false;
+    uint32_t *const k_ring = (uint32_t *)(lds + L::kData), *const v_ring = k_ring + L::kRing * 16;
+    // tiles past the last are that one once more (brought in and not used: no branches), keys past the end the last four
+    auto look_up = [&](int t0, int count) {
+        for (int i = threadIdx.x; i < count * 16; i += NW * 64) {
+            const int t = t0 + i / 16, key = min(ka + min(t, tiles - 1) * kBlockKeys + i % 16 * 4, (kb - 1) & ~3);
+            int page = table_row[a.page.div(key)];
+            if ((unsigned)page >= (unsigned)a.n_pages) bad_page = true, page = 0;
+            const int64_t slot = a.page.mod(key);
+            const int at = t % L::kRing * 16 + i % 16;
+            k_ring[at] = (uint32_t)((page * a.ks[0] + slot * a.ks[1]) >> 3);
+            v_ring[at] = (uint32_t)((page * a.vs[0] + slot * a.vs[1]) >> 3);
+        }
+    };
+    const uint32_t k_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds, v_lds = k_lds + L::kBuffers * L::kTile;
+    struct Bases {
+        uint32_t at[kLoads * (kHalves ? 2 : 1)];  // of the four keys of each load, 16 bytes
+    };
+    auto bases_of = [&](const uint32_t *ring, int t) {
+        Bases y;
+        ring += t % L::kRing * 16;
+#pragma unroll
+        for (int c = 0; c < kLoads; ++c) {
+            if constexpr (kHalves) {
+                y.at[2 * c] = ring[first_key(c) / 4], y.at[2 * c + 1] = ring[first_key(c) / 4 + 1];
+            } else {
+                y.at[c] = ring[first_key(c) / 4];
+            }
+        }
+        return y;
+    };
+    auto load = [&](const char *head, const Bases &y, uint32_t step, int piece, bool k, uint32_t to) {
+#pragma unroll
+        for (int c = 0; c < kLoads; ++c) {
+            const int first = first_key(c);
+            const int p = DP == 256 && k ? piece ^ (first & 8) ^ (first_key(0) & 8) : piece;
+            const uint32_t off = in_group * step + p * 16;
+            const uint32_t at = to + (uint32_t)(c * NW + wave) * 1024;
+            if (FULL || p * 8 < a.dim) {
+                if constexpr (kHalves) {
+                    load_to_lds(head + ((uint64_t)(lane < 32 ? y.at[2 * c] : y.at[2 * c + 1]) << 4) + off, at);
+                } else {
+                    const uint32_t base = __builtin_amdgcn_readfirstlane(y.at[c]);
+                    load_to_lds(head + ((uint64_t)base << 4), DP == 256 ? off + (first & 3) * step : off, at);
+                }
+            }
+        }
+    };
+    auto buffer = [&](int t) { return (uint32_t)(t % L::kBuffers) * L::kTile; };
+    auto load_k = [&](int t, const Bases &y) { load(kh, y, k_step, k_piece, true, k_lds + buffer(t)); };
+    auto load_v = [&](int t, const Bases &y) { load(vh, y, v_step, v_piece, false, v_lds + buffer(t)); };
+
+    // The phases bring in K two tiles ahead and V one; the second half of the wavefronts, a phase late, one more.
+    const int late = NW == 8 ? wave >> 2 : 0;
+    look_up(0, min(L::kRing, tiles + 4));
+    if constexpr (!FULL) {  // pieces past dim stay 0
+        for (int i = threadIdx.x; i < L::kData / 16; i += NW * 64) ((u32x4 *)lds)[i] = u32x4{0, 0, 0, 0};
+    }
+    if (!__syncthreads_and(!real || sees >= kb)) return;
+    load_k(0, bases_of(k_ring, 0));
+    load_k(1, bases_of(k_ring, 1));
+    load_v(0, bases_of(v_ring, 0));
+    if (late) {
+        load_k(2, bases_of(k_ring, 2));
+        load_v(1, bases_of(v_ring, 1));
+    }
     u32x4 q[NS];
     {
         const char *p = (const char *)a.q + (x.b * a.qs[0] + x.t * a.qs[1] + x.head * a.qs[2]) * 2;
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             const int at = (s * 2 + g) * 16;
-            q[s] = at < a.dim * 2 ? *(const u32x4 *)(p + at) : u32x4{0, 0, 0, 0};
+            q[s] = FULL || at < a.dim * 2 ? *(const u32x4 *)(p + at) : u32x4{0, 0, 0, 0};
         }
     }
+    wait_loads<0>();
+    __syncthreads();
+
     float m = kNoMax, l = 0.0f;
     bool far = false;
     f32x16 acc[ND];
@@ -606,32 +610,6 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
     for (int i = 0; i < ND; ++i)
 #pragma unroll
         for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
-
-    // What the phases bring in for the next ones: K a tile ahead, V for this one; the second half of the wavefronts, a phase late, one tile more.
-    const int late = NW == 8 ? wave >> 2 : 0;
-    int page = page_of(0), page_next = page_of(1);
-    int64_t bases = base_of(0, page, a.ks), bases_v = base_of(0, page, a.vs);  // of the tile whose K, V is brought in next
-    load_k(bases);
-    store_k(0);
-    auto step = [&](int t) {  // from tile t's addresses to tile t + 1's; its page came in a step earlier
-        bases_v = alike ? bases : base_of(t, page, a.vs);
-        page = page_next;
-        bases = base_of(t + 1, page, a.ks);
-    };
-    step(0);
-    if (late) {
-        page_next = page_of(2);
-        load_v(bases_v);
-        store_v(0);
-        load_k(bases);
-        store_k(1);
-        step(1);
-    }
-    load_k(bases);       // tile 1 + late
-    load_v(bases_v);     // tile late
-    page_next = page_of(2 + late);
-    step(1 + late);
-    page_next = page_of(3 + late);
     f32x16 s[2];
     u32x4 p[2][2];
     auto barrier = [&]() {
@@ -639,22 +617,33 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
         __syncthreads();
         __builtin_amdgcn_sched_barrier(0);
     };
-    // Products of tile t with V and of tile t + 1 with K (either may be left out).  Reads from LDS run kAhead products in front: one takes four products' time.
-    constexpr int kFirst = 2 * NS, kSecond = 4 * ND, kAhead = 6;
+    // Products of tile t with V and of tile t + 1 with K (either may be left out).  Reads from LDS run kAhead in front: one takes four products' time.
+    const int q16 = lane >> 4, i16 = lane & 15, v_key = 4 * (q16 >> 1) + i16 / 4;
+    const uint32_t k_at = n * L::kRow + ((g ^ k_swizzle(n)) << 4);
+    const uint32_t v_at = v_key * L::kRow + ((((q16 & 1) * 2 + (i16 & 3) / 2) ^ v_swizzle(v_key)) << 4) + (i16 & 1) * 8;
+    typedef const __attribute__((address_space(3))) u32x4 *Lds16;
+    typedef __attribute__((address_space(3))) s16x4 *Lds8;
     auto products = [&](auto second, auto first, int t) {
-        constexpr bool kBoth = decltype(second)::value && decltype(first)::value;
-        const char *k = k_lds + ((t + 1) & 1) * kBlockKeys * L::kK, *v = v_lds + (t & 1) * DP * L::kV;
+        constexpr bool kSecond = decltype(second)::value, kFirst = decltype(first)::value;
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
-        if constexpr (decltype(second)::value) {
+        if constexpr (kSecond) {
+            const uint32_t v = v_lds + buffer(t) + v_at;
 #pragma unroll
             for (int y = 0; y < 2; ++y)
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
+                for (int z = 0; z < 2; ++z)
 #pragma unroll
-                    for (int i = 0; i < ND; ++i) acc[i] = mma32<ELT>(*(const u32x4 *)(v + (i * 32 + n) * L::kV + (y * 4 + x * 2 + g) * 16), p[y][x], acc[i]);
+                    for (int i = 0; i < ND; ++i) {
+                        const uint32_t at = (v ^ (i << 6)) + (y * 2 + z) * 16 * L::kRow;
+                        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds8)(uintptr_t)at);
+                        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds8)(uintptr_t)(at + 8 * L::kRow));
+                        const u32x2 lw = __builtin_bit_cast(u32x2, lo), hw = __builtin_bit_cast(u32x2, hi);
+                        acc[i] = mma32<ELT>(u32x4{lw[0], lw[1], hw[0], hw[1]}, p[y][z], acc[i]);
+                    }
         }
-        if constexpr (decltype(first)::value) {
+        if constexpr (kFirst) {
+            const uint32_t k = k_lds + buffer(t + 1) + k_at;
 #pragma unroll
             for (int y = 0; y < 2; ++y)
 #pragma unroll
@@ -662,16 +651,28 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
 #pragma unroll
             for (int i = 0; i < NS; ++i)
 #pragma unroll
-                for (int y = 0; y < 2; ++y) s[y] = mma32<ELT>(*(const u32x4 *)(k + (y * 32 + n) * L::kK + (i * 2 + g) * 16), q[i], s[y]);
+                for (int y = 0; y < 2; ++y) s[y] = mma32<ELT>(*(Lds16)(uintptr_t)((k ^ (i << 5)) + y * 32 * L::kRow), q[i], s[y]);
         }
-        constexpr int kAll = kBoth ? kFirst + kSecond : decltype(first)::value ? kFirst : kSecond;
+        // (of the second product, two reads each)
+        constexpr int kReads = (kSecond ? 8 * ND : 0) + (kFirst ? 2 * NS : 0), kAhead = 8;
         __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);  // reads from LDS
+        int reads = kAhead;
+        if constexpr (kSecond) {
 #pragma unroll
-        for (int i = 0; i < kAll - kAhead; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);     // a product
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            for (int i = 0; i < 4 * ND; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);  // a product
+                if (reads < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                reads += 2;
+            }
         }
-        __builtin_amdgcn_sched_group_barrier(0x8, kAhead, 0);
+        if constexpr (kFirst) {
+#pragma unroll
+            for (int i = 0; i < 2 * NS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                if (reads < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                reads += 1;
+            }
+        }
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -727,36 +728,44 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
                 sum += s[y][j];
             }
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-                p[y][x] = u32x4{E::pack(s[y][8 * x], s[y][8 * x + 1]), E::pack(s[y][8 * x + 2], s[y][8 * x + 3]), E::pack(s[y][8 * x + 4], s[y][8 * x + 5]),
-                                E::pack(s[y][8 * x + 6], s[y][8 * x + 7])};
+            for (int z = 0; z < 2; ++z)
+                p[y][z] = u32x4{E::pack(s[y][8 * z], s[y][8 * z + 1]), E::pack(s[y][8 * z + 2], s[y][8 * z + 3]), E::pack(s[y][8 * z + 4], s[y][8 * z + 5]),
+                                E::pack(s[y][8 * z + 6], s[y][8 * z + 7])};
         }
         l += sum;
     };
-    barrier();
+    // One meeting a tile: the first half of the wavefronts comes from its vector phase, the second from its products.  It says that what the next products read has come in, and
+    // that the tile whose buffers the next loads fill has been read.  (Four wavefronts, in step and with a buffer less, meet behind their products too.)
+    auto end = [&]() {  // of what the last tile needs; what lies behind the last key has weight 0, which NaN would not heed
+        wait_loads<0>();
+        const int left = kb - ka - (tiles - 1) * kBlockKeys;
+        if (left < kBlockKeys) {
+#pragma unroll
+            for (int c = 0; c < kLoads; ++c)
+                if (first_key(c) + in_load >= left)
+                    *(__attribute__((address_space(3))) u32x4 *)(uintptr_t)(v_lds + buffer(tiles - 1) + (c * NW + wave) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+        }
+        barrier();
+    };
     if (late) barrier();
     products(No{}, Yes{}, -1);
     barrier();
     for (int t = 0; t < tiles - 1; ++t) {
-        const int page_new = page_of(t + 4 + late);  // (in front of the data's loads: what waits for it does not wait for them)
+        if (tiles > L::kRing && t > 0 && t % (L::kRing / 2) == 0) look_up(t + L::kRing / 2, L::kRing / 2);  // over the addresses of tiles that are there
+        const Bases next_k = bases_of(k_ring, t + 2 + late), next_v = bases_of(v_ring, t + 1 + late);
+        load_k(t + 2 + late, next_k);
+        load_v(t + 1 + late, next_v);
         softmax(t);
-        store_k(t + 1 + late);
-        store_v(t + late);
-        load_k(bases);
-        load_v(bases_v);
-        step(t + 2 + late);
-        page_next = page_new;
+        wait_loads<2 * kLoads>();
         barrier();
         products(Yes{}, Yes{}, t);
         barrier();
     }
     softmax(tiles - 1);
-    store_v(tiles - 1 + late);
-    barrier();
+    end();
     products(Yes{}, No{}, tiles - 1);
     if (!late && NW == 8) barrier();
-    bad_page |= __any(bad_page) ? ATK_STATUS_BAD_PAGE : 0;
-    if (bad_page && a.status && lane == 0) atomicOr(a.status, bad_page);
+    if (bad_page && a.status) atomicOr(a.status, ATK_STATUS_BAD_PAGE);
     l += __shfl_xor(l, 32, 64);
     if (!real) return;
     const int64_t row = ((int64_t)x.b * a.tokens + x.t) * a.heads + x.head;
@@ -767,7 +776,7 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int d = i * 32 + j * 8 + g * 4;
-            if (d < a.dim) *(f32x4 *)(o + d) = f32x4{acc[i][4 * j], acc[i][4 * j + 1], acc[i][4 * j + 2], acc[i][4 * j + 3]};
+            if (FULL || d < a.dim) *(f32x4 *)(o + d) = f32x4{acc[i][4 * j], acc[i][4 * j + 1], acc[i][4 * j + 2], acc[i][4 * j + 3]};
         }
 }
 
@@ -801,54 +810,67 @@ __device__ __forceinline__ void attn_own(const AttnDev &a, int y, char *lds) {
 template <int DP, int RT, int NW>
 constexpr int attn_lds_bytes() { return 2 * NW * RT * 16 * 4 + RT * 16 * (DP + 4) * 4; }
 
-// Few rows on the shared keys: the wavefronts of a workgroup share its keys out.
+// A unit of the shared keys: head, rows and keys.
+struct SharedUnit {
+    int h, block, split, row, ka, kb;
+    __device__ __forceinline__ SharedUnit(const AttnDev &a, int u) {
+        bool bad = false;  // (told by attn_range)
+        block = u % a.prefix_blocks, h = u / a.prefix_blocks % a.kv_heads, split = u / (a.prefix_blocks * a.kv_heads);
+        row = seq_row(a, 0, &bad);
+        ka = split * a.prefix_keys, kb = row < 0 ? ka : min(a.prefix_len, ka + a.prefix_keys);
+    }
+};
+
+// Few rows on the shared keys: the wavefronts of a workgroup share its keys out.  Own keys.  Of attn_block_kernel's units (masked_grid), those with a row that sees only a part of the
+// keys - a sequence that ends before them: tile by tile, with masks.
 template <int ELT, int DP, int RT>
-__global__ __launch_bounds__(kAttnWaves * 64) void attn_range_kernel(const AttnDev a) {
+__global__ __launch_bounds__(kAttnWaves * 64, RT == 1 && DP <= 128 ? 2 : 1) void attn_range_kernel(const AttnDev a) {
     __shared__ __align__(16) char lds[attn_lds_bytes<DP, RT, kAttnWaves>()];
-    const int id = blockIdx.x;
-    if (id >= a.prefix_grid) {
-        attn_own<ELT, DP, kAttnWaves>(a, id - a.prefix_grid, lds);
+    int id = blockIdx.x;
+    const int n_rows = a.batch * a.tokens * a.group;
+    if (id < a.prefix_grid) {
+        const int u = xcd_unit(id, a.n_prefix);
+        if (u < 0) return;
+        const SharedUnit s(a, u);
+        attn_range<ELT, DP, RT, kAttnWaves>(a, s.h, s.block * RT * 16, n_rows, -1, a.table + s.row * a.table_stride, s.ka, s.kb, s.split, lds);
         return;
     }
-    const int u = xcd_unit(id, a.n_prefix);
-    if (u < 0) return;
-    bool bad = false;
-    const int block = u % a.prefix_blocks, h = u / a.prefix_blocks % a.kv_heads, split = u / (a.prefix_blocks * a.kv_heads);
-    const int row = seq_row(a, 0, &bad);
-    const int ka = split * a.prefix_keys, kb = row < 0 ? ka : min(a.prefix_len, ka + a.prefix_keys);
-    attn_range<ELT, DP, RT, kAttnWaves>(a, h, block * RT * 16, a.batch * a.tokens * a.group, -1, a.table + row * a.table_stride, ka, kb, split, lds);
+    id -= a.prefix_grid;
+    if (RT > 1 || id >= a.masked_grid) {
+        attn_own<ELT, DP, kAttnWaves>(a, id - a.masked_grid, lds);
+        return;
+    }
+    if constexpr (RT == 1) {
+        const int u = xcd_unit(id, a.n_prefix);
+        if (u < 0) return;
+        const SharedUnit s(a, u);
+        const int r0 = s.block * a.block_rows;
+        bool all = s.ka < s.kb;
+        for (int r = r0 + threadIdx.x; r < min(n_rows, r0 + a.block_rows); r += kAttnWaves * 64) {
+            const AttnRow x = attn_row(a, s.h, r, -1);
+            bool bad = false;
+            if (seq_len(a, seq_row(a, x.b, &bad), &bad) - (a.tokens - 1 - x.t) < s.kb) all = false;
+        }
+        if (__syncthreads_and(all)) return;
+        for (int r = r0; r < min(n_rows, r0 + a.block_rows); r += 16) {
+            attn_range<ELT, DP, 1, kAttnWaves>(a, s.h, r, n_rows, -1, a.table + s.row * a.table_stride, s.ka, s.kb, s.split, lds);
+            __syncthreads();
+        }
+    }
 }
 
 // Many: its wavefronts share its rows out.
 template <int ELT, int DP, int NW, bool FULL>
 __global__ __launch_bounds__(NW * 64, DP <= 128 ? 2 : 1) void attn_block_kernel(const AttnDev a) {
-    constexpr int kRangeBytes = attn_lds_bytes<DP, 1, NW>();
-    __shared__ __align__(16) char lds[BlockLds<DP>::kBytes > kRangeBytes ? BlockLds<DP>::kBytes : kRangeBytes];
+    __shared__ __align__(1024) char lds[BlockLds<DP, NW>::kBytes];
     const int u = xcd_unit(blockIdx.x, a.n_prefix);
     if (u < 0) return;
-    bool bad = false;
-    const int block = u % a.prefix_blocks, h = u / a.prefix_blocks % a.kv_heads, split = u / (a.prefix_blocks * a.kv_heads);
-    const int row = seq_row(a, 0, &bad), n_rows = a.batch * a.tokens * a.group, r0 = block * NW * 32;
-    const int ka = split * a.prefix_keys, kb = row < 0 ? ka : min(a.prefix_len, ka + a.prefix_keys);
-    const int32_t *table = a.table + row * a.table_stride;
-    // a row that sees only a part of these keys (a sequence that ends before them): tile by tile, with masks
-    bool all = true;
-    for (int r = r0 + threadIdx.x; r < min(n_rows, r0 + NW * 32); r += NW * 64) {
-        const AttnRow w = attn_row(a, h, r, -1);
-        if (seq_len(a, seq_row(a, w.b, &bad), &bad) - (a.tokens - 1 - w.t) < kb) all = false;
-    }
-    if (ka < kb && __syncthreads_and(all)) {
-        attn_block<ELT, DP, NW, FULL>(a, h, r0, n_rows, table, ka, kb, split, lds);
-    } else {
-        for (int t = 0; t < NW * 2; ++t) {
-            __syncthreads();
-            attn_range<ELT, DP, 1, NW>(a, h, r0 + t * 16, n_rows, -1, table, ka, kb, split, lds);
-        }
-    }
+    const SharedUnit s(a, u);
+    if (s.ka < s.kb) attn_block<ELT, DP, NW, FULL>(a, s.h, s.block * NW * 32, a.batch * a.tokens * a.group, a.table + s.row * a.table_stride, s.ka, s.kb, s.split, lds);
 }
 
 // rt: 16-row tiles of a workgroup of attn_range_kernel; 0: attn_block_kernel on the shared keys, waves of 32 rows, and own keys in a launch of their own: they are bound by
-// memory, and one workgroup of attn_block_kernel takes all registers of a CU (in one launch 64 samples' 130 MB took 53 us, apart 24 + 22)
+// memory, and one workgroup of attn_block_kernel takes all registers of a CU (in one launch 64 samples' 130 MB took 53 us, apart 25 + 24)
 hipError_t launch_attn_bf16(const AttnDev &a, int dp, int rt, int waves, hipStream_t stream);
 hipError_t launch_attn_f16(const AttnDev &a, int dp, int rt, int waves, hipStream_t stream);
 hipError_t launch_attn_f32(const AttnDev &a, int dp, int rt, int waves, hipStream_t stream);
@@ -877,11 +899,11 @@ hipError_t launch_attn_dp(AttnDev a, int rt, int waves, hipStream_t stream) {
                 hipLaunchKernelGGL((attn_block_kernel<ELT, DP, 4, false>), g, dim3(256), 0, stream, a);
             }
             const hipError_t e = hipGetLastError();
-            if (e != hipSuccess || a.n_own == 0) return e;
-            a.prefix_grid = 0;
+            if (e != hipSuccess) return e;
+            a.masked_grid = a.prefix_grid, a.prefix_grid = 0;
         }
     }
-    const dim3 g((uint32_t)(a.prefix_grid + (a.n_own + 7) / 8 * 8)), threads(kAttnWaves * 64);
+    const dim3 g((uint32_t)(a.prefix_grid + a.masked_grid + (a.n_own + 7) / 8 * 8)), threads(kAttnWaves * 64);
     if constexpr (attn_max_rt(ELT, DP) >= 2) {
         if (rt == 2) {
             hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 2>), g, threads, 0, stream, a);
