@@ -1,7 +1,7 @@
 """What a decoder needs beside the selection: attention of a batch that shares a long prefix, verification of drafted
 tokens, and the pages of the cache between them.
 
-Argument marshalling only, as in binding.py: the work is done by the HIP library (include/atk_decode.h), on torch's
+Argument marshalling only, as in binding.py (calls on plain tensors by the extension module of csrc/atk_decode_torch.cpp): the work is done by the HIP library (include/atk_decode.h), on torch's
 current stream of the tensors' device, without synchronising; every call may be captured into a graph.  Shapes, types
 and strides are checked here and raise; what lies on the device - page numbers, sequence numbers, lengths - is checked by
 the kernels, which never follow a bad one and or a bit into the `status` tensor of the call (ATK_STATUS_*).
@@ -9,6 +9,7 @@ the kernels, which never follow a bad one and or a bit into the `status` tensor 
 from __future__ import annotations
 
 import ctypes
+import os
 
 from . import binding
 from .binding import ATK_BF16, ATK_F32
@@ -19,8 +20,10 @@ ATK_STATUS_BAD_SEQ = 2
 ATK_STATUS_BAD_PAGE = 4
 ATK_STATUS_BAD_LEN = 8
 
+_TORCH_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "lib", "_atk_decode.so")
 _vp, _i64, _ci = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int
 _lib = None
+_plain = None  # the extension module, from the first call on; False where it cannot be used
 
 
 class _AttentionArgs(ctypes.Structure):
@@ -54,6 +57,45 @@ def _library():
             f.restype, f.argtypes = res, types
         _lib = lib
     return _lib
+
+
+def _load_plain():
+    """Load (once) the extension module that marshals calls on plain tensors, as binding.py does its own.  It only saves time."""
+    global _plain
+    import importlib.machinery
+    import importlib.util
+
+    import torch
+
+    lib = _library()
+    try:
+        loader = importlib.machinery.ExtensionFileLoader("_atk_decode", _TORCH_PATH)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_atk_decode", loader))
+        loader.exec_module(module)
+        if module.torch_version != torch.__version__.split("+")[0]:
+            raise ImportError("built for torch %s, this is %s" % (module.torch_version, torch.__version__))
+        module.use(*(ctypes.cast(getattr(lib, "atk_" + n), _vp).value for n in ("attention_workspace_bytes", "shared_prefix_attention", "verify_workspace_bytes", "verify_drafts",
+                                                                                "copy_pages", "fork_sequences", "append_tokens", "free_sequences", "compact_pages")))
+    except ImportError as e:
+        import warnings
+
+        _plain = False
+        warnings.warn("%s cannot be used (%s): calls take some microseconds more on the host.  `python -c 'import __graft_entry__ as g; g.build()'` at the "
+                      "repository root builds it." % (_TORCH_PATH, e), RuntimeWarning, stacklevel=4)
+        return False
+    _plain = module
+    return module
+
+
+def _fast(name, *args):
+    """What the extension module makes of a call: its result, or None for what it leaves to the code here."""
+    module = _load_plain() if _plain is None else _plain
+    if not module:
+        return None
+    got = getattr(module, name)(*args)
+    if type(got) is int:
+        binding._check(got)
+    return got
 
 
 def _dtype(t, what):
@@ -105,6 +147,10 @@ def shared_prefix_attention(q, k_pages, v_pages, page_table, lens, prefix_len, s
 
     Returns out (B, T, heads, dim), with return_lse also the log of the sum of exp of the scaled scores (B, T, heads) f32.
     A token that sees no key gets 0 and -inf."""
+    if out is None:
+        got = _fast("attention", q, k_pages, v_pages, page_table, lens, prefix_len, seqs, scale, return_lse, status)
+        if got is not None:
+            return got
     import torch
 
     if q.dim() != 4 or k_pages.dim() != 4 or v_pages.dim() != 4:
@@ -165,6 +211,9 @@ def verify_drafts(target_probs, draft_tokens, draft_probs, accept_random, final_
     max(p - q, 0), or from p where every draft was accepted: the first index whose running sum exceeds final_random times the total.
 
     Returns accepted (B) int32 and tokens (B, L + 1) int32: the accepted ones, the drawn one, then -1."""
+    got = _fast("verify", target_probs, draft_tokens, draft_probs, accept_random, final_random, n_drafts)
+    if got is not None:
+        return got
     import torch
 
     if target_probs.dim() != 3 or draft_tokens.dim() != 2:
@@ -241,6 +290,7 @@ class PageTables:
         self._work = torch.zeros((size,), dtype=torch.uint8, device=device)
         self._args = _Tables(page_table.data_ptr(), lens.data_ptr(), refs.data_ptr(), free_pages.data_ptr(), n_free.data_ptr(), status.data_ptr(), self._work.data_ptr(),
                              rows, row_pages, pages, page_size, size)
+        self._address, self._device = ctypes.addressof(self._args), device.index
 
     @classmethod
     def empty(cls, pages, page_size, rows, row_pages, device="cuda"):
@@ -273,6 +323,8 @@ def copy_pages(src_pools, src_ids, dst_pools, dst_ids, status=None):
 
     The pools are lists of contiguous tensors (pages, page_size, ...), src_ids and dst_ids int32 tensors; destinations are distinct and
     no page is both a source and a destination.  A page number out of range is passed over and reported in `status`."""
+    if _fast("copy", src_pools, src_ids, dst_pools, dst_ids, status) is not None:
+        return
     if len(src_pools) != len(dst_pools):
         raise ValueError("src_pools and dst_pools must be equally many")
     if src_ids.dim() != 1:
@@ -312,6 +364,8 @@ def fork_sequences(tables, pools, parents, children):
     """Makes row children[i] of the tables, empty until now, a copy of row parents[i]: whole pages are shared, a last page that is
     filled in part is copied, in all pools.  parents and children: int32 (n,), children distinct.  All or nothing: with too few
     free pages, or a child that holds something, nothing changes and tables.status says so."""
+    if _fast("fork", tables._address, tables._device, pools, parents, children) is not None:
+        return
     n = _seqs(tables, parents, None, "parents")
     _seqs(tables, children, n, "children")
     a = tables._args
@@ -325,6 +379,8 @@ def append_tokens(tables, pools, seqs, values):
 
     Takes fresh pages as they are needed, and a copy of a last page that is filled in part while other rows hold it too.  All or
     nothing: with too few free pages, or a row that is too short, nothing changes and tables.status says so."""
+    if _fast("append", tables._address, tables._device, pools, seqs, values) is not None:
+        return
     n = _seqs(tables, seqs, None, "seqs")
     a = tables._args
     ptrs, token_bytes = _pools(pools, tables.device, a.n_pages, a.page_size)
@@ -347,6 +403,8 @@ def append_tokens(tables, pools, seqs, values):
 def free_sequences(tables, seqs, drop=None):
     """Drops the last drop[i] tokens of row seqs[i] (all of them without `drop`) and gives back the pages that hold none of the rest,
     the lowest on top of the stack.  seqs, drop: int32 (n,), seqs distinct."""
+    if _fast("free", tables._address, tables._device, seqs, drop) is not None:
+        return
     n = _seqs(tables, seqs, None, "seqs")
     if drop is not None:
         _seqs(tables, drop, n, "drop")
@@ -357,6 +415,9 @@ def free_sequences(tables, seqs, drop=None):
 def compact_pages(tables, pools):
     """Moves the held pages to the lowest numbers, in all pools, tables and the stack.  Returns remap (pages,) int32: the new number of
     each page, -1 for those that were free - for page lists that a program keeps beside the tables."""
+    got = _fast("compact", tables._address, tables._device, pools)
+    if got is not None:
+        return got
     import torch
 
     a = tables._args
