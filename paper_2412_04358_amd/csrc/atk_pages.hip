@@ -51,12 +51,13 @@ constexpr int kWorkHead = 64;    // bytes in front of the bits
 template <int UNIT>
 struct Unit;
 template <>
-struct Unit<16> { typedef uint4 T; };
+struct Unit<16> { typedef uint32_t T __attribute__((ext_vector_type(4))); };
 template <>
 struct Unit<4> { typedef uint32_t T; };
 template <>
 struct Unit<1> { typedef uint8_t T; };
-template <int UNIT>
+// AROUND: around the caches, for whole pages, more of them than the caches hold (500 pages of 295 MB in all: 68 us -> 59; not for what the next call reads again: fork would be slower).
+template <int UNIT, bool AROUND = false>
 __device__ __forceinline__ void copy_bytes(char *dst, const char *src, int64_t bytes) {
     typedef typename Unit<UNIT>::T T;
     const int64_t n = bytes / UNIT;
@@ -64,9 +65,14 @@ __device__ __forceinline__ void copy_bytes(char *dst, const char *src, int64_t b
     for (; i + 3 * kThreads < n; i += 4 * kThreads) {
         T t[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) t[j] = ((const T *)src)[i + j * kThreads];
+        for (int j = 0; j < 4; ++j) t[j] = AROUND ? __builtin_nontemporal_load((const T *)src + i + j * kThreads) : ((const T *)src)[i + j * kThreads];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) ((T *)dst)[i + j * kThreads] = t[j];
+        for (int j = 0; j < 4; ++j) {
+            if (AROUND)
+                __builtin_nontemporal_store(t[j], (T *)dst + i + j * kThreads);
+            else
+                ((T *)dst)[i + j * kThreads] = t[j];
+        }
     }
     for (; i < n; i += kThreads) ((T *)dst)[i] = ((const T *)src)[i];
 }
@@ -94,17 +100,17 @@ __device__ __forceinline__ void copy_pools(int n, int units, DST dst, SRC src, W
     }
 }
 
-// One pool: unit u goes to the byte where(u) of dst.
+// One pool: unit u goes to the byte where(u) of dst.  Around the caches (512 samples' five tokens in 24 pools, fork and append: 185 us -> 179).
 template <int UNIT, typename WHERE>
 __device__ __forceinline__ void copy_pool(char *dst, const char *src, int units, WHERE where) {
     typedef typename Unit<UNIT>::T T;
     for (int u0 = threadIdx.x; u0 < units; u0 += 4 * kThreads) {
         T t[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) t[j] = ((const T *)src)[min(u0 + j * kThreads, units - 1)];
+        for (int j = 0; j < 4; ++j) t[j] = __builtin_nontemporal_load((const T *)src + min(u0 + j * kThreads, units - 1));
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (u0 + j * kThreads < units) *(T *)(dst + where(u0 + j * kThreads)) = t[j];
+            if (u0 + j * kThreads < units) __builtin_nontemporal_store(t[j], (T *)(dst + where(u0 + j * kThreads)));
     }
 }
 
@@ -144,13 +150,15 @@ __device__ __forceinline__ int scan_threads(int v, int *before) {
     return all;
 }
 
-// The workgroup's status bits together.
-__device__ __forceinline__ int or_threads(int bits) {
-    int all = 0;
+// Sums of a and b and all bits of c over the workgroup.
+__device__ __forceinline__ void meet_threads(int *a, int *b, int *c) {
+    __shared__ int waves[3][kThreads / 64];
+    for (int w = 1; w < 64; w <<= 1) *a += __shfl_xor(*a, w, 64), *b += __shfl_xor(*b, w, 64), *c |= __shfl_xor(*c, w, 64);
+    if ((threadIdx.x & 63) == 0) waves[0][threadIdx.x >> 6] = *a, waves[1][threadIdx.x >> 6] = *b, waves[2][threadIdx.x >> 6] = *c;
+    __syncthreads();
+    *a = *b = *c = 0;
 #pragma unroll
-    for (int b = 1; b <= ATK_STATUS_BAD_LEN; b <<= 1)
-        if (__syncthreads_or(bits & b)) all |= b;
-    return all;
+    for (int w = 0; w < kThreads / 64; ++w) *a += waves[0][w], *b += waves[1][w], *c |= waves[2][w];
 }
 
 // Pushes the pages whose bits are set, the lowest last, and clears the bits.  By one workgroup.
@@ -191,23 +199,32 @@ __device__ __forceinline__ void give_back(const PagesDev &t, int page) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------- copy
+// f(page i, pool, piece of the page) for this workgroup's share of all of them.  (Their number mostly fits 32 bits, whose quotients take a tenth of 64 bits'.)
+template <typename F>
+__device__ __forceinline__ void for_units(int64_t n, int n_pools, int pieces, F f) {
+    const int64_t units = n * n_pools * pieces;
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        if (units <= 0xffffffffu) {
+            const uint32_t y = (uint32_t)u / (uint32_t)pieces, i = y / (uint32_t)n_pools;
+            f(i, (int)(y - i * n_pools), (int)((uint32_t)u - y * pieces));
+        } else {
+            const int64_t y = u / pieces, i = y / n_pools;
+            f(i, (int)(y - i * n_pools), (int)(u - y * pieces));
+        }
+    }
+}
 template <int UNIT>
 __global__ __launch_bounds__(kThreads) void pages_copy_kernel(const PoolPairs pools, int n_pools, int64_t page_bytes, int64_t piece, int pieces, int src_pages,
                                                               int dst_pages, const int32_t *src_ids, const int32_t *dst_ids, int64_t n, int32_t *status) {
-    const int64_t units = n * n_pools * pieces;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int x = (int)(u % pieces);
-        const int64_t y = u / pieces;
-        const int pool = (int)(y % n_pools);
-        const int64_t i = y / n_pools;
+    for_units(n, n_pools, pieces, [&](int64_t i, int pool, int x) {
         const int src = src_ids[i], dst = dst_ids[i];
         if ((unsigned)src >= (unsigned)src_pages || (unsigned)dst >= (unsigned)dst_pages) {
             if (threadIdx.x == 0 && status) atomicOr(status, ATK_STATUS_BAD_PAGE);
-            continue;
+            return;
         }
         const int64_t at = x * piece;
-        copy_bytes<UNIT>(pools.dst[pool] + dst * page_bytes + at, pools.src[pool] + src * page_bytes + at, min(piece, page_bytes - at));
-    }
+        copy_bytes<UNIT, true>(pools.dst[pool] + dst * page_bytes + at, pools.src[pool] + src * page_bytes + at, min(piece, page_bytes - at));
+    });
 }
 
 // ---------------------------------------------------------------------------------------------------------------- fork
@@ -230,13 +247,10 @@ __device__ __forceinline__ ForkNeed fork_need(const PagesDev &t, const int32_t *
         else if (t.page.mod(len)) ++total, before += i < mine;
         if (t.lens[c] != 0) bad |= ATK_STATUS_BAD_SEQ;
     }
-    ForkNeed r;
-    int x;
-    r.total = scan_threads(total, &x);
-    r.before = scan_threads(before, &x);
-    r.bad = or_threads(bad);
-    if (r.total > *t.n_free) r.bad |= ATK_STATUS_NO_PAGES;
-    return r;
+    const int n_free = *t.n_free;
+    meet_threads(&total, &before, &bad);
+    if (total > n_free) bad |= ATK_STATUS_NO_PAGES;
+    return ForkNeed{total, before, bad};
 }
 
 template <int UNIT>
@@ -324,17 +338,15 @@ __global__ __launch_bounds__(kThreads) void pages_append_kernel(const PagesDev t
                                                                 const int32_t *seqs, int64_t n, int64_t tokens, int shares, bool tables) {
     const int64_t i = blockIdx.x / shares;
     const int share = (int)(blockIdx.x % shares);
-    int total = 0, before = 0, bad = 0, x;
+    int total = 0, before = 0, bad = 0;
+    const int n_free = *t.n_free;
     for (int64_t j = threadIdx.x; j < n; j += kThreads) {
         const AppendSeq s = append_seq(t, seqs, j, tokens);
         bad |= s.bad;
         total += s.takes();
         if (j < i) before += s.takes();
     }
-    total = scan_threads(total, &x);
-    before = scan_threads(before, &x);
-    bad = or_threads(bad);
-    const int n_free = *t.n_free;
+    meet_threads(&total, &before, &bad);
     if (total > n_free) bad |= ATK_STATUS_NO_PAGES;
     const int64_t page_bytes = (int64_t)t.page.d * token_bytes;
     if (!bad) {
@@ -520,14 +532,10 @@ template <int UNIT>
 __global__ __launch_bounds__(kThreads) void pages_move_kernel(const PagesDev t, const Pools pools, int n_pools, int64_t page_bytes, int64_t piece, int pieces,
                                                               const int32_t *remap, const int32_t *moves, const int32_t *n_moves, bool tables) {
     const int n = *n_moves;
-    const int64_t units = (int64_t)n * n_pools * pieces;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int x = (int)(u % pieces);
-        const int64_t y = u / pieces;
-        const int pool = (int)(y % n_pools), i = (int)(y / n_pools);
+    for_units(n, n_pools, pieces, [&](int64_t i, int pool, int x) {
         const int64_t at = x * piece;
-        copy_bytes<UNIT>(pools.p[pool] + moves[t.n_pages + i] * page_bytes + at, pools.p[pool] + moves[i] * page_bytes + at, min(piece, page_bytes - at));
-    }
+        copy_bytes<UNIT, true>(pools.p[pool] + moves[t.n_pages + i] * page_bytes + at, pools.p[pool] + moves[i] * page_bytes + at, min(piece, page_bytes - at));
+    });
     if (!tables) return;
     const int64_t threads = (int64_t)gridDim.x * kThreads, me = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     for (int64_t i = me; i < n; i += threads) {
