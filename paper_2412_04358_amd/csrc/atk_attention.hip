@@ -124,7 +124,8 @@ static void plan_blocks(const atk_attention_args *p, int64_t rows, AttnPlan *pl)
     pl->waves = 4;
     for (int waves = 4; waves <= attn_max_waves(pl->dp); waves *= 2) {
         const int64_t blocks = attn_ceil(rows, 32 * waves), base = blocks * p->kv_heads;
-        for (int64_t splits = 1; splits <= std::min<int64_t>(steps, 512); ++splits) {
+        for (int64_t wanted = kNumCU / 8; wanted <= 4 * kNumCU; wanted += std::min<int64_t>(wanted, kNumCU)) {  // workgroups: an eighth of the CUs to four on each
+            const int64_t splits = std::min(steps, std::max<int64_t>(1, wanted / base));
             const int64_t tiles = attn_ceil(steps, splits), groups = base * attn_ceil(steps, tiles);
             const bool full = waves == 8 || (groups > kNumCU && pl->dp <= 128);
             const double rounds = (double)attn_ceil(groups, waves == 4 && full ? 2 * kNumCU : kNumCU);

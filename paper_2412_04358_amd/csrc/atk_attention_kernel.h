@@ -21,8 +21,11 @@
 namespace atk {
 
 constexpr float kNoMax = -__builtin_inff();
-constexpr int kAttnWaves = 4;      // of a workgroup of attn_range_kernel: they take turns at the 32-key tiles of its range and join through LDS
-constexpr int kTileKeys = 32;
+constexpr int kAttnWaves = 4;      // of a workgroup of attn_range_kernel: they take turns at the tiles of its range and join through LDS
+constexpr int kTileKeys = 32;      // keys of a wavefront that ranges are cut by
+// Halves of 16 keys that a wavefront takes at a time: two, whose keys are the 32 of a 16-bit product; one in f32, whose products take a key of each lane group, where K and V of 32 keys would
+// leave a SIMD one wavefront (12 sequences of 16 heads on 2047 + 191 keys of 128: 29 us with two halves).
+constexpr int attn_halves(int elt) { return elt == ATK_F32 ? 1 : 2; }
 constexpr float kLazyMax = 8.0f;   // the maximum that weights are taken relative to follows the true one when that is 2^8 above it: 2^8 times the largest weight is
                                    // far from f32's and bf16's range, and rescaling is rare
 
@@ -107,13 +110,14 @@ __device__ __forceinline__ bool not_finite(uint32_t w) {
     return (w & lo) == lo || (w & hi) == hi;
 }
 
-// Eight rows of V as a lane has them: DVL elements each.
+// The rows of V that a lane has, four of each half: kDvl elements each.
 template <int ELT, int DP>
 struct VRows {
     static constexpr int kDvl = DP / 16;                                    // elements of a lane's piece of a row
     static constexpr int kWords = kDvl * AttnElt<ELT>::kBytes / 4;          // 32-bit words of it
     static constexpr int kVec = kWords % 4 == 0 ? 4 : 2;                    // words of a load
-    uint32_t w[8][kWords];
+    static constexpr int kRows = 4 * attn_halves(ELT);
+    uint32_t w[kRows][kWords];
 
     __device__ __forceinline__ void load(int j, const char *row, int n, int dim) {
 #pragma unroll
@@ -145,22 +149,24 @@ struct VRows {
     __device__ __forceinline__ bool any_not_finite() const {
         bool bad = false;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < kRows; ++j)
 #pragma unroll
             for (int x = 0; x < kWords; ++x) bad |= not_finite<ELT>(w[j][x]);
         return bad;
     }
 };
 
-// A lane's eight weights as an operand.
+// A lane's weights as operands, four of each half.
 template <int ELT>
 struct Weights {
-    u32x4 w[ELT == ATK_F32 ? 2 : 1];
-    __device__ __forceinline__ void set(const f32x4 &a, const f32x4 &b) {
+    u32x4 w;
+    __device__ __forceinline__ void set(const f32x4 *s) {
+        const f32x4 a = s[0];
         if constexpr (ELT == ATK_F32) {
-            w[0] = __builtin_bit_cast(u32x4, a), w[1] = __builtin_bit_cast(u32x4, b);
+            w = __builtin_bit_cast(u32x4, a);
         } else {
-            w[0] = u32x4{AttnElt<ELT>::pack(a[0], a[1]), AttnElt<ELT>::pack(a[2], a[3]), AttnElt<ELT>::pack(b[0], b[1]), AttnElt<ELT>::pack(b[2], b[3])};
+            const f32x4 b = s[1];
+            w = u32x4{AttnElt<ELT>::pack(a[0], a[1]), AttnElt<ELT>::pack(a[2], a[3]), AttnElt<ELT>::pack(b[0], b[1]), AttnElt<ELT>::pack(b[2], b[3])};
         }
     }
 };
@@ -169,11 +175,11 @@ template <int ELT, int DP>
 __device__ __forceinline__ f32x4 mma_pv(const VRows<ELT, DP> &v, int i, const Weights<ELT> &p, f32x4 c) {
     if constexpr (ELT == ATK_F32) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v.w[j][i]), __uint_as_float(p.w[j / 4][j % 4]), c, 0, 0, 0);
+        for (int j = 0; j < 4; ++j)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v.w[j][i]), __uint_as_float(p.w[j]), c, 0, 0, 0);
         return c;
     } else {
-        return AttnElt<ELT>::mma(v.operand(i), p.w[0], c);
+        return AttnElt<ELT>::mma(v.operand(i), p.w, c);
     }
 }
 
@@ -214,6 +220,8 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
     constexpr int kPiece = 16 / E::kBytes;            // elements of 16 bytes
     constexpr int NC = DP / (4 * kPiece);             // 16-byte pieces of a row that a lane has
     constexpr int NT = DP / 16;                       // products along d
+    constexpr int NX = attn_halves(ELT), TK = 16 * NX;
+    constexpr uint32_t kAll = (uint32_t)((1ull << TK) - 1);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int n = lane & 15, g = lane >> 4;
 
@@ -250,20 +258,20 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
     }
     const char *kh = (const char *)a.k + h * a.ks[2] * E::kBytes, *vh = (const char *)a.v + h * a.vs[2] * E::kBytes;
 
-    // lane j (and j + 32) looks key k0 + j up, a tile ahead; keys past the end are read as the last one and masked
-    auto page_of = [&](int k0) { return table_row[a.page.div(min(k0 + (lane & 31), kb - 1))]; };
-    int page_next = ka < kb ? page_of(ka + wave * kTileKeys) : 0;
-    for (int k0 = ka + wave * kTileKeys; k0 < kb; k0 += NW * kTileKeys) {
+    // lane j (and those TK apart) looks key k0 + j up, a tile ahead; keys past the end are read as the last one and masked
+    auto page_of = [&](int k0) { return table_row[a.page.div(min(k0 + (lane & (TK - 1)), kb - 1))]; };
+    int page_next = ka < kb ? page_of(ka + wave * TK) : 0;
+    for (int k0 = ka + wave * TK; k0 < kb; k0 += NW * TK) {
         int page = page_next;
-        page_next = page_of(min(k0 + NW * kTileKeys, kb - 1));
+        page_next = page_of(min(k0 + NW * TK, kb - 1));
         const bool good = (unsigned)page < (unsigned)a.n_pages;
         bad_page |= !good;
         if (!good) page = 0;
-        const uint32_t valid = (uint32_t)__ballot(good);
+        const uint32_t valid = (uint32_t)__ballot(good) & kAll;
 
-        u32x4 kf[2][NC];
+        u32x4 kf[NX][NC];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < NX; ++x) {
             const int key = min(k0 + x * 16 + n, kb - 1);
             const char *row = kh + (__shfl(page, x * 16 + n, 64) * a.ks[0] + a.page.mod(key) * a.ks[1]) * E::kBytes;
 #pragma unroll
@@ -274,29 +282,29 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
         }
         VRows<ELT, DP> v;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < 4 * NX; ++j) {
             const int at = (j / 4) * 16 + g * 4 + j % 4;
             const int key = min(k0 + at, kb - 1);
             const char *row = vh + (__shfl(page, at, 64) * a.vs[0] + a.page.mod(key) * a.vs[1]) * E::kBytes;
             v.load(j, row, n, a.dim);
         }
-        f32x4 s[RT][2];
+        f32x4 s[RT][NX];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
+            for (int x = 0; x < NX; ++x) {
                 s[rt][x] = f32x4{0, 0, 0, 0};
 #pragma unroll
                 for (int c = 0; c < NC; ++c) s[rt][x] = E::mma(kf[x][c], q[rt][c], s[rt][x]);
             }
-        const bool masked = k0 + kTileKeys > min_lim || valid != 0xffffffffu;
+        const bool masked = k0 + TK > min_lim || valid != kAll;
         bool apart = false;  // a value that is not finite beside a mask: 0 * it would not be 0
         if (masked) {
             asm volatile("");  // (a branch, no selections)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
+                for (int x = 0; x < NX; ++x)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int at = x * 16 + g * 4 + j;
@@ -308,7 +316,11 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
         bool raise = false;
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            float t = fmaxf(fmaxf(fmaxf(s[rt][0][0], s[rt][0][1]), fmaxf(s[rt][0][2], s[rt][0][3])), fmaxf(fmaxf(s[rt][1][0], s[rt][1][1]), fmaxf(s[rt][1][2], s[rt][1][3])));
+            float t = s[rt][0][0];
+#pragma unroll
+            for (int x = 0; x < NX; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) t = fmaxf(t, s[rt][x][j]);
             t = fmaxf(t, __shfl_xor(t, 16, 64));
             t = fmaxf(t, __shfl_xor(t, 32, 64));
             top[rt] = t;
@@ -336,7 +348,7 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
             const float ref = zero * a.scale2 - E::kBias;
             float sum = 0.0f;
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+            for (int x = 0; x < NX; ++x)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float e = __builtin_amdgcn_exp2f(far ? fmaf(s[rt][x][j] - zero, a.scale2, E::kBias) : fmaf(s[rt][x][j], a.scale2, -ref));
@@ -344,7 +356,7 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
                     sum += e;
                 }
             l[rt] += sum;
-            p[rt].set(s[rt][0], s[rt][1]);
+            p[rt].set(s[rt]);
         }
         if (!apart) {
 #pragma unroll
@@ -359,7 +371,7 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
                     const int limit = __shfl(lim[rt], c, 64);
                     VRows<ELT, DP> u = v;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
+                    for (int j = 0; j < 4 * NX; ++j) {
                         const int at = (j / 4) * 16 + g * 4 + j % 4;
                         if (k0 + at >= limit || !(valid >> at & 1))
 #pragma unroll
@@ -587,6 +599,15 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
     load_k(0, bases_of(k_ring, 0));
     load_k(1, bases_of(k_ring, 1));
     load_v(0, bases_of(v_ring, 0));
+    // What lies behind the last key has weight 0, which NaN in V would not heed: a wavefront clears it in what it has brought in, before the first products that read it.
+    auto clear_tail = [&]() {
+        const int left = kb - ka - (tiles - 1) * kBlockKeys;
+        if (left == kBlockKeys) return;
+#pragma unroll
+        for (int c = 0; c < kLoads; ++c)
+            if (first_key(c) + in_load >= left)
+                *(__attribute__((address_space(3))) u32x4 *)(uintptr_t)(v_lds + buffer(tiles - 1) + (c * NW + wave) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+    };
     if (late) {
         load_k(2, bases_of(k_ring, 2));
         load_v(1, bases_of(v_ring, 1));
@@ -601,6 +622,7 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
         }
     }
     wait_loads<0>();
+    if (tiles == 1) clear_tail();
     __syncthreads();
 
     float m = kNoMax, l = 0.0f;
@@ -734,19 +756,6 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
         }
         l += sum;
     };
-    // One meeting a tile: the first half of the wavefronts comes from its vector phase, the second from its products.  It says that what the next products read has come in, and
-    // that the tile whose buffers the next loads fill has been read.  (Four wavefronts, in step and with a buffer less, meet behind their products too.)
-    auto end = [&]() {  // of what the last tile needs; what lies behind the last key has weight 0, which NaN would not heed
-        wait_loads<0>();
-        const int left = kb - ka - (tiles - 1) * kBlockKeys;
-        if (left < kBlockKeys) {
-#pragma unroll
-            for (int c = 0; c < kLoads; ++c)
-                if (first_key(c) + in_load >= left)
-                    *(__attribute__((address_space(3))) u32x4 *)(uintptr_t)(v_lds + buffer(tiles - 1) + (c * NW + wave) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-        }
-        barrier();
-    };
     if (late) barrier();
     products(No{}, Yes{}, -1);
     barrier();
@@ -757,12 +766,15 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
         load_v(t + 1 + late, next_v);
         softmax(t);
         wait_loads<2 * kLoads>();
+        if (late && t == tiles - 2) clear_tail();  // (the first half of the wavefronts comes to the last tile's V a phase sooner)
         barrier();
         products(Yes{}, Yes{}, t);
         barrier();
     }
     softmax(tiles - 1);
-    end();
+    wait_loads<0>();
+    if (!late && tiles > 1) clear_tail();
+    barrier();
     products(Yes{}, No{}, tiles - 1);
     if (!late && NW == 8) barrier();
     if (bad_page && a.status) atomicOr(a.status, ATK_STATUS_BAD_PAGE);

@@ -1,8 +1,8 @@
 // verify_drafts: accepted drafts, and one token drawn from what is left of the target's probabilities (include/atk_decode.h).
 //
 // Only one row of the target's probabilities is needed whole, and after a rejection one of the draft's: those of the first rejected
-// token.  verify_sums_kernel finds it (a few gathers, done again by every workgroup of the request), and sums the weights of a part of that row;
-// verify_draw_kernel finds the part, then the thread's eight elements, then the element at which the running sum passes the goal.  Sums are f64: an index is what comes out, and the
+// token.  verify_sums_kernel finds it (a few gathers, done again by every workgroup of the request), and sums the weights of tiles of that row;
+// verify_draw_kernel finds the tile, then a lane's eight elements, then the element at which the running sum passes the goal.  Sums are f64: an index is what comes out, and the
 // running sum of 10^5 f32 would be off by more than the weights.
 #include "atk_decode_common.h"
 
@@ -13,10 +13,10 @@ struct VerifyDev {
     const int32_t *draft_tokens, *n_drafts;
     const float *u, *r;
     int32_t *accepted, *tokens;
-    double2 *sums;  // [request][part]: residual weights, target's weights
+    double2 *sums;  // [request][tile]: residual weights, target's weights
     int64_t ts[2], ds[2];
-    int64_t vocab, part;
-    int drafts, parts;
+    int64_t vocab;
+    int drafts, tiles, groups;  // tiles of a row, workgroups that share them
 };
 
 template <int ELT>
@@ -128,29 +128,38 @@ __device__ __forceinline__ double wave_sum(double v) {
     return v;
 }
 
-__device__ __forceinline__ void sum256(double *a, double *b) {
-    __shared__ double2 waves[4];
-    *a = wave_sum(*a), *b = wave_sum(*b);
-    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = double2{*a, *b};
-    __syncthreads();
-    *a = (waves[0].x + waves[1].x) + (waves[2].x + waves[3].x), *b = (waves[0].y + waves[1].y) + (waves[2].y + waves[3].y);
-}
+// Tiles of a workgroup: enough that a request's accepted drafts, a chain of three dependent reads, are not looked for too often (64 requests of 128256: 11.7 us with one tile, 10.0 with two).
+constexpr int kMostTiles = 4;
 
 template <int ELT>
 __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyDev a) {
-    const int64_t b = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+    __shared__ double2 waves[kMostTiles][4];
+    const int64_t b = blockIdx.x / a.groups;
+    const int group = (int)(blockIdx.x % a.groups), each = (a.tiles + a.groups - 1) / a.groups, lane = threadIdx.x & 63;
     const VerifyRow<ELT> row(a, b);
-    const int64_t from = part * a.part, to = min(a.vocab, from + a.part);
-    double2 s = {0, 0};
-    for (int64_t v = from + threadIdx.x * kEach; v < to; v += kTile) {
-        double left[kEach], all[kEach];
-        weights8<ELT>(row, v, to, left, all);
+    double2 s[kMostTiles];
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) s.x += left[e], s.y += all[e];
+    for (int k = 0; k < kMostTiles; ++k) {
+        s[k] = double2{0, 0};
+        const int64_t v = ((int64_t)group * each + k) * kTile + threadIdx.x * kEach;
+        if (k < each && v < a.vocab) {
+            double left[kEach], all[kEach];
+            weights8<ELT>(row, v, a.vocab, left, all);
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) s[k].x += left[e], s[k].y += all[e];
+        }
     }
-    sum256(&s.x, &s.y);
-    if (threadIdx.x == 0 && part == 0) a.accepted[b] = row.accepted;
-    if (threadIdx.x == 0) a.sums[blockIdx.x] = s;
+#pragma unroll
+    for (int k = 0; k < kMostTiles; ++k) {
+        if (k >= each) break;
+        s[k].x = wave_sum(s[k].x), s[k].y = wave_sum(s[k].y);
+        if (lane == 0) waves[k][threadIdx.x >> 6] = s[k];
+    }
+    __syncthreads();
+    const int k = threadIdx.x, tile = group * each + k;
+    if (k < each && tile < a.tiles)
+        a.sums[b * a.tiles + tile] = double2{(waves[k][0].x + waves[k][1].x) + (waves[k][2].x + waves[k][3].x), (waves[k][0].y + waves[k][1].y) + (waves[k][2].y + waves[k][3].y)};
+    if (threadIdx.x == 0 && group == 0) a.accepted[b] = row.accepted;
 }
 
 // The first lane whose running sum of weights (from *run on) passes the goal, -1 if none, and *run is behind them all then; *before: a lane's running sum without its own;
@@ -174,20 +183,20 @@ template <int ELT>
 __global__ __launch_bounds__(64) void verify_draw_kernel(const VerifyDev a) {
     const int lane = threadIdx.x;
     const int64_t b = blockIdx.x;
-    const double2 *s = a.sums + b * a.parts;
+    const double2 *s = a.sums + b * a.tiles;
     const double r = (double)a.r[b];
-    const double2 mine = lane < a.parts ? s[lane] : double2{0, 0};
+    const double2 mine = lane < a.tiles ? s[lane] : double2{0, 0};
     const VerifyRow<ELT> row(a, b, a.accepted[b]);
     double left = mine.x, all = mine.y;
-    for (int i = lane + 64; i < a.parts; i += 64) left += s[i].x, all += s[i].y;
+    for (int i = lane + 64; i < a.tiles; i += 64) left += s[i].x, all += s[i].y;
     left = wave_sum(left), all = wave_sum(all);
     const bool of_target = !(left > 0);  // nothing left (or sums that are no numbers): p itself
     const double goal = r * (of_target ? all : left);
-    // the part, ...
+    // the tile, ...
     int pick = -1, token = -1;
     double run = 0, start = 0, before;
-    for (int i0 = 0; i0 < a.parts; i0 += 64) {
-        const double2 x = i0 == 0 ? mine : i0 + lane < a.parts ? s[i0 + lane] : double2{0, 0};
+    for (int i0 = 0; i0 < a.tiles; i0 += 64) {
+        const double2 x = i0 == 0 ? mine : i0 + lane < a.tiles ? s[i0 + lane] : double2{0, 0};
         int last = -1;
         const int got = find64(of_target ? x.y : x.x, goal, &run, &last, &before);
         const int who = got >= 0 ? got : last;
@@ -195,63 +204,58 @@ __global__ __launch_bounds__(64) void verify_draw_kernel(const VerifyDev a) {
         if (got >= 0) break;
     }
     if (pick >= 0) {
-        // ... the lane's eight elements of a quarter of a tile, and the one among them
-        const int64_t from = (int64_t)pick * a.part, to = min(a.vocab, from + a.part);
+        // ... the lane's eight elements of a quarter of it, and the one among them
+        const int64_t v0 = (int64_t)pick * kTile;
         constexpr int kQuarter = 64 * kEach;
+        double w[4][kEach], sum[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t v = v0 + k * kQuarter + lane * kEach;
+            double t[kEach];
+            weights8<ELT>(row, v, a.vocab, w[k], t);
+            sum[k] = 0;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+                if (of_target) w[k][e] = t[e];
+                sum[k] += w[k][e];
+            }
+        }
         run = start;
         bool found = false;
-        for (int64_t v0 = from; v0 < to && !found; v0 += kTile) {
-            double w[4][kEach], sum[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int64_t v = v0 + k * kQuarter + lane * kEach;
-                double t[kEach];
-                weights8<ELT>(row, v, to, w[k], t);
-                sum[k] = 0;
+        for (int k = 0; k < 4; ++k) {
+            if (found) continue;
+            int last = -1;
+            const int got = find64(sum[k], goal, &run, &last, &before);
+            const int who = got >= 0 ? got : last;
+            found = got >= 0;
+            if (who < 0) continue;
+            int at = -1;
+            bool done = false;
 #pragma unroll
-                for (int e = 0; e < kEach; ++e) {
-                    if (of_target) w[k][e] = t[e];
-                    sum[k] += w[k][e];
-                }
+            for (int e = 0; e < kEach; ++e) {
+                if (done || !(w[k][e] > 0)) continue;
+                at = e;
+                before += w[k][e];
+                done = before > goal;
             }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (found) continue;
-                int last = -1;
-                const int got = find64(sum[k], goal, &run, &last, &before);
-                const int who = got >= 0 ? got : last;
-                found = got >= 0;
-                if (who < 0) continue;
-                int at = -1;
-                bool done = false;
-#pragma unroll
-                for (int e = 0; e < kEach; ++e) {
-                    if (done || !(w[k][e] > 0)) continue;
-                    at = e;
-                    before += w[k][e];
-                    done = before > goal;
-                }
-                token = (int)(v0 + k * kQuarter) + who * kEach + __shfl(at, who, 64);
-            }
+            token = (int)(v0 + k * kQuarter) + who * kEach + __shfl(at, who, 64);
         }
     }
     for (int i = lane; i <= a.drafts; i += 64)
         a.tokens[b * (a.drafts + 1) + i] = i < row.accepted ? a.draft_tokens[b * a.drafts + i] : i == row.accepted ? token : -1;
 }
 
-// Elements of a part: a tile, or as many tiles as keep the parts of all requests at about eight workgroups a CU.
-static int64_t verify_part(int64_t batch, int64_t vocab) {
-    const int64_t tiles = (vocab + kTile - 1) / kTile, each = batch * tiles / (8 * kNumCU);
-    return kTile * std::max<int64_t>(1, std::min<int64_t>(4, each));
-}
-static int64_t verify_parts(int64_t batch, int64_t vocab) {
-    const int64_t part = verify_part(batch, vocab);
-    return (vocab + part - 1) / part;
+static int64_t verify_tiles(int64_t vocab) { return (vocab + kTile - 1) / kTile; }
+// Workgroups of a request: a tile each, or as many tiles as keep all requests at about eight workgroups a CU.
+static int64_t verify_groups(int64_t batch, int64_t vocab) {
+    const int64_t tiles = verify_tiles(vocab), each = (batch * tiles + 8 * kNumCU - 1) / (8 * kNumCU);
+    return (tiles + std::min<int64_t>(each, kMostTiles) - 1) / std::min<int64_t>(each, kMostTiles);
 }
 
 template <int ELT>
 static hipError_t launch_verify(const VerifyDev &a, int64_t batch, hipStream_t s) {
-    hipLaunchKernelGGL((verify_sums_kernel<ELT>), dim3((uint32_t)(batch * a.parts)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((verify_sums_kernel<ELT>), dim3((uint32_t)(batch * a.groups)), dim3(256), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((verify_draw_kernel<ELT>), dim3((uint32_t)batch), dim3(64), 0, s, a);
@@ -266,8 +270,8 @@ extern "C" {
 
 int64_t atk_verify_workspace_bytes(int64_t batch, int64_t drafts, int64_t vocab) {
     if (batch < 1 || batch > (1 << 24) || drafts < 0 || drafts > (1 << 20) || vocab < 1 || vocab >= (INT64_C(1) << 30)) return ATK_ERR_ARGS;
-    if (batch * verify_parts(batch, vocab) >= (INT64_C(1) << 31)) return ATK_ERR_ARGS;  // workgroups
-    return batch * verify_parts(batch, vocab) * (int64_t)sizeof(double2);
+    if (batch * verify_groups(batch, vocab) >= (INT64_C(1) << 31)) return ATK_ERR_ARGS;  // workgroups
+    return batch * verify_tiles(vocab) * (int64_t)sizeof(double2);
 }
 
 int atk_verify_drafts(const void *target_probs, const int64_t target_stride[2], const void *draft_probs, const int64_t draft_stride[2],
@@ -290,8 +294,7 @@ int atk_verify_drafts(const void *target_probs, const int64_t target_stride[2], 
         a.ts[i] = target_stride[i], a.ds[i] = draft_probs ? draft_stride[i] : 0;
         if (a.ts[i] < 0 || a.ds[i] < 0) return ATK_ERR_ARGS;
     }
-    a.vocab = vocab, a.drafts = (int)drafts, a.parts = (int)verify_parts(batch, vocab);
-    a.part = verify_part(batch, vocab);
+    a.vocab = vocab, a.drafts = (int)drafts, a.tiles = (int)verify_tiles(vocab), a.groups = (int)verify_groups(batch, vocab);
     const hipStream_t s = (hipStream_t)stream;
     const hipError_t e = dtype == ATK_F32 ? launch_verify<ATK_F32>(a, batch, s) : dtype == ATK_BF16 ? launch_verify<ATK_BF16>(a, batch, s) : launch_verify<ATK_F16>(a, batch, s);
     return e == hipSuccess ? ATK_OK : set_hip_error(e);

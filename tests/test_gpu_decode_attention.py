@@ -70,7 +70,9 @@ def check(q, k, v, table, lens, prefix, seqs=None, scale=None, got=None):
     assert (np.abs(got_out - want)[finite] <= tol[finite]).all(), np.nanmax((np.abs(got_out - want) / tol)[finite & (tol > 0)])
     live = np.isfinite(wlse)
     assert np.array_equal(got_lse[~live & ~np.isnan(wlse)], wlse[~live & ~np.isnan(wlse)])
-    assert (np.abs(got_lse - wlse)[live] <= (weight + 4 * E * (1 + np.abs(wlse)))[live]).all()
+    with np.errstate(invalid="ignore"):
+        off = np.abs(got_lse - wlse)
+    assert (off[live] <= (weight + 4 * E * (1 + np.abs(wlse)))[live]).all()
     return out, lse
 
 
@@ -107,6 +109,46 @@ def test_many_rows_on_the_prefix(dtype, B, T, H, Hk, D, prefix, ps):
     out, _ = check(*args[:4], lens, prefix)
     same = [b for b in range(B) if b not in (B // 2, B - 1)]
     assert (out[same].float() - clean[same].float()).abs().max() <= 4 * HALF[dtype] * clean.float().abs().max()
+
+
+@pytest.mark.parametrize("dtype", TYPES[:2], ids=str)
+@pytest.mark.parametrize("B,H,Hk,D,prefix", [(40, 4, 2, 64, 37), (40, 4, 2, 64, 101), (70, 8, 2, 64, 999), (70, 8, 2, 128, 1333), (40, 2, 1, 128, 205), (9, 32, 4, 200, 150), (300, 4, 4, 128, 66)])
+def test_nothing_behind_a_prefix_that_ends_inside_a_page(dtype, B, H, Hk, D, prefix):
+    # the first sequence ends with the prefix: behind it, in the same page, its slots hold NaN
+    args = make(B, 1, H, Hk, D, prefix, [prefix] + [prefix + 1 + i % 9 for i in range(1, B)], 16, dtype, seed=prefix)
+    check(*args, prefix)
+
+
+@pytest.mark.parametrize("dtype", TYPES[:2], ids=str)
+@pytest.mark.parametrize("B,Hk,D,prefix,ps", [(33, 32, 64, 60013, 16), (300, 8, 128, 30001, 32), (40, 64, 64, 45000, 64)])
+def test_long_prefixes_of_many_rows(dtype, B, Hk, D, prefix, ps):
+    # ranges of more tiles than addresses are kept for: against products in 64 bits on the GPU
+    g = torch.Generator(device="cuda").manual_seed(prefix)
+    shared, M = prefix // ps, prefix // ps + 2
+    P = shared + 2 * B
+    table = torch.empty((B, M), dtype=torch.int64, device="cuda")
+    ids = torch.randperm(P, generator=g, device="cuda")
+    table[:, :shared], table[:, shared:] = ids[:shared], ids[shared:].reshape(B, 2)
+    k, v = (torch.randn((P, ps, Hk, D), generator=g, device="cuda").to(dtype) for _ in range(2))
+    left = prefix - shared * ps
+    for x in (k, v):
+        x[table[1:, shared], :left] = x[table[0, shared], :left].clone()
+    q = torch.randn((B, 1, Hk, D), generator=g, device="cuda").to(dtype)
+    lens = torch.full((B,), prefix, dtype=torch.int32, device="cuda")
+    out, lse = atk.shared_prefix_attention(q, k, v, table.int(), lens, prefix, return_lse=True)
+    h = HALF[dtype]
+    for head in range(Hk):
+        kk, vv = (x[table[0], :, head].reshape(-1, D)[:prefix].double() for x in (k, v))
+        s = q[:, 0, head].double() @ kk.t() * D ** -0.5
+        w = torch.softmax(s, 1)
+        want, mass = w @ vv, w @ vv.abs()
+        weight = 2 * (D + 4) * E * D ** -0.5 * (q[:, 0, head].double().abs() @ kk.abs().t()).amax(1) + (4 + prefix) * E
+        tol = mass * (h + 2 * weight)[:, None] + h * want.abs()
+        if dtype == torch.float16:
+            tol = tol + 2 * prefix * vv.abs().max() * 2.0 ** -31 + 2.0 ** -24
+        assert ((out[:, 0, head].double() - want).abs() <= tol).all()
+        wlse = torch.logsumexp(s, 1)
+        assert ((lse[:, 0, head].double() - wlse).abs() <= weight + 4 * E * (1 + wlse.abs())).all()
 
 
 @pytest.mark.parametrize("dtype", TYPES[:2], ids=str)
