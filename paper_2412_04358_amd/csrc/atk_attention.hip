@@ -51,13 +51,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const AttnDev a) {
     const int64_t b = bt / a.tokens, t = bt % a.tokens;
     const float f = l == 0.0f ? 0.0f : 1.0f / l;
     if (lane < LPR && d < a.dim) {
-        char *out = (char *)a.out + (b * a.os[0] + t * a.os[1] + head * a.os[2] + d) * AttnElt<ELT>::kBytes;
-        if constexpr (ELT == ATK_F32)
-            *(f32x4 *)out = o * f;
-        else
-            *(u32x2 *)out = u32x2{AttnElt<ELT>::pack(o[0] * f, o[1] * f), AttnElt<ELT>::pack(o[2] * f, o[3] * f)};
+        store_out<ELT>((char *)a.out + (b * a.os[0] + t * a.os[1] + head * a.os[2] + d) * AttnElt<ELT>::kBytes, o * f);
     }
-    if (a.lse && lane == 0) a.lse[row] = l == 0.0f ? kNoMax : (m == kNoMax ? l : fmaf(m, a.scale, (log2f(l) - AttnElt<ELT>::kBias) * 0.6931471805599453f));
+    if (a.lse && lane == 0) a.lse[row] = row_lse<ELT>(a, m, l);
 }
 
 template <int ELT>
@@ -73,12 +69,20 @@ static hipError_t launch_join(const AttnDev &a, int dp, hipStream_t stream) {
     return hipGetLastError();
 }
 
+static int64_t attn_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 struct AttnPlan {
-    int dp, rt, waves, prefix_splits, prefix_blocks, prefix_keys, own_splits, own_blocks;
+    int dp, rt, waves, own_from, prefix_splits, prefix_blocks, prefix_keys, own_splits, own_blocks;
+    bool around;
     int64_t rows, parts, o_bytes, bytes;
 };
 
-static int64_t attn_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Keys of a sequence (by its row's pages) up to which a workgroup takes them all, shared ones and own, in one launch without parts.  Heads of 128: 8 sequences of 460 keys 14.3 us against
+// 16.5 with shared keys apart, of 700 18.4 against 16.6; workgroups that fill the chip twice: 64 sequences of 700 22.5 against 26.9, of 1000 28.2 against 28.4; f32: 4 sequences of
+// 120 10.4 against 14.3, of 240 15.3 against 14.4.
+static int64_t attn_together(int dtype, int64_t groups) { return dtype == ATK_F32 ? 192 : groups >= 2 * kNumCU ? 896 : 512; }
+// Own keys past the caches from more bytes on than the Infinity Cache holds (128 samples on 65536 + 1125 keys: 280 us -> 269; with less, 12 sequences in f32: 33 us -> 37).
+constexpr int64_t kCacheBytes = INT64_C(256) << 20;
 
 static int check_attention(const atk_attention_args *p, bool pointers) {
     if (!p) return ATK_ERR_NULL_PTR;
@@ -142,26 +146,32 @@ static int plan_attention(const atk_attention_args *p, AttnPlan *pl) {
     const int group = (int)(p->heads / p->kv_heads);
     pl->dp = p->dim <= 64 ? 64 : p->dim <= 128 ? 128 : 256;
     const int64_t rows = p->batch * p->tokens * group, own_rows = p->tokens * group;
-    // a sequence's own keys: as many as its row could hold, the device knows how many there are; workgroups for about three a CU
-    const int64_t own = p->row_pages * p->page_size - p->prefix_len, step = kAttnWaves * kTileKeys;
+    // A sequence's own keys: as many as its row could hold, the device knows how many there are; workgroups for about three a CU.  Few keys are one workgroup's, shared ones and own,
+    // and that is the whole call.
+    const int64_t step = kAttnWaves * kTileKeys, all = p->row_pages * p->page_size;
     pl->own_blocks = (int)attn_ceil(own_rows, 16);
     const int64_t own_base = p->batch * p->kv_heads * pl->own_blocks;
-    pl->own_splits = own > 0 ? (int)std::min(attn_ceil(own, step), std::max<int64_t>(1, 3 * kNumCU / own_base)) : 0;
+    const bool together = all <= attn_together(p->dtype, own_base);
+    const int64_t own = together ? all : all - p->prefix_len;
+    pl->own_from = together ? 0 : (int)p->prefix_len;
+    pl->own_splits = together ? 1 : own > 0 ? (int)std::min(attn_ceil(own, step), std::max<int64_t>(1, 3 * kNumCU / own_base)) : 0;
+    pl->around = p->batch * own * p->kv_heads * p->dim * 2 * (p->dtype == ATK_F32 ? 4 : 2) > kCacheBytes;
     // how the shared keys meet the rows: up to two 16-row tiles in every wavefront, or 32 rows a wavefront and keys by way of LDS
     // (attn_block_kernel's addresses: four tokens' offsets and a page's place in 16 bytes are 32 bits)
     auto reaches = [&](const int64_t *stride) {
         const int64_t most = INT64_C(1) << 34;
         return stride[1] < (INT64_C(1) << 28) && stride[1] <= most / p->page_size && stride[0] <= most / p->n_pages;
     };
-    pl->rt = rows <= 16 || p->prefix_len == 0 ? 1 : 2, pl->waves = kAttnWaves;
+    const bool shared = p->prefix_len > 0 && !together;
+    pl->rt = rows <= 16 || !shared ? 1 : 2, pl->waves = kAttnWaves;
     pl->prefix_splits = 0, pl->prefix_keys = 0;
-    if (rows > 32 && p->dtype != ATK_F32 && p->prefix_len > 0 && p->page_size % 4 == 0 && reaches(p->k_stride) && reaches(p->v_stride)) {
+    if (rows > 32 && p->dtype != ATK_F32 && shared && p->page_size % 4 == 0 && reaches(p->k_stride) && reaches(p->v_stride)) {
         pl->rt = 0;
         plan_blocks(p, rows, pl);
     } else {
         if (pl->rt > attn_max_rt(p->dtype, pl->dp)) pl->rt = 1;
         pl->prefix_blocks = (int)attn_ceil(rows, 16 * pl->rt);
-        if (p->prefix_len > 0) split_prefix(p, pl, step, std::max<int64_t>(1, 2 * kNumCU / (pl->prefix_blocks * p->kv_heads)));
+        if (shared) split_prefix(p, pl, step, std::max<int64_t>(1, 2 * kNumCU / (pl->prefix_blocks * p->kv_heads)));
     }
     const int64_t base = pl->prefix_blocks * p->kv_heads;
     pl->rows = p->batch * p->tokens * p->heads;
@@ -204,7 +214,7 @@ int atk_shared_prefix_attention(const atk_attention_args *p, void *work, int64_t
     a.rows = (int)p->rows, a.row_pages = (int)p->row_pages, a.n_pages = (int)p->n_pages;
     a.prefix_len = (int)p->prefix_len;
     a.prefix_splits = pl.prefix_splits, a.prefix_blocks = pl.prefix_blocks, a.prefix_keys = pl.prefix_keys;
-    a.own_splits = pl.own_splits, a.own_blocks = pl.own_blocks;
+    a.own_splits = pl.own_splits, a.own_blocks = pl.own_blocks, a.own_from = pl.own_from, a.around = pl.around;
     a.n_prefix = pl.prefix_splits * pl.prefix_blocks * a.kv_heads;
     a.prefix_grid = (a.n_prefix + 7) / 8 * 8;
     a.masked_grid = 0, a.block_rows = pl.rt == 0 ? 32 * pl.waves : 0;
@@ -217,7 +227,7 @@ int atk_shared_prefix_attention(const atk_attention_args *p, void *work, int64_t
     hipError_t e = p->dtype == ATK_F32    ? launch_attn_f32(a, pl.dp, pl.rt, pl.waves, s)
                    : p->dtype == ATK_BF16 ? launch_attn_bf16(a, pl.dp, pl.rt, pl.waves, s)
                                           : launch_attn_f16(a, pl.dp, pl.rt, pl.waves, s);
-    if (e == hipSuccess)
+    if (e == hipSuccess && pl.parts > 1)
         e = p->dtype == ATK_F32    ? launch_join<ATK_F32>(a, pl.dp, s)
             : p->dtype == ATK_BF16 ? launch_join<ATK_BF16>(a, pl.dp, s)
                                    : launch_join<ATK_F16>(a, pl.dp, s);

@@ -45,8 +45,10 @@ struct AttnDev {
     int prefix_splits, prefix_blocks, prefix_keys;  // ranges of the shared keys, row blocks, keys of a range (a multiple of a workgroup's tiles)
     int own_splits, own_blocks;
     int n_prefix, prefix_grid, n_own;  // units of the shared keys and workgroups for them, which come first; units of own keys
+    int own_from;                      // where own keys begin: prefix_len, or 0 where a sequence's workgroups take the shared ones as well
     int masked_grid, block_rows;       // workgroups that look for attn_block_kernel's units with masks; rows of such a unit
     int parts;         // prefix_splits + own_splits
+    bool around;       // own keys past the caches
     FastDiv page;
     float scale, scale2;  // scale2: scale * log2(e)
 };
@@ -110,6 +112,12 @@ __device__ __forceinline__ bool not_finite(uint32_t w) {
     return (w & lo) == lo || (w & hi) == hi;
 }
 
+// AROUND: past the caches, for keys that are read once and are more than the caches hold.
+template <bool AROUND, typename T>
+__device__ __forceinline__ T fetch(const void *p) {
+    return AROUND ? __builtin_nontemporal_load((const T *)p) : *(const T *)p;
+}
+
 // The rows of V that a lane has, four of each half: kDvl elements each.
 template <int ELT, int DP>
 struct VRows {
@@ -119,17 +127,18 @@ struct VRows {
     static constexpr int kRows = 4 * attn_halves(ELT);
     uint32_t w[kRows][kWords];
 
+    template <bool AROUND>
     __device__ __forceinline__ void load(int j, const char *row, int n, int dim) {
 #pragma unroll
         for (int x = 0; x < kWords; x += kVec) {
             const int word = n * kWords + x;
             if (DP * AttnElt<ELT>::kBytes / 4 == kVec || word * 4 < dim * AttnElt<ELT>::kBytes) {
                 if (kVec == 4) {
-                    u32x4 t = *(const u32x4 *)(row + word * 4);
+                    const u32x4 t = fetch<AROUND, u32x4>(row + word * 4);
 #pragma unroll
                     for (int y = 0; y < 4; ++y) w[j][x + y] = t[y];
                 } else {
-                    u32x2 t = *(const u32x2 *)(row + word * 4);
+                    const u32x2 t = fetch<AROUND, u32x2>(row + word * 4);
                     w[j][x] = t[0], w[j][x + 1] = t[1];
                 }
             } else {
@@ -183,6 +192,20 @@ __device__ __forceinline__ f32x4 mma_pv(const VRows<ELT, DP> &v, int i, const We
     }
 }
 
+// What becomes of a row: the log of the sum of exponentials from its maximum and sum, four elements of its result.
+template <int ELT>
+__device__ __forceinline__ float row_lse(const AttnDev &a, float m, float l) {
+    if (l == 0.0f) return kNoMax;
+    return m == kNoMax ? l : fmaf(m, a.scale, (log2f(l) - AttnElt<ELT>::kBias) * 0.6931471805599453f);
+}
+template <int ELT>
+__device__ __forceinline__ void store_out(char *out, const f32x4 &o) {
+    if constexpr (ELT == ATK_F32)
+        *(f32x4 *)out = o;
+    else
+        *(u32x2 *)out = u32x2{AttnElt<ELT>::pack(o[0], o[1]), AttnElt<ELT>::pack(o[2], o[3])};
+}
+
 // Row r of the rows that read head h of a range: where its query lies, and how many keys it sees.
 struct AttnRow {
     int b, t, head;
@@ -214,8 +237,11 @@ __device__ __forceinline__ int seq_len(const AttnDev &a, int row, bool *bad) {
     return len < 0 ? 0 : (int)most;
 }
 
-template <int ELT, int DP, int RT, int NW>
-__device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int n_rows, int own_b, const int32_t *table_row, int ka, int kb, int part, char *lds) {
+// Rows r0 .. r0 + 16 * RT - 1 of the n_rows that read head h (own_b: those of that sequence; -1: of all) against keys ka .. kb - 1.  Keys below `shared` are looked up in
+// the row `first` of the table.
+template <int ELT, int DP, int RT, int NW, bool AROUND = false>
+__device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int n_rows, int own_b, const int32_t *table_row, int ka, int kb, int part, char *lds,
+                                           const int32_t *first = nullptr, int shared = 0) {
     typedef AttnElt<ELT> E;
     constexpr int kPiece = 16 / E::kBytes;            // elements of 16 bytes
     constexpr int NC = DP / (4 * kPiece);             // 16-byte pieces of a row that a lane has
@@ -259,7 +285,10 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
     const char *kh = (const char *)a.k + h * a.ks[2] * E::kBytes, *vh = (const char *)a.v + h * a.vs[2] * E::kBytes;
 
     // lane j (and those TK apart) looks key k0 + j up, a tile ahead; keys past the end are read as the last one and masked
-    auto page_of = [&](int k0) { return table_row[a.page.div(min(k0 + (lane & (TK - 1)), kb - 1))]; };
+    auto page_of = [&](int k0) {
+        const int key = min(k0 + (lane & (TK - 1)), kb - 1);
+        return (key < shared ? first : table_row)[a.page.div(key)];
+    };
     int page_next = ka < kb ? page_of(ka + wave * TK) : 0;
     for (int k0 = ka + wave * TK; k0 < kb; k0 += NW * TK) {
         int page = page_next;
@@ -277,7 +306,7 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int at = (c * 4 + g) * 16;
-                kf[x][c] = at < a.dim * E::kBytes ? *(const u32x4 *)(row + at) : u32x4{0, 0, 0, 0};
+                kf[x][c] = at < a.dim * E::kBytes ? fetch<AROUND, u32x4>(row + at) : u32x4{0, 0, 0, 0};
             }
         }
         VRows<ELT, DP> v;
@@ -286,7 +315,7 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
             const int at = (j / 4) * 16 + g * 4 + j % 4;
             const int key = min(k0 + at, kb - 1);
             const char *row = vh + (__shfl(page, at, 64) * a.vs[0] + a.page.mod(key) * a.vs[1]) * E::kBytes;
-            v.load(j, row, n, a.dim);
+            v.template load<AROUND>(j, row, n, a.dim);
         }
         f32x4 s[RT][NX];
 #pragma unroll
@@ -437,6 +466,19 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
         if (r >= n_rows) continue;
         const AttnRow x = attn_row(a, h, r, own_b);
         const int64_t row = ((int64_t)x.b * a.tokens + x.t) * a.heads + x.head;
+        if (a.parts == 1) {  // nothing to join
+            if (g == 0 && a.lse) a.lse[row] = row_lse<ELT>(a, m[rt], total[rt]);
+            const float f = total[rt] == 0.0f ? 0.0f : 1.0f / total[rt];
+            char *out = (char *)a.out + (x.b * a.os[0] + x.t * a.os[1] + x.head * a.os[2]) * E::kBytes;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < NT; i += 4) {
+                    const int d = (g * 4 + j) * NT + i;
+                    if (d < a.dim) store_out<ELT>(out + d * E::kBytes, f32x4{acc[rt][i][j] * f, acc[rt][i + 1][j] * f, acc[rt][i + 2][j] * f, acc[rt][i + 3][j] * f});
+                }
+            continue;
+        }
         if (g == 0) a.parts_ml[row * a.parts + part] = float2{m[rt], total[rt]};
         float *o = a.parts_o + (row * a.parts + part) * a.dim;
 #pragma unroll
@@ -799,8 +841,8 @@ __device__ __forceinline__ int xcd_unit(int id, int n) {
     return (id >> 3) < per && u < n ? u : -1;
 }
 
-// Own keys of a sequence: workgroup y of those.
-template <int ELT, int DP, int NW>
+// Own keys of a sequence, or (own_from 0) all of them: workgroup y of those.
+template <int ELT, int DP, int NW, bool AROUND>
 __device__ __forceinline__ void attn_own(const AttnDev &a, int y, char *lds) {
     bool bad = false;  // (told by attn_range)
     y = xcd_unit(y, a.n_own);
@@ -811,12 +853,19 @@ __device__ __forceinline__ void attn_own(const AttnDev &a, int y, char *lds) {
     x /= a.kv_heads;
     const int split = x % a.own_splits, b = x / a.own_splits;
     const int row = seq_row(a, b, &bad), len = seq_len(a, row, &bad);
-    const int keys = max(0, len - a.prefix_len);
+    int from0 = a.own_from;
+    const int32_t *first = a.table;
+    if (from0 < a.prefix_len) {
+        const int s = seq_row(a, 0, &bad);
+        first += s * a.table_stride;
+        if (s < 0) from0 = a.prefix_len;
+    }
+    const int keys = max(0, len - from0);
     constexpr int kStep = NW * kTileKeys;
     const int per = (int)(((int64_t)keys + a.own_splits * kStep - 1) / (a.own_splits * kStep)) * kStep;
-    const int64_t from = a.prefix_len + (int64_t)split * per;
+    const int64_t from = from0 + (int64_t)split * per;
     const int ka = (int)min((int64_t)len, from), kb = (int)min((int64_t)len, from + per);
-    attn_range<ELT, DP, 1, NW>(a, h, block * 16, a.tokens * a.group, b, a.table + row * a.table_stride, ka, max(ka, kb), a.prefix_splits + split, lds);
+    attn_range<ELT, DP, 1, NW, AROUND>(a, h, block * 16, a.tokens * a.group, b, a.table + row * a.table_stride, ka, max(ka, kb), a.prefix_splits + split, lds, first, a.prefix_len);
 }
 
 template <int DP, int RT, int NW>
@@ -835,7 +884,7 @@ struct SharedUnit {
 
 // Few rows on the shared keys: the wavefronts of a workgroup share its keys out.  Own keys.  Of attn_block_kernel's units (masked_grid), those with a row that sees only a part of the
 // keys - a sequence that ends before them: tile by tile, with masks.
-template <int ELT, int DP, int RT>
+template <int ELT, int DP, int RT, bool AROUND>
 __global__ __launch_bounds__(kAttnWaves * 64, RT == 1 && DP <= 128 ? 2 : 1) void attn_range_kernel(const AttnDev a) {
     __shared__ __align__(16) char lds[attn_lds_bytes<DP, RT, kAttnWaves>()];
     int id = blockIdx.x;
@@ -849,7 +898,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, RT == 1 && DP <= 128 ? 2 : 1) void
     }
     id -= a.prefix_grid;
     if (RT > 1 || id >= a.masked_grid) {
-        attn_own<ELT, DP, kAttnWaves>(a, id - a.masked_grid, lds);
+        attn_own<ELT, DP, kAttnWaves, AROUND>(a, id - a.masked_grid, lds);
         return;
     }
     if constexpr (RT == 1) {
@@ -918,11 +967,14 @@ hipError_t launch_attn_dp(AttnDev a, int rt, int waves, hipStream_t stream) {
     const dim3 g((uint32_t)(a.prefix_grid + a.masked_grid + (a.n_own + 7) / 8 * 8)), threads(kAttnWaves * 64);
     if constexpr (attn_max_rt(ELT, DP) >= 2) {
         if (rt == 2) {
-            hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 2>), g, threads, 0, stream, a);
+            hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 2, false>), g, threads, 0, stream, a);
             return hipGetLastError();
         }
     }
-    hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 1>), g, threads, 0, stream, a);
+    if (a.around)
+        hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 1, true>), g, threads, 0, stream, a);
+    else
+        hipLaunchKernelGGL((attn_range_kernel<ELT, DP, 1, false>), g, threads, 0, stream, a);
     return hipGetLastError();
 }
 template <int ELT>

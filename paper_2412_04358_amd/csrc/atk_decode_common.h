@@ -19,8 +19,6 @@ struct FastDiv {
     }
 #ifdef __HIPCC__
     __device__ __forceinline__ int div(int n) const { return (int)((__umulhi(mul, (uint32_t)n) + (uint32_t)n) >> shift); }
-    // of a scalar: no vector instruction
-    __device__ __forceinline__ int div_uniform(int n) const { return (int)(((uint32_t)(((uint64_t)mul * (uint32_t)n) >> 32) + (uint32_t)n) >> shift); }
     __device__ __forceinline__ int mod(int n) const { return n - div(n) * (int)d; }
 #endif
 };

@@ -51,10 +51,23 @@ def make(B, T, H, Hk, D, prefix, lens, ps, dtype, seed=0, head_major=False, spar
     return dev + [table.int().cuda(), torch.tensor(lens, dtype=torch.int32).cuda()]
 
 
-def check(q, k, v, table, lens, prefix, seqs=None, scale=None, got=None):
+def wider(table, ps, keys=2048):
+    """The table with room for more pages: sequences that could be long have their shared keys taken apart from their own."""
+    wide = torch.full((table.shape[0], table.shape[1] + keys // ps), -1, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = table
+    return wide
+
+
+def check(q, k, v, table, lens, prefix, seqs=None, scale=None):
+    got = _check(q, k, v, table, lens, prefix, seqs, scale)
+    _check(q, k, v, wider(table, k.shape[1]), lens, prefix, seqs, scale)
+    return got
+
+
+def _check(q, k, v, table, lens, prefix, seqs, scale):
     D = q.shape[3]
     status = torch.zeros((1,), dtype=torch.int32, device="cuda")
-    out, lse = got if got is not None else atk.shared_prefix_attention(q, k, v, table, lens, prefix, seqs=seqs, scale=scale, return_lse=True, status=status)
+    out, lse = atk.shared_prefix_attention(q, k, v, table, lens, prefix, seqs=seqs, scale=scale, return_lse=True, status=status)
     torch.cuda.synchronize()
     c = [x.double().cpu().numpy() for x in (q, k, v)]
     want, wlse, mass, size, count, top = oracle.attention(*c, table.cpu().numpy(), lens.cpu().numpy(), prefix, None if seqs is None else seqs.cpu().numpy(), D ** -0.5 if scale is None else scale)
@@ -184,10 +197,13 @@ def test_rows_that_see_nothing(dtype):
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
-def test_masked_values_have_no_influence(dtype, value):
+@pytest.mark.parametrize("wide", [False, True])
+def test_masked_values_have_no_influence(dtype, value, wide):
     # the last new token's key and value are not finite: the queries before it do not see them
     q, k, v, table, lens = make(3, 4, 8, 2, 64, 33, [37, 70, 50], 16, dtype, seed=9)
-    clean, _ = check(q, k, v, table, lens, 33)
+    if wide:
+        table = wider(table, 16)
+    clean, _ = _check(q, k, v, table, lens, 33, None, None)
     for b in range(3):
         n = int(lens[b]) - 1
         k[table[b, n // 16].long(), n % 16] = value
@@ -262,8 +278,10 @@ def test_same_result_every_time_and_on_other_streams():
         assert torch.equal(g[0], want[0]) and torch.equal(g[1], want[1])
 
 
-def test_graph_follows_lengths():
+@pytest.mark.parametrize("keys", [0, 2048])
+def test_graph_follows_lengths(keys):
     q, k, v, table, lens = make(4, 1, 8, 2, 64, 100, [164, 150, 130, 120], 16, torch.float16, seed=13)
+    table = wider(table, 16, keys)
     out = torch.empty_like(q)
     atk.shared_prefix_attention(q, k, v, table, lens, 100, out=out)
     torch.cuda.synchronize()
@@ -279,9 +297,11 @@ def test_graph_follows_lengths():
         assert torch.equal(out, want), step
 
 
-def test_bad_numbers_on_the_device():
+@pytest.mark.parametrize("keys", [0, 2048])
+def test_bad_numbers_on_the_device(keys):
     status = torch.zeros((1,), dtype=torch.int32, device="cuda")
     args = make(3, 1, 4, 2, 64, 20, [30, 40, 50], 16, torch.bfloat16, seed=14)
+    args[3] = wider(args[3], 16, keys)
     good = atk.shared_prefix_attention(*args, 20, status=status)
     assert status.item() == 0
     q, k, v, table, lens = args
@@ -298,6 +318,19 @@ def test_bad_numbers_on_the_device():
     assert status.item() & atk.ATK_STATUS_BAD_LEN and torch.equal(out[0], good[0]) and (out[2] == 0).all()
     out = atk.shared_prefix_attention(q, k, v, bad, lens, 20)    # without a status: as quiet
     assert torch.equal(out[0], good[0])
+
+
+def test_shared_keys_are_read_through_the_first_row():
+    # the other rows hold nothing there, and the first one is no row: nobody has shared keys then
+    for keys in (0, 2048):
+        q, k, v, table, lens = make(3, 1, 4, 2, 64, 40, [50, 60, 45], 16, torch.bfloat16, seed=15)
+        table = wider(table, 16, keys)
+        want = atk.shared_prefix_attention(q, k, v, table, lens, 32)
+        table[1:, :2] = -1
+        status = torch.zeros((1,), dtype=torch.int32, device="cuda")
+        assert torch.equal(atk.shared_prefix_attention(q, k, v, table, lens, 32, status=status), want) and status.item() == 0
+        out = atk.shared_prefix_attention(q, k, v, table, lens, 32, seqs=torch.tensor([99, 1, 2], dtype=torch.int32, device="cuda"), status=status)
+        assert status.item() == atk.ATK_STATUS_BAD_SEQ and (out[0] == 0).all() and torch.isfinite(out).all()
 
 
 def test_pages_past_32_bits():
