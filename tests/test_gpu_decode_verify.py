@@ -42,19 +42,24 @@ def test_shapes(dtype, B, L, V, pad):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
-def test_no_drafts_and_ragged_drafts(dtype):
-    target, tokens, draft, u, r = make(6, 4, 3001, dtype, seed=5, agree=0.1)
+@pytest.mark.parametrize("V", [3001, 70001])   # rows by one workgroup, rows by many
+def test_no_drafts_and_ragged_drafts(dtype, V):
+    target, tokens, draft, u, r = make(6, 4, V, dtype, seed=5, agree=0.1)
     check(target, tokens, draft, u, r, torch.tensor([0, 1, 2, 3, 4, 9], dtype=torch.int32, device="cuda"))
     check(target, tokens, draft, u, r, torch.tensor([-3, 1, 0, 0, 4, 4], dtype=torch.int32, device="cuda"))
-    args = make(3, 0, 500, dtype, seed=6)
+    args = make(3, 0, V, dtype, seed=6)
     accepted, out = check(*args)
     assert (accepted == 0).all() and out.shape == (3, 1)
     check(args[0], args[1], None, args[3], args[4])
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
-def test_certain_drafts(dtype):
+@pytest.mark.parametrize("V", [37, 66003])
+def test_certain_drafts(dtype, V):
     target, tokens, _, u, r = make(40, 4, 37, dtype, seed=7)
+    wide = torch.zeros((40, 5, V), dtype=dtype, device="cuda")
+    wide[..., V - 37:] = target
+    target = wide
     tokens = target[:, :4].float().argmax(2).int()
     accepted, out = check(target, tokens, None, u, r)
     rejected = accepted < 4
@@ -75,30 +80,31 @@ def test_borders():
             assert out.tolist() == [[2, -1]] if want == 0 else [[0, token]]
 
 
-def test_weights_of_nothing():
-    z = torch.zeros((2, 2, 300), device="cuda")
+@pytest.mark.parametrize("V", [300, 70000])
+def test_weights_of_nothing(V):
+    z = torch.zeros((2, 2, V), device="cuda")
     u, r = torch.full((2, 1), 0.5, device="cuda"), torch.tensor([0.0, 0.9], device="cuda")
-    tokens = torch.tensor([[5], [299]], dtype=torch.int32, device="cuda")
+    tokens = torch.tensor([[5], [V - 1]], dtype=torch.int32, device="cuda")
     accepted, out = check(z, tokens, z[:, :1], u, r)                      # no weight anywhere: no token
     assert (accepted == 0).all() and (out == -1).all()
     p = z.clone()
     p[:, :, 7], p[:, :, 250] = 0.5, 0.5
     accepted, out = check(p, tokens, p[:, :1], u, r)                      # rejected (p is 0 there) with nothing left: p itself
     assert out[:, 0].tolist() == [7, 250]
-    accepted, out = check(p, torch.tensor([[-1], [300]], dtype=torch.int32, device="cuda"), z[:, :1], u, r)   # tokens outside the vocabulary
+    accepted, out = check(p, torch.tensor([[-1], [V]], dtype=torch.int32, device="cuda"), z[:, :1], u, r)   # tokens outside the vocabulary
     assert (accepted == 0).all() and out[:, 0].tolist() == [7, 250]
     p[:, :, 8], p[:, :, 100] = float("nan"), -0.25                        # weigh nothing
     accepted, out = atk.verify_drafts(p, tokens, z[:, :1], u, r)
     assert out[:, 0].tolist() == [7, 250]
     p[:, :, 9] = float("inf")                                             # no sum: some index, none out of range
     _, out = atk.verify_drafts(p, tokens, z[:, :1], u, r)
-    assert ((out[:, 0] >= -1) & (out[:, 0] < 300)).all()
+    assert ((out[:, 0] >= -1) & (out[:, 0] < V)).all()
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 def test_ends_of_the_running_sum(dtype):
     # single weights at the first and last element, equal weights (exact sums), r from 0 to the largest below 1
-    for V in (257, 4096, 20001):
+    for V in (257, 4096, 20001, 32768, 66001, 133000):
         p = torch.zeros((4, 1, V), dtype=dtype)
         p[0, 0, 0] = p[1, 0, V - 1] = 1.0
         p[2, 0, :] = 2.0 ** -12
@@ -111,8 +117,9 @@ def test_ends_of_the_running_sum(dtype):
             assert np.array_equal(out.cpu().numpy(), want)
 
 
-def test_streams_and_graph():
-    args = make(8, 4, 32001, torch.bfloat16, seed=21)
+@pytest.mark.parametrize("V", [32001, 90001])
+def test_streams_and_graph(V):
+    args = make(8, 4, V, torch.bfloat16, seed=21)
     want = check(*args)
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
