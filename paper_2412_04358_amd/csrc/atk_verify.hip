@@ -103,13 +103,21 @@ struct Raw8 {  // eight elements as they lie in memory
 template <int ELT>
 __device__ __forceinline__ void weights8(const VerifyRow<ELT> &row, int64_t v, int64_t to, double *left, double *all) {
     if (v + kEach <= to) {
-        Raw8<ELT> p, q;
+        Raw8<ELT> p;
         p.load(row.p, v);
-        if (row.q) q.load(row.q, v);
+        if (row.q) {
+            Raw8<ELT> q;
+            q.load(row.q, v);
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) left[e] = p.value(e) - q.value(e);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) left[e] = v + e == row.certain ? p.value(e) - 1.0 : p.value(e);
+        }
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
-            const double x = p.value(e), y = row.q ? x - q.value(e) : v + e == row.certain ? x - 1.0 : x;
-            left[e] = y > 0 ? y : 0.0, all[e] = x > 0 ? x : 0.0;
+            const double x = p.value(e);
+            left[e] = left[e] > 0 ? left[e] : 0.0, all[e] = x > 0 ? x : 0.0;
         }
     } else {
 #pragma unroll
