@@ -22,7 +22,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const AttnDev a) {
     const int d = (lane % LPR) * 4;
     f32x4 o = {0, 0, 0, 0};
     if (d < a.dim) {
-        // eight parts in flight: one after the other their loads were nearly all of the time (64 samples, 17 parts: 9.9 us against 5.2)
+        // eight parts in flight: one after the other their loads were nearly all of the time (64 samples, 17 parts: 9.9 us against 7.5)
         constexpr int kStep = 64 / LPR;
         const float *from = a.parts_o + row * a.parts * a.dim + d;
         for (int p0 = lane / LPR; p0 < a.parts; p0 += 8 * kStep) {

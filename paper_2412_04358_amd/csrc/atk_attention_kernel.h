@@ -24,7 +24,7 @@ constexpr float kNoMax = -__builtin_inff();
 constexpr int kAttnWaves = 4;      // of a workgroup of attn_range_kernel: they take turns at the tiles of its range and join through LDS
 constexpr int kTileKeys = 32;      // keys of a wavefront that ranges are cut by
 // Halves of 16 keys that a wavefront takes at a time: two, whose keys are the 32 of a 16-bit product; one in f32, whose products take a key of each lane group, where K and V of 32 keys would
-// leave a SIMD one wavefront (12 sequences of 16 heads on 2047 + 191 keys of 128: 29 us with two halves).
+// leave a SIMD one wavefront (12 sequences of 16 heads on 2047 + 191 keys of 128: 29 us with two halves, 26 with one).
 constexpr int attn_halves(int elt) { return elt == ATK_F32 ? 1 : 2; }
 constexpr float kLazyMax = 8.0f;   // the maximum that weights are taken relative to follows the true one when that is 2^8 above it: 2^8 times the largest weight is
                                    // far from f32's and bf16's range, and rescaling is rare
@@ -500,7 +500,8 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
 //   each 32 keys those with 8 * i + 4 * (lane / 32) + 0..3; step x of the second product takes i = 2 x and 2 x + 1.
 //   A tile is a phase of products (those of the tile before with V, this one's with K) and one of vector instructions (maximum, exponentials, packing, the next
 //   tiles' loads), and with eight wavefronts each SIMD has two of them, one of each half: the second half is a phase late, so that one of the two has the matrix
-//   units while the other one has the vector unit.  128 samples of 32 heads on 65536 keys: 139 us, 0.99 PFLOP/s where a large matrix product reaches 1.1; the matrix units are busy for
+//   units while the other one has the vector unit.  128 samples of 32 heads on 65536 keys: 139 us by itself (0.99 PFLOP/s where a
+//   large matrix product reaches 1.1), 148 to 151 right after other launches; the matrix units are busy for
 //   55 % of the cycles, and the clock is down to 1.7 GHz, as it is under matrix products of such data alone.  With one meeting of the wavefronts a tile in place of two: 160 us.
 //   K and V come from memory into LDS without passing through registers, row by row, 1 KB an instruction, a tile ahead.  (By way of registers, with V transposed there, the loads' and
 //   stores' instructions were half of the vector phase: 128 samples' 65536 keys took 184 us, and take 139.)  V is transposed on the way out, by

@@ -1,11 +1,11 @@
 // verify_drafts: accepted drafts, and one token drawn from what is left of the target's probabilities (include/atk_decode.h).
 //
-// 64 requests of 5 drafts over 128256 tokens in bf16: 33 MB at the least, 10 + 8 us; one request over 32000: 9 us for the call.
+// 64 requests of 5 drafts over 128256 tokens in bf16: 33 MB at the least, 11 + 8 us; one request over 32000 f32: 9 us, one launch.
 //
 // Only one row of the target's probabilities is needed whole, and after a rejection one of the draft's: those of the first rejected
 // token.  verify_sums_kernel finds it (a few gathers, done again by every workgroup of the request), and sums the weights of tiles of that row;
-// verify_draw_kernel finds the tile, then a lane's eight elements, then the element at which the running sum passes the goal.  verify_row_kernel does both for short rows.  Sums are f64: an index is what comes out, and the
-// running sum of 10^5 f32 would be off by more than the weights.
+// verify_draw_kernel finds the tile, then a lane's eight elements, then the element at which the running sum passes the goal.
+// verify_row_kernel does both for short rows.  Sums are f64: an index is what comes out, and the running sum of 10^5 f32 would be off by more than the weights.
 #include "atk_decode_common.h"
 
 namespace atk {
