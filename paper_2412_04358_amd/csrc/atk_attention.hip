@@ -120,24 +120,37 @@ static void split_prefix(const atk_attention_args *p, AttnPlan *pl, int64_t step
 // attn_block_kernel: four or eight wavefronts a workgroup, and how many ranges.  More ranges fill more CUs, and every range costs each row a partial result that is written and read
 // again.  In microseconds, as measured with heads of 128: a workgroup takes 7 and for each tile of 64 keys 2.2 with eight wavefronts, 1.4 with four and 2.5 with two workgroups
 // of four on a CU; partial results 0.65 a megabyte.
-static void plan_blocks(const atk_attention_args *p, int64_t rows, AttnPlan *pl) {
+// attn_mixed_kernel: one workgroup of four on a CU, of which own keys then take the other half; `own`: microseconds of own keys by themselves (4.4 TB/s, and a launch), as many
+// as the sequences' rows could hold.  64 samples on 8192 + 384 keys, 32 heads on 8 of 128: 58 us -> 49.  Only the device knows the lengths, so it may not cost much where own keys
+// are few (kMixedLoss): 128 samples on 65536 + 1125 keys would take 248 us and not 270, but on 65536 alone 200 and not 165.
+constexpr double kMixedLoss = 10;
+static void plan_blocks(const atk_attention_args *p, int64_t rows, double own, AttnPlan *pl) {
     const double wide = pl->dp == 64 ? 0.6 : pl->dp == 128 ? 1.0 : 2.0;
     const int64_t steps = attn_ceil(p->prefix_len, kBlockKeys);
-    double best = 0;
-    int64_t best_splits = 1;
+    double best = 0, mixed = 0;
+    int64_t best_splits = 1, mixed_splits = 0;
     pl->waves = 4;
-    for (int waves = 4; waves <= attn_max_waves(pl->dp); waves *= 2) {
+    auto each = [&](int waves, int64_t most, auto cost) {
         const int64_t blocks = attn_ceil(rows, 32 * waves), base = blocks * p->kv_heads;
-        for (int64_t wanted = kNumCU / 8; wanted <= 4 * kNumCU; wanted += std::min<int64_t>(wanted, kNumCU)) {  // workgroups: an eighth of the CUs to four on each
+        for (int64_t wanted = kNumCU / 8; wanted <= most; wanted += std::min<int64_t>(wanted, kNumCU)) {  // workgroups: an eighth of the CUs to four on each
             const int64_t splits = std::min(steps, std::max<int64_t>(1, wanted / base));
-            const int64_t tiles = attn_ceil(steps, splits), groups = base * attn_ceil(steps, tiles);
+            const int64_t tiles = attn_ceil(steps, splits), ranges = attn_ceil(steps, tiles);
+            cost(splits, tiles, base * ranges, 0.65e-6 * 4 * (double)(rows * p->kv_heads * p->dim) * (double)ranges);
+        }
+    };
+    for (int waves = 4; waves <= attn_max_waves(pl->dp); waves *= 2)
+        each(waves, 4 * kNumCU, [&](int64_t splits, int64_t tiles, int64_t groups, double partial) {
             const bool full = waves == 8 || (groups > kNumCU && pl->dp <= 128);
             const double rounds = (double)attn_ceil(groups, waves == 4 && full ? 2 * kNumCU : kNumCU);
-            const double mb = 1e-6 * 4 * (double)(rows * p->kv_heads * p->dim) * (double)attn_ceil(steps, tiles);
-            const double us = rounds * (7 + tiles * wide * (waves == 8 ? 2.2 : full ? 2.5 : 1.4)) + 0.65 * mb;
+            const double us = rounds * (7 + tiles * wide * (waves == 8 ? 2.2 : full ? 2.5 : 1.4)) + partial;
             if (best == 0 || us < best) best = us, best_splits = splits, pl->waves = waves;
-        }
-    }
+        });
+    if (own > 0 && attn_max_waves(pl->dp) >= 8)
+        each(kAttnWaves, kNumCU, [&](int64_t splits, int64_t tiles, int64_t groups, double partial) {
+            const double alone = 7 + tiles * wide * 1.4, us = std::max(alone, own) + partial;
+            if (groups <= kNumCU && alone + partial <= best + kMixedLoss && us < best + own && (mixed == 0 || us < mixed)) mixed = us, mixed_splits = splits;
+        });
+    if (mixed_splits) pl->rt = kMixed, pl->waves = kAttnWaves, best_splits = mixed_splits;
     pl->prefix_blocks = (int)attn_ceil(rows, 32 * pl->waves);
     split_prefix(p, pl, kBlockKeys, best_splits);
 }
@@ -155,7 +168,8 @@ static int plan_attention(const atk_attention_args *p, AttnPlan *pl) {
     const int64_t own = together ? all : all - p->prefix_len;
     pl->own_from = together ? 0 : (int)p->prefix_len;
     pl->own_splits = together ? 1 : own > 0 ? (int)std::min(attn_ceil(own, step), std::max<int64_t>(1, 3 * kNumCU / own_base)) : 0;
-    pl->around = p->batch * own * p->kv_heads * p->dim * 2 * (p->dtype == ATK_F32 ? 4 : 2) > kCacheBytes;
+    const int64_t own_bytes = p->batch * own * p->kv_heads * p->dim * 2 * (p->dtype == ATK_F32 ? 4 : 2);
+    pl->around = own_bytes > kCacheBytes;
     // how the shared keys meet the rows: up to two 16-row tiles in every wavefront, or 32 rows a wavefront and keys by way of LDS
     // (attn_block_kernel's addresses: four tokens' offsets and a page's place in 16 bytes are 32 bits)
     auto reaches = [&](const int64_t *stride) {
@@ -167,7 +181,7 @@ static int plan_attention(const atk_attention_args *p, AttnPlan *pl) {
     pl->prefix_splits = 0, pl->prefix_keys = 0;
     if (rows > 32 && p->dtype != ATK_F32 && shared && p->page_size % 4 == 0 && reaches(p->k_stride) && reaches(p->v_stride)) {
         pl->rt = 0;
-        plan_blocks(p, rows, pl);
+        plan_blocks(p, rows, own > 0 ? 3 + own_bytes / 4.4e6 : 0, pl);
     } else {
         if (pl->rt > attn_max_rt(p->dtype, pl->dp)) pl->rt = 1;
         pl->prefix_blocks = (int)attn_ceil(rows, 16 * pl->rt);
@@ -217,7 +231,7 @@ int atk_shared_prefix_attention(const atk_attention_args *p, void *work, int64_t
     a.own_splits = pl.own_splits, a.own_blocks = pl.own_blocks, a.own_from = pl.own_from, a.around = pl.around;
     a.n_prefix = pl.prefix_splits * pl.prefix_blocks * a.kv_heads;
     a.prefix_grid = (a.n_prefix + 7) / 8 * 8;
-    a.masked_grid = 0, a.block_rows = pl.rt == 0 ? 32 * pl.waves : 0;
+    a.masked_grid = 0, a.block_rows = pl.rt <= 0 ? 32 * pl.waves : 0;
     a.n_own = a.batch * a.kv_heads * pl.own_blocks * pl.own_splits;
     a.parts = (int)pl.parts;
     a.page.set((uint32_t)p->page_size);

@@ -883,60 +883,83 @@ struct SharedUnit {
     }
 };
 
-// Few rows on the shared keys: the wavefronts of a workgroup share its keys out.  Own keys.  Of attn_block_kernel's units (masked_grid), those with a row that sees only a part of the
-// keys - a sequence that ends before them: tile by tile, with masks.
+// Of attn_block_kernel's units (the first masked_grid workgroups), those with a row that sees only a part of the keys - a sequence that ends before them: tile by tile, with masks.  Then
+// own keys.
+template <int ELT, int DP, bool AROUND>
+__device__ __forceinline__ void attn_rest(const AttnDev &a, int id, char *lds) {
+    if (id >= a.masked_grid) {
+        attn_own<ELT, DP, kAttnWaves, AROUND>(a, id - a.masked_grid, lds);
+        return;
+    }
+    const int u = xcd_unit(id, a.n_prefix), n_rows = a.batch * a.tokens * a.group;
+    if (u < 0) return;
+    const SharedUnit s(a, u);
+    const int r0 = s.block * a.block_rows;
+    bool all = s.ka < s.kb;
+    for (int r = r0 + threadIdx.x; r < min(n_rows, r0 + a.block_rows); r += kAttnWaves * 64) {
+        const AttnRow x = attn_row(a, s.h, r, -1);
+        bool bad = false;
+        if (seq_len(a, seq_row(a, x.b, &bad), &bad) - (a.tokens - 1 - x.t) < s.kb) all = false;
+    }
+    if (__syncthreads_and(all)) return;
+    for (int r = r0; r < min(n_rows, r0 + a.block_rows); r += 16) {
+        attn_range<ELT, DP, 1, kAttnWaves>(a, s.h, r, n_rows, -1, a.table + s.row * a.table_stride, s.ka, s.kb, s.split, lds);
+        __syncthreads();
+    }
+}
+
+// Few rows on the shared keys: the wavefronts of a workgroup share its keys out.  And the rest.
 template <int ELT, int DP, int RT, bool AROUND>
 __global__ __launch_bounds__(kAttnWaves * 64, RT == 1 && DP <= 128 ? 2 : 1) void attn_range_kernel(const AttnDev a) {
     __shared__ __align__(16) char lds[attn_lds_bytes<DP, RT, kAttnWaves>()];
     int id = blockIdx.x;
-    const int n_rows = a.batch * a.tokens * a.group;
     if (id < a.prefix_grid) {
         const int u = xcd_unit(id, a.n_prefix);
         if (u < 0) return;
         const SharedUnit s(a, u);
-        attn_range<ELT, DP, RT, kAttnWaves>(a, s.h, s.block * RT * 16, n_rows, -1, a.table + s.row * a.table_stride, s.ka, s.kb, s.split, lds);
+        attn_range<ELT, DP, RT, kAttnWaves>(a, s.h, s.block * RT * 16, a.batch * a.tokens * a.group, -1, a.table + s.row * a.table_stride, s.ka, s.kb, s.split, lds);
         return;
     }
     id -= a.prefix_grid;
-    if (RT > 1 || id >= a.masked_grid) {
-        attn_own<ELT, DP, kAttnWaves, AROUND>(a, id - a.masked_grid, lds);
-        return;
-    }
-    if constexpr (RT == 1) {
-        const int u = xcd_unit(id, a.n_prefix);
-        if (u < 0) return;
-        const SharedUnit s(a, u);
-        const int r0 = s.block * a.block_rows;
-        bool all = s.ka < s.kb;
-        for (int r = r0 + threadIdx.x; r < min(n_rows, r0 + a.block_rows); r += kAttnWaves * 64) {
-            const AttnRow x = attn_row(a, s.h, r, -1);
-            bool bad = false;
-            if (seq_len(a, seq_row(a, x.b, &bad), &bad) - (a.tokens - 1 - x.t) < s.kb) all = false;
-        }
-        if (__syncthreads_and(all)) return;
-        for (int r = r0; r < min(n_rows, r0 + a.block_rows); r += 16) {
-            attn_range<ELT, DP, 1, kAttnWaves>(a, s.h, r, n_rows, -1, a.table + s.row * a.table_stride, s.ka, s.kb, s.split, lds);
-            __syncthreads();
-        }
-    }
+    if constexpr (RT == 1)
+        attn_rest<ELT, DP, AROUND>(a, id, lds);
+    else
+        attn_own<ELT, DP, kAttnWaves, AROUND>(a, id, lds);
 }
 
 // Many: its wavefronts share its rows out.
 template <int ELT, int DP, int NW, bool FULL>
-__global__ __launch_bounds__(NW * 64, DP <= 128 ? 2 : 1) void attn_block_kernel(const AttnDev a) {
-    __shared__ __align__(1024) char lds[BlockLds<DP, NW>::kBytes];
-    const int u = xcd_unit(blockIdx.x, a.n_prefix);
+__device__ __forceinline__ void attn_block_unit(const AttnDev &a, int id, char *lds) {
+    const int u = xcd_unit(id, a.n_prefix);
     if (u < 0) return;
     const SharedUnit s(a, u);
     if (s.ka < s.kb) attn_block<ELT, DP, NW, FULL>(a, s.h, s.block * NW * 32, a.batch * a.tokens * a.group, a.table + s.row * a.table_stride, s.ka, s.kb, s.split, lds);
 }
+template <int ELT, int DP, int NW, bool FULL>
+__global__ __launch_bounds__(NW * 64, DP <= 128 ? 2 : 1) void attn_block_kernel(const AttnDev a) {
+    __shared__ __align__(1024) char lds[BlockLds<DP, NW>::kBytes];
+    attn_block_unit<ELT, DP, NW, FULL>(a, blockIdx.x, lds);
+}
 
-// rt: 16-row tiles of a workgroup of attn_range_kernel; 0: attn_block_kernel on the shared keys, waves of 32 rows, and own keys in a launch of their own: they are bound by
-// memory, and one workgroup of attn_block_kernel takes all registers of a CU (in one launch 64 samples' 130 MB took 53 us, apart 25 + 24)
+// Many rows and the rest in one launch: a workgroup of each to a CU (plan_blocks), so that the matrix units and memory work side by side.  The workgroups come in the order of their
+// numbers, so all of the first kind are there when the others begin; in turns, 64 samples on 8192 + 384 keys took 58 us and not 50.
+template <int ELT, int DP, bool FULL, bool AROUND>
+__global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_mixed_kernel(const AttnDev a) {
+    static_assert(BlockLds<DP, kAttnWaves>::kBytes >= attn_lds_bytes<DP, 1, kAttnWaves>(), "LDS of either kind");
+    __shared__ __align__(1024) char lds[BlockLds<DP, kAttnWaves>::kBytes];
+    const int id = blockIdx.x;
+    if (id < a.prefix_grid)
+        attn_block_unit<ELT, DP, kAttnWaves, FULL>(a, id, lds);
+    else
+        attn_rest<ELT, DP, AROUND>(a, id - a.prefix_grid, lds);
+}
+
+// rt: 16-row tiles of a workgroup of attn_range_kernel; 0: attn_block_kernel on the shared keys, waves of 32 rows, and own keys in a launch of their own; kMixed: both in one
 hipError_t launch_attn_bf16(const AttnDev &a, int dp, int rt, int waves, hipStream_t stream);
 hipError_t launch_attn_f16(const AttnDev &a, int dp, int rt, int waves, hipStream_t stream);
 hipError_t launch_attn_f32(const AttnDev &a, int dp, int rt, int waves, hipStream_t stream);
 
+constexpr int kMixed = -1;
 // 16-row tiles of a workgroup's rows that attn_range_kernel is built for: registers hold Q, K, V and O of RT tiles, up to 512 words of a lane
 constexpr int attn_max_rt(int elt, int dp) { return dp > 128 ? 1 : 2; }
 // wavefronts of a workgroup of attn_block_kernel: eight at 256 words of a lane, or four at up to 512
@@ -944,6 +967,19 @@ constexpr int attn_max_waves(int dp) { return dp > 128 ? 4 : 8; }
 
 template <int ELT, int DP>
 hipError_t launch_attn_dp(AttnDev a, int rt, int waves, hipStream_t stream) {
+    if constexpr (ELT != ATK_F32 && attn_max_waves(DP) >= 8) {
+        if (rt == kMixed) {
+            const dim3 g((uint32_t)(2 * a.prefix_grid + (a.n_own + 7) / 8 * 8)), threads(kAttnWaves * 64);
+            a.masked_grid = a.prefix_grid;
+            if (a.dim < DP)  // (rare: without the instance past the caches)
+                hipLaunchKernelGGL((attn_mixed_kernel<ELT, DP, false, false>), g, threads, 0, stream, a);
+            else if (a.around)
+                hipLaunchKernelGGL((attn_mixed_kernel<ELT, DP, true, true>), g, threads, 0, stream, a);
+            else
+                hipLaunchKernelGGL((attn_mixed_kernel<ELT, DP, true, false>), g, threads, 0, stream, a);
+            return hipGetLastError();
+        }
+    }
     if constexpr (ELT != ATK_F32) {
         if (rt == 0) {
             const dim3 g((uint32_t)a.prefix_grid);
