@@ -234,6 +234,7 @@ int atk_shared_prefix_attention(const atk_attention_args *p, void *work, int64_t
     a.masked_grid = 0, a.block_rows = pl.rt <= 0 ? 32 * pl.waves : 0;
     a.n_own = a.batch * a.kv_heads * pl.own_blocks * pl.own_splits;
     a.parts = (int)pl.parts;
+    a.direct = pl.parts == 1 && pl.rt > 0;  // attn_block writes parts only, and where its ranges are all there is, they can be one
     a.page.set((uint32_t)p->page_size);
     a.scale = (float)p->scale;
     a.scale2 = (float)(p->scale * 1.4426950408889634);
@@ -241,7 +242,7 @@ int atk_shared_prefix_attention(const atk_attention_args *p, void *work, int64_t
     hipError_t e = p->dtype == ATK_F32    ? launch_attn_f32(a, pl.dp, pl.rt, pl.waves, s)
                    : p->dtype == ATK_BF16 ? launch_attn_bf16(a, pl.dp, pl.rt, pl.waves, s)
                                           : launch_attn_f16(a, pl.dp, pl.rt, pl.waves, s);
-    if (e == hipSuccess && pl.parts > 1)
+    if (e == hipSuccess && !a.direct)
         e = p->dtype == ATK_F32    ? launch_join<ATK_F32>(a, pl.dp, s)
             : p->dtype == ATK_BF16 ? launch_join<ATK_BF16>(a, pl.dp, s)
                                    : launch_join<ATK_F16>(a, pl.dp, s);

@@ -49,6 +49,7 @@ struct AttnDev {
     int masked_grid, block_rows;       // workgroups that look for attn_block_kernel's units with masks; rows of such a unit
     int parts;         // prefix_splits + own_splits
     bool around;       // own keys past the caches
+    bool direct;       // one part, attn_range's: it is the result, and no join follows
     FastDiv page;
     float scale, scale2;  // scale2: scale * log2(e)
 };
@@ -466,7 +467,7 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
         if (r >= n_rows) continue;
         const AttnRow x = attn_row(a, h, r, own_b);
         const int64_t row = ((int64_t)x.b * a.tokens + x.t) * a.heads + x.head;
-        if (a.parts == 1) {  // nothing to join
+        if (a.direct) {  // nothing to join
             if (g == 0 && a.lse) a.lse[row] = row_lse<ELT>(a, m[rt], total[rt]);
             const float f = total[rt] == 0.0f ? 0.0f : 1.0f / total[rt];
             char *out = (char *)a.out + (x.b * a.os[0] + x.t * a.os[1] + x.head * a.os[2]) * E::kBytes;
