@@ -116,8 +116,8 @@ int64_t atk_pages_work_bytes(int64_t n_pages);
 int atk_copy_pages(const void *const *src_pools, void *const *dst_pools, int64_t n_pools, int64_t page_bytes, int64_t src_pages,
                    int64_t dst_pages, const int32_t *src_ids, const int32_t *dst_ids, int64_t n, int32_t *status, void *stream);
 
-/* Makes row children[i], empty before, a copy of row parents[i]: whole pages are shared, a last page that is filled in part is
- * copied (its filled tokens) to a fresh one.  children are distinct.  All or nothing. */
+/* Makes row children[i], empty before, a copy of row parents[i] as it is at the call (a parent that is a child of the same call is empty):
+ * whole pages are shared, a last page that is filled in part is copied (its filled tokens) to a fresh one.  children are distinct.  All or nothing. */
 int atk_fork_sequences(const atk_page_tables *t, void *const *pools, int64_t n_pools, int64_t token_bytes, const int32_t *parents,
                        const int32_t *children, int64_t n, void *stream);
 

@@ -112,9 +112,9 @@ class Pages:
         if sum(self.lens[p] % self.ps > 0 for p in parents) > len(self.free):
             self.status |= 1
             return
-        for p, c in zip(parents, children):
-            n = self.lens[p]
-            row = self.table[p][:self._held(n)]
+        before = [(self.lens[p], self.table[p][:self._held(self.lens[p])]) for p in parents]   # (a parent may be a child of the same call)
+        for (n, row), c in zip(before, children):
+            row = list(row)
             part = n % self.ps
             for page in row[:-1] if part else row:
                 self.refs[page] += 1

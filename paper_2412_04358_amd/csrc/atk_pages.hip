@@ -300,7 +300,15 @@ __global__ __launch_bounds__(kThreads) void pages_fork_kernel(const PagesDev t, 
         if (threadIdx.x == 0) t.tell(need.bad);
         return;
     }
-    for (int64_t j = threadIdx.x; j < n; j += kThreads) t.lens[children[j]] = t.lens[parents[j]];
+    // Lengths as they were at the call, also where a parent is a child of another pair: children were empty, so a parent's length that is a new one by now - which are
+    // stored as their complements until all have been read - was 0.
+    for (int64_t j = threadIdx.x; j < n; j += kThreads) t.lens[children[j]] = ~max(0, t.lens[parents[j]]);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    for (int64_t j = threadIdx.x; j < n; j += kThreads) {
+        const int len = t.lens[children[j]];
+        if (len < 0) t.lens[children[j]] = ~len;
+    }
     if (threadIdx.x == 0) *t.n_free -= need.total;
 }
 

@@ -361,8 +361,8 @@ def _seqs(tables, t, n, what):
 
 
 def fork_sequences(tables, pools, parents, children):
-    """Makes row children[i] of the tables, empty until now, a copy of row parents[i]: whole pages are shared, a last page that is
-    filled in part is copied, in all pools.  parents and children: int32 (n,), children distinct.  All or nothing: with too few
+    """Makes row children[i] of the tables, empty until now, a copy of row parents[i] as it is at the call (so a child of the same call
+    is an empty parent): whole pages are shared, a last page that is filled in part is copied, in all pools.  parents and children: int32 (n,), children distinct.  All or nothing: with too few
     free pages, or a child that holds something, nothing changes and tables.status says so."""
     if _fast("fork", tables._address, tables._device, pools, parents, children) is not None:
         return
