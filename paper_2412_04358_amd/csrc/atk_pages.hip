@@ -245,7 +245,7 @@ __device__ __forceinline__ ForkNeed fork_need(const PagesDev &t, const int32_t *
             continue;
         }
         const int len = t.lens[p];
-        if (len < 0 || t.pages(len) > t.row_pages) bad |= ATK_STATUS_BAD_LEN;
+        if (len < 0 || len > t.row_pages * t.page.d) bad |= ATK_STATUS_BAD_LEN;  // (before any quotient: those are of 31 bits)
         else if (t.page.mod(len)) ++total, before += i < mine;
         if (t.lens[c] != 0) bad |= ATK_STATUS_BAD_SEQ;
     }
