@@ -123,7 +123,7 @@ int atk_fork_sequences(const atk_page_tables *t, void *const *pools, int64_t n_p
 
 /* Adds `tokens` tokens to each of the distinct rows seqs[i]: takes fresh pages, copies a part-filled last page that other rows
  * hold too, and stores values[p] (n, tokens, token_bytes; value_strides[p] bytes between sequences) into pool p.  Rows that all hold
- * one part-filled page at the call each get a copy of it.  All or nothing. */
+ * one part-filled page at the call each get a copy of it.  All or nothing.  n * (ceil(tokens / page_size) + 1) is below 2^31. */
 int atk_append_tokens(const atk_page_tables *t, void *const *pools, const void *const *values, const int64_t *value_strides,
                       int64_t n_pools, int64_t token_bytes, const int32_t *seqs, int64_t n, int64_t tokens, void *stream);
 

@@ -688,6 +688,8 @@ int atk_append_tokens(const atk_page_tables *t, void *const *pools, const void *
     if (rc != ATK_OK) return rc;
     if (n < 0 || n > t->rows || tokens < 0 || tokens > (1 << 30)) return ATK_ERR_ARGS;
     if (n == 0 || tokens == 0) return ATK_OK;
+    // pages that the call could take, which its workgroups count in 31 bits (and no cache has: 2^28 at most)
+    if (n * ((tokens + t->page_size - 1) / t->page_size + 1) > INT32_MAX) return ATK_ERR_ARGS;
     if (!seqs || (n_pools > 0 && !value_strides)) return ATK_ERR_NULL_PTR;
     if ((uintptr_t)seqs & 3) return ATK_ERR_ALIGN;
     for (int64_t i = 0; i < n_pools; ++i) {
