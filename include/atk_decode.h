@@ -8,6 +8,9 @@
  * captured into a graph.  What only the device sees - page numbers, sequence numbers, lengths - is checked by the
  * kernels: a bad one is never used as an address, and is reported by a bit of *status (device, one int32, only ever
  * or-ed to, may be NULL).
+ *
+ * Sizes whose launches would have 2^32 threads and more are ATK_ERR_ARGS: batch * tokens * heads from 2^26 on, 2^24 sequences of a call on
+ * pages, 2^22 requests of up to 128 KB of probabilities each.
  */
 #ifndef ATK_DECODE_H
 #define ATK_DECODE_H

@@ -187,13 +187,14 @@ static int plan_attention(const atk_attention_args *p, AttnPlan *pl) {
         pl->prefix_blocks = (int)attn_ceil(rows, 16 * pl->rt);
         if (shared) split_prefix(p, pl, step, std::max<int64_t>(1, 2 * kNumCU / (pl->prefix_blocks * p->kv_heads)));
     }
-    const int64_t base = pl->prefix_blocks * p->kv_heads;
     pl->rows = p->batch * p->tokens * p->heads;
     pl->parts = pl->prefix_splits + pl->own_splits;
     pl->o_bytes = pl->rows * pl->parts * p->dim * 4;
     pl->bytes = pl->o_bytes + pl->rows * pl->parts * 8;
-    const int64_t most = INT64_C(1) << 30;  // workgroups
-    return base * std::max(1, pl->prefix_splits) < most && own_base * std::max(1, pl->own_splits) < most ? ATK_OK : ATK_ERR_ARGS;
+    // launch_attn_dp's launches, and the join's
+    const int64_t shared_groups = (pl->prefix_blocks * p->kv_heads * pl->prefix_splits + 7) / 8 * 8, own_groups = (own_base * pl->own_splits + 7) / 8 * 8;
+    const bool fit = launches(shared_groups, 64 * pl->waves) && launches((pl->rt == kMixed ? 2 : 1) * shared_groups + own_groups, 64 * kAttnWaves) && launches(attn_ceil(pl->rows, 4), 256);
+    return fit ? ATK_OK : ATK_ERR_ARGS;
 }
 
 }  // namespace atk

@@ -23,6 +23,9 @@ struct FastDiv {
 #endif
 };
 
+// A launch has fewer than 2^32 threads; past that HIP refuses it.
+constexpr bool launches(int64_t workgroups, int threads) { return workgroups < (INT64_C(1) << 32) / threads; }
+
 int set_hip_error(hipError_t e);  // ATK_ERR_HIP, with e for atk_last_hip_error()
 
 }  // namespace atk

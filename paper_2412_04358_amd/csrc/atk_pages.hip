@@ -660,7 +660,7 @@ int atk_fork_sequences(const atk_page_tables *t, void *const *pools, int64_t n_p
     uintptr_t bits = (uintptr_t)token_bytes;
     if (rc == ATK_OK) rc = check_pools(pools, n_pools, token_bytes, &bits);
     if (rc != ATK_OK) return rc;
-    if (n < 0 || n > t->rows) return ATK_ERR_ARGS;
+    if (n < 0 || n > t->rows || !launches(n, kThreads)) return ATK_ERR_ARGS;
     if (n == 0) return ATK_OK;
     if (!parents || !children) return ATK_ERR_NULL_PTR;
     if (((uintptr_t)parents | (uintptr_t)children) & 3) return ATK_ERR_ALIGN;
@@ -686,7 +686,7 @@ int atk_append_tokens(const atk_page_tables *t, void *const *pools, const void *
     if (rc == ATK_OK) rc = check_pools(pools, n_pools, token_bytes, &bits);
     if (rc == ATK_OK && n * tokens > 0) rc = check_pools(values, n_pools, token_bytes, &bits);
     if (rc != ATK_OK) return rc;
-    if (n < 0 || n > t->rows || tokens < 0 || tokens > (1 << 30)) return ATK_ERR_ARGS;
+    if (n < 0 || n > t->rows || !launches(n, kThreads) || tokens < 0 || tokens > (1 << 30)) return ATK_ERR_ARGS;
     if (n == 0 || tokens == 0) return ATK_OK;
     // pages that the call could take, which its workgroups count in 31 bits (and no cache has: 2^28 at most)
     if (n * ((tokens + t->page_size - 1) / t->page_size + 1) > INT32_MAX) return ATK_ERR_ARGS;
@@ -714,7 +714,7 @@ int atk_append_tokens(const atk_page_tables *t, void *const *pools, const void *
 int atk_free_sequences(const atk_page_tables *t, const int32_t *seqs, const int32_t *drop, int64_t n, void *stream) {
     int rc = check_tables(t);
     if (rc != ATK_OK) return rc;
-    if (n < 0 || n > t->rows) return ATK_ERR_ARGS;
+    if (n < 0 || n > t->rows || !launches(n, kThreads)) return ATK_ERR_ARGS;
     if (n == 0) return ATK_OK;
     if (!seqs) return ATK_ERR_NULL_PTR;
     if (((uintptr_t)seqs | (uintptr_t)drop) & 3) return ATK_ERR_ALIGN;

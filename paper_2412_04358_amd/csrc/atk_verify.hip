@@ -371,6 +371,7 @@ static int64_t verify_groups(int64_t batch, int64_t vocab) {
 // Rows of up to 128 KB by one workgroup each: 9.1 us -> 6.9 for one request of 4000 f32, 13.1 -> 11.2 for 64 of 32000, 16.0 -> 11.3 for 128 of 32000 bf16; one of 128256 bf16 would
 // take 16 us so and takes 8.4 in two launches, 64 of them 25 and 20.
 static bool verify_by_row(int64_t vocab, int elt) { return vocab * (elt == ATK_F32 ? 4 : 2) <= (128 << 10); }
+static bool verify_fits(int64_t batch, int64_t vocab, int elt) { return verify_by_row(vocab, elt) ? launches(batch, kRowWaves * 64) : launches(batch * verify_groups(batch, vocab), 256); }
 static_assert((128 << 10) / 2 <= kRowWaves * kRowChunks * kChunk, "a sixteenth's chunks have their places");
 
 template <int ELT>
@@ -394,7 +395,7 @@ extern "C" {
 
 int64_t atk_verify_workspace_bytes(int64_t batch, int64_t drafts, int64_t vocab) {
     if (batch < 1 || batch > (1 << 24) || drafts < 0 || drafts > (1 << 20) || vocab < 1 || vocab >= (INT64_C(1) << 30)) return ATK_ERR_ARGS;
-    if (batch * verify_groups(batch, vocab) >= (INT64_C(1) << 31)) return ATK_ERR_ARGS;  // workgroups
+    if (!verify_fits(batch, vocab, ATK_F32) && !verify_fits(batch, vocab, ATK_BF16)) return ATK_ERR_ARGS;
     return batch * verify_tiles(vocab) * (int64_t)sizeof(double2);
 }
 
@@ -404,6 +405,7 @@ int atk_verify_drafts(const void *target_probs, const int64_t target_stride[2], 
     const int64_t need = atk_verify_workspace_bytes(batch, drafts, vocab);
     if (need < 0) return (int)need;
     if (dtype != ATK_F32 && dtype != ATK_BF16 && dtype != ATK_F16) return ATK_ERR_DTYPE;
+    if (!verify_fits(batch, vocab, dtype)) return ATK_ERR_ARGS;
     if (!target_probs || !target_stride || (draft_probs && !draft_stride) || !final_random || !accepted || !tokens || !work) return ATK_ERR_NULL_PTR;
     if (drafts > 0 && (!draft_tokens || !accept_random)) return ATK_ERR_NULL_PTR;
     const int es = dtype == ATK_F32 ? 4 : 2;

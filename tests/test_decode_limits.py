@@ -33,3 +33,54 @@ def test_append_of_more_pages_than_are_counted(lib, n, tokens, page_size):
     one, stride = (ctypes.c_void_p * 1)(FAKE), (ctypes.c_int64 * 1)(0)
     t = _tables(page_size=page_size, row_pages=(1 << 30) // page_size if tokens >> 20 else 1 << 16)
     assert lib.atk_append_tokens(t, one, one, stride, 1, 256, FAKE, n, tokens, None) == ARGS
+
+
+def _attention(**kw):
+    i3 = ctypes.c_int64 * 3
+    a = dict(q=FAKE, k=FAKE, v=FAKE, out=FAKE, page_table=FAKE, lens=FAKE, batch=1, tokens=1, heads=64, kv_heads=64, dim=64, page_size=16, n_pages=100, rows=1 << 26, row_pages=20,
+             table_stride=20, prefix_len=0, scale=0.125, dtype=1)
+    a.update(kw)
+    H, D = a["heads"], a["dim"]
+    for n in ("q_stride", "out_stride"):
+        a[n] = i3(a["tokens"] * H * D, H * D, D)
+    for n in ("k_stride", "v_stride"):
+        a[n] = i3(16 * a["kv_heads"] * D, a["kv_heads"] * D, D)
+    return decode._AttentionArgs(**a)
+
+
+@pytest.mark.parametrize("kw,fits", [
+    (dict(batch=1 << 18), False), (dict(batch=(1 << 18) - 1), True),                # one workgroup a sequence and head, 2^24 of them
+    (dict(batch=1 << 20, kv_heads=1), False), (dict(batch=1 << 19, kv_heads=1, tokens=2), False), (dict(batch=(1 << 20) - 1, kv_heads=1), True),      # 2^26 rows to join
+    (dict(batch=1, tokens=1 << 20, kv_heads=8, row_pages=1 << 17, table_stride=1 << 17), False), (dict(batch=1, tokens=(1 << 20) - 1, kv_heads=8, row_pages=1 << 17, table_stride=1 << 17), True),
+    (dict(batch=1 << 20, kv_heads=64, heads=64, prefix_len=320, dtype=0), False),
+])
+def test_attention_of_more_rows_than_a_launch_takes(lib, kw, fits):
+    need = lib.atk_attention_workspace_bytes(_attention(**kw))
+    assert need > 0 if fits else need == ARGS
+    if not fits:
+        assert lib.atk_shared_prefix_attention(_attention(**kw), FAKE, 1 << 60, None) == ARGS
+
+
+@pytest.mark.parametrize("batch,vocab,dtype,fits", [(1 << 22, 8, 0, False), ((1 << 22) - 1, 8, 0, True), (1 << 22, 65536, 1, False), (1 << 22, 65536, 0, False), (1 << 20, 32769, 0, True),
+                                                    (1 << 20, 128256, 1, False), (1 << 24, 4, 1, False)])
+def test_verification_of_more_requests_than_a_launch_takes(lib, batch, vocab, dtype, fits):
+    s = (ctypes.c_int64 * 2)(0, 0)
+
+    def call(work_bytes):
+        return lib.atk_verify_drafts(FAKE, s, FAKE, s, FAKE, FAKE, FAKE, None, batch, 1, vocab, dtype, FAKE, FAKE, FAKE, work_bytes, None)
+
+    # (one that fits is refused for its workspace, behind the sizes)
+    assert call(0) == (-8 if fits else ARGS)
+    if fits:
+        assert lib.atk_verify_workspace_bytes(batch, 1, vocab) > 0
+
+
+def test_pages_of_more_sequences_than_a_launch_takes(lib):
+    one, stride = (ctypes.c_void_p * 1)(FAKE), (ctypes.c_int64 * 1)(0)
+    t = _tables(rows=1 << 25, row_pages=2, page_size=16)
+    for n in (1 << 24, 1 << 25):
+        assert lib.atk_fork_sequences(t, one, 1, 256, FAKE, FAKE, n, None) == ARGS
+        assert lib.atk_append_tokens(t, one, one, stride, 1, 256, FAKE, n, 1, None) == ARGS
+        assert lib.atk_free_sequences(t, FAKE, None, n, None) == ARGS
+    # (one less is refused for its addresses only)
+    assert lib.atk_free_sequences(t, FAKE + 2, None, (1 << 24) - 1, None) == -7
