@@ -566,7 +566,7 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
     const int r = r0 + wave * 32 + n;
     const bool real = r < n_rows;
     const AttnRow x = attn_row(a, h, real ? r : 0, -1);
-    bool bad = false;
+    bool bad = false;  // (told by attn_rest)
     const int sees = seq_len(a, seq_row(a, x.b, &bad), &bad) - (a.tokens - 1 - x.t);
 
     // What comes in.  Four keys that begin at a multiple of four lie in one page (page_size % 4 == 0, and so ka): a load has the address of its four keys, a scalar that a
@@ -896,12 +896,13 @@ __device__ __forceinline__ void attn_rest(const AttnDev &a, int id, char *lds) {
     if (u < 0) return;
     const SharedUnit s(a, u);
     const int r0 = s.block * a.block_rows;
-    bool all = s.ka < s.kb;
+    bool all = s.ka < s.kb, bad_len = false;
     for (int r = r0 + threadIdx.x; r < min(n_rows, r0 + a.block_rows); r += kAttnWaves * 64) {
         const AttnRow x = attn_row(a, s.h, r, -1);
-        bool bad = false;
-        if (seq_len(a, seq_row(a, x.b, &bad), &bad) - (a.tokens - 1 - x.t) < s.kb) all = false;
+        bool bad_seq = false;  // (sees nothing: attn_range tells)
+        if (seq_len(a, seq_row(a, x.b, &bad_seq), &bad_len) - (a.tokens - 1 - x.t) < s.kb) all = false;
     }
+    if (bad_len && a.status) atomicOr(a.status, ATK_STATUS_BAD_LEN);
     if (__syncthreads_and(all)) return;
     for (int r = r0; r < min(n_rows, r0 + a.block_rows); r += 16) {
         attn_range<ELT, DP, 1, kAttnWaves>(a, s.h, r, n_rows, -1, a.table + s.row * a.table_stride, s.ka, s.kb, s.split, lds);
