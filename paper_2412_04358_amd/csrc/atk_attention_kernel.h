@@ -544,7 +544,8 @@ struct BlockLds {
     static constexpr int kBytes = kData + 2 * kRing * 16 * 4;
 };
 
-// Rows r0 .. r0 + 32 * NW - 1 of head h against keys ka .. kb - 1 (one at least), all of which every one of these rows has to see: nothing is written if one does not.
+// Rows r0 .. r0 + 32 * NW - 1 of head h against keys ka .. kb - 1 (one at least), all of which every one of these rows has to see: nothing is written if one does not, or if a
+// key's page is none (attn_rest then does the rows, with masks).
 // FULL: dim == DP.
 template <int ELT, int DP, int NW, bool FULL>
 __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int n_rows, const int32_t *table_row, int ka, int kb, int part, char *lds) {
@@ -821,7 +822,7 @@ __device__ __forceinline__ void attn_block(const AttnDev &a, int h, int r0, int 
     barrier();
     products(Yes{}, No{}, tiles - 1);
     if (!late && NW == 8) barrier();
-    if (bad_page && a.status) atomicOr(a.status, ATK_STATUS_BAD_PAGE);
+    if (__syncthreads_or(bad_page)) return;
     l += __shfl_xor(l, 32, 64);
     if (!real) return;
     const int64_t row = ((int64_t)x.b * a.tokens + x.t) * a.heads + x.head;
@@ -884,8 +885,8 @@ struct SharedUnit {
     }
 };
 
-// Of attn_block_kernel's units (the first masked_grid workgroups), those with a row that sees only a part of the keys - a sequence that ends before them: tile by tile, with masks.  Then
-// own keys.
+// Of attn_block_kernel's units (the first masked_grid workgroups), those with a row that sees only a part of the keys - a sequence that ends before them, a page that is none: tile by
+// tile, with masks.  Then own keys.
 template <int ELT, int DP, bool AROUND>
 __device__ __forceinline__ void attn_rest(const AttnDev &a, int id, char *lds) {
     if (id >= a.masked_grid) {
@@ -903,9 +904,13 @@ __device__ __forceinline__ void attn_rest(const AttnDev &a, int id, char *lds) {
         if (seq_len(a, seq_row(a, x.b, &bad_seq), &bad_len) - (a.tokens - 1 - x.t) < s.kb) all = false;
     }
     if (bad_len && a.status) atomicOr(a.status, ATK_STATUS_BAD_LEN);
+    const int32_t *table_row = a.table + s.row * a.table_stride;
+    if (s.ka < s.kb)
+        for (int j = a.page.div(s.ka) + threadIdx.x, to = a.page.div(s.kb - 1); j <= to; j += kAttnWaves * 64)
+            if ((unsigned)table_row[j] >= (unsigned)a.n_pages) all = false;
     if (__syncthreads_and(all)) return;
     for (int r = r0; r < min(n_rows, r0 + a.block_rows); r += 16) {
-        attn_range<ELT, DP, 1, kAttnWaves>(a, s.h, r, n_rows, -1, a.table + s.row * a.table_stride, s.ka, s.kb, s.split, lds);
+        attn_range<ELT, DP, 1, kAttnWaves>(a, s.h, r, n_rows, -1, table_row, s.ka, s.kb, s.split, lds);
         __syncthreads();
     }
 }
