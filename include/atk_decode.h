@@ -44,7 +44,7 @@ enum {
  *   j < lens[s] - (tokens - 1 - t).  Keys j < prefix_len are read through the row of the first sequence of the call, once
  *   for all of them: the caller sees to it that the others hold the same there.
  *   out = sum_j softmax_j(scale * q.k_j) * v_j over the visible keys, lse = log sum_j exp(scale * q.k_j); a query that sees
- *   no key, or whose scores are all -inf, gets 0 and -inf.  What is not visible has no influence, NaN and infinities included.  Nor is a key
+ *   no key, or whose scores are all -inf, gets 0 and -inf.  (Beside others a visible key with a score of -inf weighs 0, and 0 times NaN or infinity is NaN.)  What is not visible has no influence, NaN and infinities included.  Nor is a key
  *   whose page is outside the cache visible, nor any of a sequence whose row number is outside the table; a length past the row's pages counts as all of them.
  *
  *   q, out     (batch, tokens, heads, dim) of `dtype`, dim contiguous, strides in elements for the first three.

@@ -36,7 +36,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const AttnDev a) {
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                if (p0 + j * kStep >= a.parts || x[j].y == 0.0f) continue;  // (no visible key in it: nothing was written)
+                if (p0 + j * kStep >= a.parts) continue;
                 const float f = x[j].x == kNoMax ? 1.0f : __builtin_amdgcn_exp2f((x[j].x - m) * a.scale2);
                 o += f * v[j];
             }
@@ -49,6 +49,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const AttnDev a) {
     const int head = (int)(row % a.heads);
     const int64_t bt = row / a.heads;
     const int64_t b = bt / a.tokens, t = bt % a.tokens;
+    if (l == 0.0f) o = f32x4{0, 0, 0, 0};  // no key, or scores of -inf alone, whose values do not count even if they are NaN
     const float f = l == 0.0f ? 0.0f : 1.0f / l;
     if (lane < LPR && d < a.dim) {
         store_out<ELT>((char *)a.out + (b * a.os[0] + t * a.os[1] + head * a.os[2] + d) * AttnElt<ELT>::kBytes, o * f);

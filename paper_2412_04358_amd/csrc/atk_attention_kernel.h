@@ -469,14 +469,17 @@ __device__ __forceinline__ void attn_range(const AttnDev &a, int h, int r0, int 
         const int64_t row = ((int64_t)x.b * a.tokens + x.t) * a.heads + x.head;
         if (a.direct) {  // nothing to join
             if (g == 0 && a.lse) a.lse[row] = row_lse<ELT>(a, m[rt], total[rt]);
-            const float f = total[rt] == 0.0f ? 0.0f : 1.0f / total[rt];
+            const float f = 1.0f / total[rt];
+            const bool none = total[rt] == 0.0f;  // no key, or scores of -inf alone, whose values do not count even if they are NaN
             char *out = (char *)a.out + (x.b * a.os[0] + x.t * a.os[1] + x.head * a.os[2]) * E::kBytes;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int i = 0; i < NT; i += 4) {
                     const int d = (g * 4 + j) * NT + i;
-                    if (d < a.dim) store_out<ELT>(out + d * E::kBytes, f32x4{acc[rt][i][j] * f, acc[rt][i + 1][j] * f, acc[rt][i + 2][j] * f, acc[rt][i + 3][j] * f});
+                    f32x4 o = f32x4{acc[rt][i][j] * f, acc[rt][i + 1][j] * f, acc[rt][i + 2][j] * f, acc[rt][i + 3][j] * f};
+                    if (none) o = f32x4{0, 0, 0, 0};
+                    if (d < a.dim) store_out<ELT>(out + d * E::kBytes, o);
                 }
             continue;
         }
