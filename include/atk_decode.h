@@ -67,7 +67,7 @@ typedef struct {
     int64_t prefix_len;
     int64_t q_stride[3], out_stride[3];    /* sequence, token, head */
     int64_t k_stride[3], v_stride[3];      /* page, token, head */
-    double scale;                          /* > 0 */
+    double scale;                          /* FLT_MIN to 1e30 */
     int32_t dtype;
 } atk_attention_args;
 int64_t atk_attention_workspace_bytes(const atk_attention_args *args);

@@ -1,4 +1,6 @@
 // shared_prefix_attention: checks, launch plan, and the kernel that joins the ranges of keys (see atk_attention_kernel.h).
+#include <cfloat>
+
 #include "atk_attention_kernel.h"
 
 namespace atk {
@@ -97,7 +99,7 @@ static int check_attention(const atk_attention_args *p, bool pointers) {
     if (p->row_pages * p->page_size > most || p->prefix_len < 0 || p->prefix_len > p->row_pages * p->page_size) return ATK_ERR_ARGS;
     if (!p->seqs && p->batch > p->rows) return ATK_ERR_ARGS;
     if (p->table_stride < p->row_pages) return ATK_ERR_ARGS;
-    if (!(p->scale > 0) || p->scale > 1e30) return ATK_ERR_ARGS;
+    if (!(p->scale >= FLT_MIN) || p->scale > 1e30) return ATK_ERR_ARGS;  // (the kernels have it in f32, where less is 0 or nearly so, and 0 * inf no number)
     if (p->dim > 256 || p->dim % piece) return ATK_ERR_UNSUPPORTED;
     for (int i = 0; i < 3; ++i) {
         if (p->q_stride[i] < 0 || p->out_stride[i] < 0 || p->k_stride[i] < 0 || p->v_stride[i] < 0) return ATK_ERR_ARGS;

@@ -84,3 +84,11 @@ def test_pages_of_more_sequences_than_a_launch_takes(lib):
         assert lib.atk_free_sequences(t, FAKE, None, n, None) == ARGS
     # (one less is refused for its addresses only)
     assert lib.atk_free_sequences(t, FAKE + 2, None, (1 << 24) - 1, None) == -7
+
+
+@pytest.mark.parametrize("scale,fits", [(5e-46, False), (1e-60, False), (5e-324, False), (1e-40, False), (1.1754e-38, False), (1.18e-38, True), (1e-6, True), (1e30, True), (1.1e30, False)])
+def test_scales_that_f32_does_not_hold(lib, scale, fits):
+    a = _attention(batch=4, scale=scale)
+    assert (lib.atk_attention_workspace_bytes(a) > 0) is fits
+    if not fits:
+        assert lib.atk_attention_workspace_bytes(a) == ARGS and lib.atk_shared_prefix_attention(a, FAKE, 1 << 40, None) == ARGS
