@@ -524,12 +524,12 @@ __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c) {
 }
 
 // 16 bytes of each lane from base + off to LDS at `lds` + 16 * lane.  (Nothing but vmcnt waits for it, and no wait that the compiler inserts, which by the builtin are for all of them
-// in front of every read from LDS.)
+// in front of every read from LDS.  m0 holds the place; as an operand it is the compiler's, which keeps track of it.)
 __device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(lds), "v"(off), "s"(base) : "memory");
 }
 __device__ __forceinline__ void load_to_lds(const char *address, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(address) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(lds), "v"(address) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void wait_loads() {  // until all but the last N are there
