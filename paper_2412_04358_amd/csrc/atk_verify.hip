@@ -287,7 +287,9 @@ __global__ __launch_bounds__(64) void verify_draw_kernel(const VerifyDev a) {
 }
 
 // The whole request by one workgroup: its wavefronts have a sixteenth of the row each, then a chunk of the sixteenth that the goal lies in, then one has the chunk.
-constexpr int kRowWaves = 16, kRowChunks = 256;   // chunks of a sixteenth at most
+constexpr int kRowBytes = 128 << 10;  // of a row at most
+constexpr int kRowWaves = 16, kRowChunks = kRowBytes / 2 / (kRowWaves * kChunk);  // chunks of a sixteenth at most: eight, four in f32
+static_assert(kRowChunks * kRowWaves * kChunk * 2 == kRowBytes && kRowChunks <= kRowWaves, "a wavefront for each chunk of a sixteenth");
 template <int ELT>
 __global__ __launch_bounds__(kRowWaves * 64) void verify_row_kernel(const VerifyDev a) {
     __shared__ double2 wave_sums[kRowWaves];
@@ -333,28 +335,21 @@ __global__ __launch_bounds__(kRowWaves * 64) void verify_row_kernel(const Verify
     const int pick = got >= 0 ? got : last;
     int token = -1;
     if (pick >= 0) {
-        const double start = __shfl(before, pick, 64);
-        for (int c = wave; c < chunks; c += kRowWaves) {
+        run = __shfl(before, pick, 64);
+        if (wave < chunks) {
             double w[kEach], t[kEach], sum = 0;
-            weights8<ELT>(row, ((int64_t)pick * chunks + c) * kChunk + lane * kEach, a.vocab, w, t);
+            weights8<ELT>(row, ((int64_t)pick * chunks + wave) * kChunk + lane * kEach, a.vocab, w, t);
 #pragma unroll
             for (int e = 0; e < kEach; ++e) sum += of_target ? t[e] : w[e];
             sum = wave_sum(sum);
-            if (lane == 0) chunk_sums[c] = sum;
+            if (lane == 0) chunk_sums[wave] = sum;
         }
         __syncthreads();
         if (wave != 0) return;
-        run = start;
-        int which = -1;
-        double from = start;
-        for (int c0 = 0; c0 < chunks; c0 += 64) {
-            last = -1;
-            const int found = find64(c0 + lane < chunks ? chunk_sums[c0 + lane] : 0.0, goal, &run, &last, &before);
-            const int who = found >= 0 ? found : last;
-            if (who >= 0) which = c0 + who, from = __shfl(before, who, 64);
-            if (found >= 0) break;
-        }
-        if (which >= 0) token = find_element<ELT>(row, ((int64_t)pick * chunks + which) * kChunk, a.vocab, of_target, goal, from);
+        last = -1;
+        const int found = find64(lane < chunks ? chunk_sums[lane] : 0.0, goal, &run, &last, &before);
+        const int which = found >= 0 ? found : last;
+        if (which >= 0) token = find_element<ELT>(row, ((int64_t)pick * chunks + which) * kChunk, a.vocab, of_target, goal, __shfl(before, which, 64));
     }
     if (wave != 0) return;
     write_tokens<ELT>(a, b, row.accepted, token);
@@ -370,9 +365,8 @@ static int64_t verify_groups(int64_t batch, int64_t vocab) {
 
 // Rows of up to 128 KB by one workgroup each: 9.1 us -> 6.9 for one request of 4000 f32, 13.1 -> 11.2 for 64 of 32000, 16.0 -> 11.3 for 128 of 32000 bf16; one of 128256 bf16 would
 // take 16 us so and takes 8.4 in two launches, 64 of them 25 and 20.
-static bool verify_by_row(int64_t vocab, int elt) { return vocab * (elt == ATK_F32 ? 4 : 2) <= (128 << 10); }
+static bool verify_by_row(int64_t vocab, int elt) { return vocab * (elt == ATK_F32 ? 4 : 2) <= kRowBytes; }
 static bool verify_fits(int64_t batch, int64_t vocab, int elt) { return verify_by_row(vocab, elt) ? launches(batch, kRowWaves * 64) : launches(batch * verify_groups(batch, vocab), 256); }
-static_assert((128 << 10) / 2 <= kRowWaves * kRowChunks * kChunk, "a sixteenth's chunks have their places");
 
 template <int ELT>
 static hipError_t launch_verify(const VerifyDev &a, int64_t batch, hipStream_t s) {
