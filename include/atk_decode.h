@@ -51,7 +51,7 @@ enum {
  *   k, v       (n_pages, page_size, kv_heads, dim) of `dtype`, dim contiguous, strides in elements for the first three: token
  *              by token or head by head in a page.  heads is a multiple of kv_heads, query head h reads head h / (heads / kv_heads).
  *   lse        (batch, tokens, heads) f32, contiguous, or NULL.
- *   dim        a multiple of 16 bytes / element size, up to 256.  Pointers of q, k, v, out on 16 bytes, strides of whole 16 bytes.
+ *   dim        a multiple of 16 bytes / element size, up to 256.  Pointers of q, k, v, out on 16 bytes, strides (but a single one's) of whole 16 bytes.
  *   work       atk_attention_workspace_bytes() bytes on 16 bytes.
  * Scores, statistics and accumulators are f32; the weights are rounded to `dtype` for the product with v.
  */

@@ -101,9 +101,11 @@ static int check_attention(const atk_attention_args *p, bool pointers) {
     if (p->table_stride < p->row_pages) return ATK_ERR_ARGS;
     if (!(p->scale >= FLT_MIN) || p->scale > 1e30) return ATK_ERR_ARGS;  // (the kernels have it in f32, where less is 0 or nearly so, and 0 * inf no number)
     if (p->dim > 256 || p->dim % piece) return ATK_ERR_UNSUPPORTED;
+    const int64_t rows[3] = {p->batch, p->tokens, p->heads}, keys[3] = {p->n_pages, p->page_size, p->kv_heads};
     for (int i = 0; i < 3; ++i) {
         if (p->q_stride[i] < 0 || p->out_stride[i] < 0 || p->k_stride[i] < 0 || p->v_stride[i] < 0) return ATK_ERR_ARGS;
-        if (p->q_stride[i] % piece || p->out_stride[i] % piece || p->k_stride[i] % piece || p->v_stride[i] % piece) return ATK_ERR_ALIGN;
+        if (rows[i] > 1 && (p->q_stride[i] % piece || p->out_stride[i] % piece)) return ATK_ERR_ALIGN;
+        if (keys[i] > 1 && (p->k_stride[i] % piece || p->v_stride[i] % piece)) return ATK_ERR_ALIGN;
     }
     if (pointers) {
         if (!p->q || !p->k || !p->v || !p->out || !p->page_table || !p->lens) return ATK_ERR_NULL_PTR;

@@ -92,3 +92,18 @@ def test_scales_that_f32_does_not_hold(lib, scale, fits):
     assert (lib.atk_attention_workspace_bytes(a) > 0) is fits
     if not fits:
         assert lib.atk_attention_workspace_bytes(a) == ARGS and lib.atk_shared_prefix_attention(a, FAKE, 1 << 40, None) == ARGS
+
+
+def test_strides_of_single_elements_are_not_used(lib):
+    i3 = ctypes.c_int64 * 3
+    odd = dict(batch=1, tokens=1, heads=1, kv_heads=1, n_pages=1, page_size=1, rows=1, prefix_len=0)
+    for name in ("q_stride", "out_stride", "k_stride", "v_stride"):
+        for many, size in enumerate((("batch", "tokens", "heads") if name[0] in "qo" else ("n_pages", "page_size", "kv_heads"))):
+            a = _attention(**odd)
+            setattr(a, name, i3(*[65 if i == many else 64 for i in range(3)]))
+            assert lib.atk_attention_workspace_bytes(a) > 0, (name, size)
+            setattr(a, size, 2)
+            a.heads, a.rows = 2 if size in ("heads", "kv_heads") else 1, 2
+            if size != "heads":
+                a.q_stride = i3(64, 64, 64) if name != "q_stride" else a.q_stride
+            assert lib.atk_attention_workspace_bytes(a) == -7, (name, size)
