@@ -14,12 +14,12 @@ def test_one_sequence_out_of_rows_of_odd_width(dtype):
     q = torch.randn((1, 3, 4, 64), generator=g, device="cuda").to(dtype)
     table, lens = torch.arange(8, dtype=torch.int32, device="cuda").reshape(1, 8), torch.tensor([100], dtype=torch.int32, device="cuda")
     wide = torch.zeros((2, 3 * 4 * 64 + 3), dtype=dtype, device="cuda")
-    odd = wide[:1, :3 * 4 * 64].view(1, 3, 4, 64)
+    odd = torch.as_strided(wide, (2, 3, 4, 64), (3 * 4 * 64 + 3, 256, 64, 1))[:1]
     odd.copy_(q)
     assert odd.stride(0) % 2
     pages = torch.as_strided(k, (1, 16, 2, 64), (7, 128, 64, 1))
     one = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
-    for out in (None, torch.zeros_like(wide)[:1, :3 * 4 * 64].view(1, 3, 4, 64)):
+    for out in (None, torch.as_strided(torch.zeros_like(wide), (2, 3, 4, 64), (3 * 4 * 64 + 3, 256, 64, 1))[:1]):
         assert torch.equal(atk.shared_prefix_attention(odd, k, v, table, lens, 40, out=out), atk.shared_prefix_attention(q, k, v, table, lens, 40))
         lens[0] = 16
         assert torch.equal(atk.shared_prefix_attention(odd, pages, pages, one, lens, 0, out=out), atk.shared_prefix_attention(q, k, k, table, lens, 0))
