@@ -107,3 +107,20 @@ def test_strides_of_single_elements_are_not_used(lib):
             if size != "heads":
                 a.q_stride = i3(64, 64, 64) if name != "q_stride" else a.q_stride
             assert lib.atk_attention_workspace_bytes(a) == -7, (name, size)
+
+
+def test_strides_that_offsets_of_16_bytes_reach(lib):
+    # 300 sequences of 8 heads on 2 of 128: the plan of many rows up to pages of 2^34 elements in all and tokens below 2^28, and 2^34 in a page; that of few rows past it
+    i3 = ctypes.c_int64 * 3
+
+    def need(page, token, which="k_stride", n_pages=8):
+        a = _attention(batch=300, heads=8, kv_heads=2, dim=128, page_size=256, n_pages=n_pages, rows=300, row_pages=8, table_stride=8, prefix_len=7 * 256)
+        a.k_stride = a.v_stride = i3(256 * 256, 256, 128)
+        setattr(a, which, i3(page, token, 128))
+        return lib.atk_attention_workspace_bytes(a)
+
+    near = need(256 * 256, 256)
+    for which in ("k_stride", "v_stride"):
+        assert need(1 << 31, 256, which) == near and need((1 << 31) + 8, 256, which) != near
+        assert need(1 << 30, 256, which, 16) == near and need((1 << 30) + 8, 256, which, 16) != near
+        assert need(256, (1 << 26), which) == near and need(256, (1 << 26) + 8, which) != near
