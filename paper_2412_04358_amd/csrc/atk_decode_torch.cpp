@@ -159,7 +159,7 @@ PyObject *verify(PyObject *, PyObject *const *x, Py_ssize_t n) {
 
 // The pools of a list: their addresses, and the bytes of a token in each; false if they are not as the calls take them.
 bool pools_of(PyObject *list, int *device, int64_t pages, int64_t page_size, std::vector<void *> *at, int64_t *token_bytes) {
-    if (!PyList_CheckExact(list)) return false;
+    if (!PyList_CheckExact(list) || pages < 1 || page_size < 1) return false;
     const Py_ssize_t n = PyList_GET_SIZE(list);
     at->resize(n);
     *token_bytes = 0;

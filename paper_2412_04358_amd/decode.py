@@ -306,6 +306,8 @@ class PageTables:
 def _pools(pools, device, pages, page_size, what="pools"):
     """Addresses of the pools and the bytes of a token in each."""
     token_bytes = 0
+    if pages < 1 or page_size < 1:
+        raise ValueError("%s must hold a page, and a token in it, at least" % what)
     for t in pools:
         if t.dim() < 2 or t.shape[0] != pages or t.shape[1] != page_size or not t.is_contiguous():
             raise ValueError("%s must be contiguous tensors (pages, page_size, ...)" % what)
