@@ -314,10 +314,12 @@ def _pools(pools, device, pages, page_size, what="pools"):
         if t.device != device:
             raise ValueError("%s must live on the GPU, all tensors on the same one" % what)
         size = t.numel() // (pages * page_size) * t.element_size()
+        if size < 1:
+            raise ValueError("%s must hold a byte for a token at least" % what)
         if token_bytes and size != token_bytes:
             raise ValueError("%s must hold equally many bytes for a token" % what)
         token_bytes = size
-    return (_vp * len(pools))(*[t.data_ptr() for t in pools]), token_bytes or 1
+    return (_vp * len(pools))(*[t.data_ptr() for t in pools]), token_bytes or 1  # (no pools: the library wants a number)
 
 
 def copy_pages(src_pools, src_ids, dst_pools, dst_ids, status=None):
