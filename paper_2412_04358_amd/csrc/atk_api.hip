@@ -855,7 +855,7 @@ bool stage2_apart(int64_t m, int64_t n, int64_t k, int64_t b, int64_t k_b, int d
 // With 65 and more buckets, multiples of nothing among them, few buckets leave lanes without columns and the others many matrix rows, batch after batch
 // of loads (256 x 12276, k = 131, b = 66, k_b = 2: 8.0 us in a workgroup, 11.7 so; k_b = 8 13.5 and 20): above 110 matrix rows to a lane (200 on rows past
 // 12288 elements, which only large batches take) 0.5 to 1.6, level on the whole.  Up to there, against what the other plans take by now, over 16000 calls
-// of N(0,1) rows and logarithms of probabilities: 0.38 to 1.26 up to three thousand elements, 0.6 on the whole; 1025 and more rows 0.4 to 0.8, one call in a hundred
+// of N(0,1) rows and logarithms of probabilities: 0.38 to 1.26 up to 3 * 1024 elements, 0.6 on the whole; 1025 and more rows 0.4 to 0.8, one call in a hundred
 // above 1.04; up to 256 rows of 6145 to 12288 elements, queues of two to four slots, at most 1024 candidates and 256 winners, 0.91 to 1.21 (8 x 8192,
 // k = 250, b = 256, k_b = 4: 5.9 us in a workgroup, 6.2 so) - where logarithms of probabilities, which the workgroup does not sort as words, take 1.36
 // times as long in it (23 x 8568, k = 75, b = 504, k_b = 2: 8.05 and 5.9), so these stay.
