@@ -53,7 +53,7 @@ enum {
  *   lse        (batch, tokens, heads) f32, contiguous, or NULL.
  *   dim        a multiple of 16 bytes / element size, up to 256.  Pointers of q, k, v, out on 16 bytes, strides (but a single one's) of whole 16 bytes.
  *   work       atk_attention_workspace_bytes() bytes on 16 bytes.
- * Scores, statistics and accumulators are f32; the weights are rounded to `dtype` for the product with v.
+ * Scores, statistics and accumulators are f32; the weights are rounded to `dtype` for the product with v, their sum is not.
  */
 typedef struct {
     const void *q, *k, *v;
@@ -116,7 +116,7 @@ typedef struct {
 int64_t atk_pages_work_bytes(int64_t n_pages);
 
 /* Copies whole pages: dst pool p, page dst_ids[i] from src pool p, page src_ids[i], i < n, for n_pools pools (host arrays of
- * device pointers).  Destinations are distinct and no source of the same call.  page_bytes: a multiple of 4, pools on 16 bytes. */
+ * device pointers).  Destinations are distinct and no source of the same call.  (16 bytes at a time where page_bytes and all pools are multiples of 16, else 4 or 1.) */
 int atk_copy_pages(const void *const *src_pools, void *const *dst_pools, int64_t n_pools, int64_t page_bytes, int64_t src_pages,
                    int64_t dst_pages, const int32_t *src_ids, const int32_t *dst_ids, int64_t n, int32_t *status, void *stream);
 

@@ -166,7 +166,9 @@ struct VRows {
     }
 };
 
-// A lane's weights as operands, four of each half.
+// A lane's weights as operands, four of each half.  In 16 bits they are rounded to the type, since its products take nothing wider, and f32 products are a seventh as fast: each weight is
+// off by half a step at most, as the result's own rounding is, and the two together by 1.4 times that on average (64 samples on 8192 + 384 keys in bf16: 2.3e-3 of the result, rounded
+// once 1.7e-3).  Their sum l is taken before, in f32.
 template <int ELT>
 struct Weights {
     u32x4 w;
@@ -889,7 +891,8 @@ struct SharedUnit {
 };
 
 // Of attn_block_kernel's units (the first masked_grid workgroups), those with a row that sees only a part of the keys - a sequence that ends before them, a page that is none: tile by
-// tile, with masks.  Then own keys.
+// tile, with masks, 16 rows after the other, and each time K and V again.  That is the way of few rows, and slow for many: one sequence of length 0 among 64 on 8192 + 384 keys makes 176 us of
+// 49, 32 of them 209; among 128 on 65536 + 1125 keys 1500 of 270.  Then own keys.
 template <int ELT, int DP, bool AROUND>
 __device__ __forceinline__ void attn_rest(const AttnDev &a, int id, char *lds) {
     if (id >= a.masked_grid) {

@@ -3,7 +3,8 @@
 // These calls move whole tokens (bound by memory: every byte read once and written once) and change a few words of the tables (bound by launches and the
 // chain of dependent reads), so each is one launch where it can be: a workgroup finds out by itself what the sequences in front of its own take from
 // the stack (a sum over the call's sequences), moves its share of the data, and the last workgroup to end - by a ticket - changes what the others read.
-// Nothing depends on the order of workgroups: pages are taken by rank and given back by number.
+// Nothing depends on the order of workgroups: pages are taken by rank and given back by number.  That each workgroup of fork and append reads all of the call's sequences
+// is little for hundreds of them and quadratic past some thousands (one pool, fork and free: 512 sequences 31 us, 2048 85, 8192 263, 32768 1690).
 // 16 sequences forked to 512 in 24 pools of 32 KB pages: fork 57 us, append of five tokens 69, free 17; compaction that moves
 // 1500 pages of 16 pools, 1.57 GB read and written, 310 us (5.1 TB/s, a large copy's rate); 500 pages of 8 pools, 295 MB, in 55 us (5.4 TB/s, part of it out of the caches); one sequence: 6, 8 and 5 us.
 #include "atk_decode_common.h"
@@ -58,7 +59,7 @@ template <>
 struct Unit<4> { typedef uint32_t T; };
 template <>
 struct Unit<1> { typedef uint8_t T; };
-// AROUND: around the caches, for whole pages, more of them than the caches hold (500 pages of 295 MB in all: 68 us -> 59; not for what the next call reads again: fork would be slower).
+// AROUND: around the caches, for whole pages, more of them than the caches hold (500 pages of 295 MB in all: 68 us -> 59, and 55 with 32-bit quotients in for_units; not for what the next call reads again: fork would be slower).
 template <int UNIT, bool AROUND = false>
 __device__ __forceinline__ void copy_bytes(char *dst, const char *src, int64_t bytes) {
     typedef typename Unit<UNIT>::T T;
@@ -494,7 +495,8 @@ __global__ __launch_bounds__(kThreads) void pages_free_kernel(const PagesDev t, 
 
 // ------------------------------------------------------------------------------------------------------------- compact
 // The plan: how many pages are held, the new number of each, the list of moves (behind the work area's bits: sources, then destinations, as many as there
-// are pages at most) and the stack.  One workgroup of 1024, a run of pages a thread.
+// are pages at most) and the stack.  One workgroup of 1024, which goes over the pages twice, 1024 at a time: 11 us for a call with 6000 pages and nothing to move, 35 with 30000, 100 with 100000,
+// 1210 with a million.
 constexpr int kPlanThreads = 1024;
 __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(const PagesDev t, int32_t *remap, int32_t *moves, int32_t *n_moves) {
     __shared__ int waves[3][kPlanThreads / 64];

@@ -287,6 +287,7 @@ __global__ __launch_bounds__(64) void verify_draw_kernel(const VerifyDev a) {
 }
 
 // The whole request by one workgroup: its wavefronts have a sixteenth of the row each, then a chunk of the sixteenth that the goal lies in, then one has the chunk.
+// (1024 threads leave 128 registers each: 84 words a lane are spilled to scratch, in all three types.)
 constexpr int kRowBytes = 128 << 10;  // of a row at most
 constexpr int kRowWaves = 16, kRowChunks = kRowBytes / 2 / (kRowWaves * kChunk);  // chunks of a sixteenth at most: eight, four in f32
 static_assert(kRowChunks * kRowWaves * kChunk * 2 == kRowBytes && kRowChunks <= kRowWaves, "a wavefront for each chunk of a sixteenth");
