@@ -42,3 +42,9 @@ from .decode import (  # noqa: F401
     shared_prefix_attention,
     verify_drafts,
 )
+from .quantized import (  # noqa: F401
+    append_quantized,
+    quantized_attention,
+    quantized_token_bytes,
+    read_quantized,
+)

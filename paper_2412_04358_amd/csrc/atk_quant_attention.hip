@@ -1,0 +1,111 @@
+// quantized_attention: checks and launch plan (see atk_quant_attention_kernel.h).
+#include <cfloat>
+
+#include "atk_quant_attention_kernel.h"
+
+namespace atk {
+
+static int64_t quant_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+struct QuantPlan {
+    int dp, rt, row_blocks, splits, chunk;
+    bool join;
+    int64_t units, rows, o_bytes, bytes;
+};
+
+static int check_quant(const atk_quant_attention_args *p, bool pointers) {
+    if (!p) return ATK_ERR_NULL_PTR;
+    if (p->dtype != ATK_F32 && p->dtype != ATK_BF16 && p->dtype != ATK_F16) return ATK_ERR_DTYPE;
+    const int64_t token_bytes = atk_quant_token_bytes(p->kv_heads, p->dim, p->bits);
+    if (token_bytes < 0) return (int)token_bytes;
+    const int es = p->dtype == ATK_F32 ? 4 : 2, piece = 16 / es;
+    const int64_t most = INT64_C(1) << 30;
+    if (p->batch < 1 || p->tokens < 1 || p->heads < 1 || p->page_size < 1 || p->n_pages < 1 || p->rows < 1 || p->row_pages < 1) return ATK_ERR_ARGS;
+    if (p->batch > most || p->tokens > most || p->heads > most || p->page_size > most || p->n_pages > most || p->rows > most || p->row_pages > most) return ATK_ERR_ARGS;
+    if (p->heads % p->kv_heads || p->batch * p->tokens > most || p->batch * p->tokens * p->heads > most) return ATK_ERR_ARGS;
+    if (p->row_pages * p->page_size > most) return ATK_ERR_ARGS;
+    if (p->n_pages * p->page_size > (INT64_C(1) << 36) / token_bytes - 1) return ATK_ERR_ARGS;  // (a row's place in 16 bytes is 32 bits)
+    if (!p->seqs && p->batch > p->rows) return ATK_ERR_ARGS;
+    if (p->table_stride < p->row_pages) return ATK_ERR_ARGS;
+    if (!(p->scale >= FLT_MIN) || p->scale > 1e30) return ATK_ERR_ARGS;  // (the kernels have it in f32, where less is 0 or nearly so, and 0 * inf no number)
+    const int64_t rows[3] = {p->batch, p->tokens, p->heads};
+    for (int i = 0; i < 3; ++i) {
+        if (p->q_stride[i] < 0 || p->out_stride[i] < 0) return ATK_ERR_ARGS;
+        if (rows[i] > 1 && (p->q_stride[i] % piece || p->out_stride[i] % piece)) return ATK_ERR_ALIGN;
+    }
+    if (pointers) {
+        if (!p->q || !p->k || !p->v || !p->out || !p->page_table || !p->lens) return ATK_ERR_NULL_PTR;
+        if (((uintptr_t)p->q | (uintptr_t)p->k | (uintptr_t)p->v | (uintptr_t)p->out) & 15) return ATK_ERR_ALIGN;
+        if (((uintptr_t)p->page_table | (uintptr_t)p->lens | (uintptr_t)p->seqs | (uintptr_t)p->lse | (uintptr_t)p->status) & 3) return ATK_ERR_ALIGN;
+    }
+    return ATK_OK;
+}
+
+static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
+    const int64_t group = p->heads / p->kv_heads, rows = p->tokens * group, all = p->row_pages * p->page_size;
+    pl->dp = p->dim <= 64 ? 64 : p->dim <= 128 ? 128 : 256;
+    pl->rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    pl->rt = std::min(pl->rt, quant_max_rt(p->dtype, pl->dp));
+    pl->row_blocks = (int)quant_ceil(rows, 16 * pl->rt);
+    const int64_t base = p->batch * p->kv_heads * pl->row_blocks, tiles = quant_ceil(all, 32);
+    // few keys: a workgroup's wavefronts share them
+    pl->join = pl->rt == 1 && tiles <= 32;
+    const int64_t wanted = 16 * kNumCU;
+    pl->splits = pl->join ? 1 : (int)std::max<int64_t>(1, std::min(quant_ceil(tiles, 4), wanted / base));
+    pl->units = base * pl->splits;
+    const int64_t per = pl->join ? 1 : kQuantWaves;
+    pl->chunk = (int)(p->kv_heads % per ? 1 : std::min<int64_t>(p->kv_heads / per, 16));
+    pl->rows = p->batch * p->tokens * p->heads;
+    pl->o_bytes = pl->splits > 1 ? pl->rows * pl->splits * p->dim * 4 : 0;
+    pl->bytes = pl->splits > 1 ? pl->o_bytes + pl->rows * pl->splits * 8 : 16;
+    const bool fit = pl->units < (INT64_C(1) << 31) && launches(quant_ceil(pl->units, per) + 8 * pl->chunk, 64 * kQuantWaves) && launches(quant_ceil(pl->rows, 4), 256);
+    return fit ? ATK_OK : ATK_ERR_ARGS;
+}
+
+}  // namespace atk
+
+using namespace atk;
+
+extern "C" {
+
+int64_t atk_quant_attention_workspace_bytes(const atk_quant_attention_args *p) {
+    int rc = check_quant(p, false);
+    QuantPlan pl;
+    if (rc == ATK_OK) rc = plan_quant(p, &pl);
+    return rc == ATK_OK ? pl.bytes : rc;
+}
+
+int atk_quant_attention(const atk_quant_attention_args *p, void *work, int64_t work_bytes, void *stream) {
+    int rc = check_quant(p, true);
+    QuantPlan pl;
+    if (rc == ATK_OK) rc = plan_quant(p, &pl);
+    if (rc != ATK_OK) return rc;
+    if (!work) return ATK_ERR_NULL_PTR;
+    if ((uintptr_t)work & 15) return ATK_ERR_ALIGN;
+    if (work_bytes < pl.bytes) return ATK_ERR_WORKSPACE;
+    QuantAttnDev d = {};
+    AttnDev &a = d.a;
+    a.q = p->q, a.k = p->k, a.v = p->v, a.out = p->out, a.lse = p->lse;
+    a.table = p->page_table, a.lens = p->lens, a.seqs = p->seqs, a.status = p->status;
+    a.parts_o = (float *)work, a.parts_ml = (float2 *)((char *)work + pl.o_bytes);
+    a.table_stride = p->table_stride;
+    for (int i = 0; i < 3; ++i) a.qs[i] = p->q_stride[i], a.os[i] = p->out_stride[i];
+    a.batch = (int)p->batch, a.tokens = (int)p->tokens, a.heads = (int)p->heads, a.kv_heads = (int)p->kv_heads;
+    a.group = a.heads / a.kv_heads, a.dim = (int)p->dim;
+    a.rows = (int)p->rows, a.row_pages = (int)p->row_pages, a.n_pages = (int)p->n_pages;
+    a.parts = pl.splits;
+    a.direct = pl.splits == 1;
+    a.page.set((uint32_t)p->page_size);
+    a.scale = (float)p->scale;
+    a.scale2 = (float)(p->scale * 1.4426950408889634);
+    d.row16 = (uint32_t)(mx_token_bytes(p->kv_heads, p->dim, p->bits) / 16);
+    d.head_codes = (uint32_t)(p->dim * p->bits / 8), d.head_units = (uint32_t)(p->dim / kMxBlock), d.code_bytes = (uint32_t)p->kv_heads * d.head_codes;
+    d.row_blocks = pl.row_blocks, d.splits = pl.splits, d.units = (int)pl.units, d.chunk = pl.chunk;
+    hipStream_t s = (hipStream_t)stream;
+    const hipError_t e = p->dtype == ATK_F32    ? launch_quant_f32(d, p->bits, pl.dp, pl.rt, pl.join, s)
+                         : p->dtype == ATK_BF16 ? launch_quant_bf16(d, p->bits, pl.dp, pl.rt, pl.join, s)
+                                                : launch_quant_f16(d, p->bits, pl.dp, pl.rt, pl.join, s);
+    return e == hipSuccess ? ATK_OK : set_hip_error(e);
+}
+
+}  // extern "C"

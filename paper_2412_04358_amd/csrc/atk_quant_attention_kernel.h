@@ -1,0 +1,489 @@
+// Attention over a cache of few bits: one range of a sequence's keys against a block of its queries.
+//
+// Ranges, their join, what a wavefront takes (32 keys at a time, everything in registers) and how the two products follow each other are those of attn_range (atk_attention_kernel.h).
+// What differs is where the operands come from.  A power of two is exact in 16 bits, and so are the codes, so keys and values become bf16 (f16) numbers by one conversion for two of them,
+// unit included, and nothing is rounded:
+//   K  a lane has 16 bytes of one key (4 bits and heads of 64: 8), of one or two blocks: operands in their order, those of q alike.
+//   V  a lane has DP / 16 elements of each of the eight keys that its weights belong to, of one block; after the conversion they are paired up as in attn_range.
+// f32 goes the same way, by three products each: a f32 number is the sum of three bf16 ones (its mantissa cut in three), so q and the weights are given whole, and the products
+// with keys and values, which are bf16 numbers, are summed up in f32.  (f32 products take eight times as long as bf16 ones.)
+#pragma once
+
+#include "atk_attention_join.h"
+#include "atk_mx.h"
+
+namespace atk {
+
+constexpr int kQuantWaves = 4;
+
+struct QuantAttnDev {
+    AttnDev a;              // (of its key fields only those that the join needs)
+    uint32_t row16;         // a token's row in 16 bytes
+    uint32_t head_codes, head_units, code_bytes;
+    int row_blocks, splits, units;
+    int chunk;              // workgroups next to each other that read the same keys: they go to one XCD
+};
+
+constexpr int quant_products(int elt) { return elt == ATK_F32 ? ATK_BF16 : elt; }  // type of the products' operands
+constexpr int quant_parts(int elt) { return elt == ATK_F32 ? 3 : 1; }              // operands that a number of q or a weight is the sum of
+
+// A pair of f32 numbers as pairs of bf16 ones of which they are the sums: cut, not rounded, so that the largest numbers stay finite.
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t *w) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+        w[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+        a = a - __uint_as_float(x & 0xffff0000u), b = b - __uint_as_float(y & 0xffff0000u);
+    }
+}
+
+template <int ELT>
+struct QuantWeights {
+    Weights<quant_products(ELT)> p[quant_parts(ELT)];
+    __device__ __forceinline__ void set(const f32x4 *s) {
+        if constexpr (ELT == ATK_F32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t w[3];
+                split_pair(s[i / 2][2 * (i & 1)], s[i / 2][2 * (i & 1) + 1], w);
+#pragma unroll
+                for (int j = 0; j < 3; ++j) p[j].w[i] = w[j];
+            }
+        } else {
+            p[0].set(s);
+        }
+    }
+};
+
+// Eight elements of a query.
+template <int ELT>
+struct QuantQuery {
+    u32x4 w[quant_parts(ELT)];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int j = 0; j < quant_parts(ELT); ++j) w[j] = u32x4{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ void load(const char *p) {
+        if constexpr (ELT == ATK_F32) {
+            const f32x4 a = ((const f32x4 *)p)[0], b = ((const f32x4 *)p)[1];
+            const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t y[3];
+                split_pair(x[2 * i], x[2 * i + 1], y);
+                // (what is left of an infinity is NaN, and the infinity alone is right)
+                const bool all = fabsf(x[2 * i]) < __builtin_inff(), all2 = fabsf(x[2 * i + 1]) < __builtin_inff();
+                const uint32_t keep = (all ? 0xffffu : 0u) | (all2 ? 0xffff0000u : 0u);
+                // (a NaN whose mantissa's upper bits are clear would be cut to an infinity)
+                w[0][i] = y[0] | (x[2 * i] != x[2 * i] ? 0x40u : 0u) | (x[2 * i + 1] != x[2 * i + 1] ? 0x400000u : 0u);
+                w[1][i] = y[1] & keep, w[2][i] = y[2] & keep;
+            }
+        } else {
+            w[0] = *(const u32x4 *)p;
+        }
+    }
+};
+
+// What a lane holds of 32 keys as it lies in memory.
+template <int BITS, int DP>
+struct QuantRaw {
+    static constexpr int kStepWords = BITS / 4;                             // words of eight elements
+    static constexpr int kPieceWords = BITS == 4 && DP == 64 ? 2 : 4;       // words of a piece of a key
+    static constexpr int kPieceSteps = kPieceWords / kStepWords;            // products that it is for
+    static constexpr int NC = DP / 32 / kPieceSteps;                        // pieces of a key
+    static constexpr int kVBytes = DP / 16 * BITS / 8;                      // bytes of V's row
+    static constexpr int kVWords = (kVBytes + 3) / 4;
+    static constexpr int kPieceDims = 8 * kPieceSteps;
+    uint32_t k[2][NC][kPieceWords], ku[2][NC], v[8][kVWords], vu[8];
+};
+
+template <int ELT, int BITS, int DP, int RT, bool JOIN>
+__global__ __launch_bounds__(64 * kQuantWaves) void quant_attn_kernel(const QuantAttnDev d) {
+    typedef AttnElt<ELT> E;
+    constexpr int PE = quant_products(ELT), PARTS = quant_parts(ELT);
+    typedef AttnElt<PE> P;
+    typedef QuantRaw<BITS, DP> Raw;
+    constexpr int NT = DP / 16, NS = DP / 32;       // products along d of the second product, of the first
+    constexpr int TK = 32, NW = kQuantWaves;
+    const AttnDev &a = d.a;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n = lane & 15, g = lane >> 4;
+
+    // workgroups of a chunk are 8 apart, which is how they come to one XCD
+    const uint32_t at8 = blockIdx.x / 8, block = (at8 / d.chunk * 8 + blockIdx.x % 8) * d.chunk + at8 % d.chunk;
+    const uint32_t unit = JOIN ? block : block * NW + wave;
+    if (unit >= (uint32_t)d.units) return;
+    const int h = (int)(unit % (uint32_t)a.kv_heads);
+    uint32_t rest = unit / (uint32_t)a.kv_heads;
+    const int split = (int)(rest % (uint32_t)d.splits);
+    rest /= (uint32_t)d.splits;
+    const int block_of = (int)(rest % (uint32_t)d.row_blocks), b = (int)(rest / (uint32_t)d.row_blocks);
+    const int n_rows = a.tokens * a.group, r0 = block_of * 16 * RT;
+
+    bool bad_len = false, bad_seq = false, bad_page = false;
+    const int s_row = seq_row(a, b, &bad_seq);
+    const int len = seq_len(a, s_row, &bad_len);
+    // the keys that the block's last query sees, in ranges of whole tiles
+    const int last_t = (min(r0 + 16 * RT, n_rows) - 1) / a.group;
+    const int end = max(0, len - (a.tokens - 1 - last_t));
+    const int range = ((end + TK - 1) / TK + d.splits - 1) / d.splits * TK;
+    const int ka = (int)min((int64_t)end, (int64_t)split * range), kb = min(end, ka + range);
+    const int32_t *table_row = a.table + max(s_row, 0) * a.table_stride;
+
+    QuantQuery<ELT> q[RT][NS];
+    int lim[RT];
+    int min_lim = kb;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = r0 + rt * 16 + n;
+        const bool real = r < n_rows;
+        const AttnRow x = attn_row(a, h, real ? r : 0, b);
+        // rows past the end are computed as if they saw all keys, and not written: they must not make tiles masked
+        lim[rt] = real ? min(kb, len - (a.tokens - 1 - x.t)) : kb;
+        min_lim = min(min_lim, lim[rt]);
+        const char *p = (const char *)a.q + (x.b * a.qs[0] + x.t * a.qs[1] + x.head * a.qs[2]) * E::kBytes;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const int dim = (s / Raw::kPieceSteps * 4 + g) * Raw::kPieceDims + s % Raw::kPieceSteps * 8;
+            if (dim < a.dim)
+                q[rt][s].load(p + dim * E::kBytes);
+            else
+                q[rt][s].clear();
+        }
+    }
+    for (int w = 1; w < 16; w <<= 1) min_lim = min(min_lim, __shfl_xor(min_lim, w, 64));
+
+    float m[RT], l[RT];  // maximum, in units of s: c * s need not be finite where s is
+    bool far = false;    // ... and is not for some query of the wavefront
+    f32x4 acc[RT][NT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m[rt] = kNoMax, l[rt] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) acc[rt][i] = f32x4{0, 0, 0, 0};
+    }
+    const char *kc = (const char *)a.k + h * d.head_codes, *vc = (const char *)a.v + h * d.head_codes;
+    const char *ku = (const char *)a.k + d.code_bytes + h * d.head_units, *vu = (const char *)a.v + d.code_bytes + h * d.head_units;
+
+    // lane j (and the one 32 behind it) looks key k0 + j up; keys past the end are read as the last one and masked
+    constexpr int kStep = JOIN ? NW * TK : TK;
+    auto page_of = [&](int k0) { return table_row[a.page.div(min(k0 + (lane & 31), kb - 1))]; };
+    uint32_t valid = 0;
+    auto places = [&](int k0, int page, uint32_t *place) {
+        const bool good = (unsigned)page < (unsigned)a.n_pages;
+        bad_page |= !good;
+        valid = (uint32_t)__ballot(good);
+        *place = ((uint32_t)(good ? page : 0) * a.page.d + (uint32_t)a.page.mod(min(k0 + (lane & 31), kb - 1))) * d.row16;
+    };
+    auto load = [&](uint32_t place, Raw &x) {
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const uint64_t row = (uint64_t)(uint32_t)__shfl((int)place, y * 16 + n, 64) << 4;
+#pragma unroll
+            for (int c = 0; c < Raw::NC; ++c) {
+                const int dim = (c * 4 + g) * Raw::kPieceDims;
+                if (dim < a.dim) {
+                    const char *p = kc + row + dim * BITS / 8;
+                    if constexpr (Raw::kPieceWords == 4) {
+                        const u32x4 t = *(const u32x4 *)p;
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) x.k[y][c][z] = t[z];
+                    } else {
+                        const u32x2 t = *(const u32x2 *)p;
+                        x.k[y][c][0] = t[0], x.k[y][c][1] = t[1];
+                    }
+                    x.ku[y][c] = (uint8_t)ku[row + dim / kMxBlock];
+                } else {
+                    x.ku[y][c] = 0;
+#pragma unroll
+                    for (int z = 0; z < Raw::kPieceWords; ++z) x.k[y][c][z] = 0;
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint64_t row = (uint64_t)(uint32_t)__shfl((int)place, (j / 4) * 16 + g * 4 + j % 4, 64) << 4;
+            const int dim = n * (DP / 16);
+            if (dim < a.dim) {
+                const char *p = vc + row + n * Raw::kVBytes;
+                if constexpr (Raw::kVBytes == 2) {
+                    x.v[j][0] = *(const uint16_t *)p;
+                } else if constexpr (Raw::kVBytes == 4) {
+                    x.v[j][0] = *(const uint32_t *)p;
+                } else if constexpr (Raw::kVBytes == 8) {
+                    const u32x2 t = *(const u32x2 *)p;
+                    x.v[j][0] = t[0], x.v[j][1] = t[1];
+                } else {
+                    const u32x4 t = *(const u32x4 *)p;
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) x.v[j][z] = t[z];
+                }
+                x.vu[j] = (uint8_t)vu[row + dim / kMxBlock];
+            } else {
+                x.vu[j] = 0;
+#pragma unroll
+                for (int z = 0; z < Raw::kVWords; ++z) x.v[j][z] = 0;
+            }
+        }
+    };
+
+    const int first = ka + (JOIN ? wave * TK : 0);
+    Raw raw;
+    int page_next = 0;
+    if (first < kb) {
+        uint32_t place;
+        places(first, page_of(first), &place);
+        page_next = page_of(first + kStep);
+        load(place, raw);
+    }
+    for (int k0 = first; k0 < kb; k0 += kStep) {
+        // operands, and then the next tile's loads into the registers that they came from
+        u32x4 kf[2][NS];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const int c = s / Raw::kPieceSteps;
+                kf[x][s] = __builtin_bit_cast(u32x4, mx_eight<PE, BITS>(&raw.k[x][c][s % Raw::kPieceSteps * Raw::kStepWords], mx_unit(raw.ku[x][c])));
+            }
+        VRows<PE, DP> v;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float unit = mx_unit(raw.vu[j]);
+            if constexpr (NT >= 8) {
+#pragma unroll
+                for (int x = 0; x < NT / 8; ++x) {
+                    const u32x4 t = __builtin_bit_cast(u32x4, mx_eight<PE, BITS>(&raw.v[j][x * Raw::kStepWords], unit));
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) v.w[j][x * 4 + y] = t[y];
+                }
+            } else {
+                v.w[j][0] = mx_pair<PE, BITS, 0>(raw.v[j], unit);
+                v.w[j][1] = mx_pair<PE, BITS, 1>(raw.v[j], unit);
+            }
+        }
+        const uint32_t now = valid;
+        if (k0 + kStep < kb) {
+            uint32_t place;
+            places(k0 + kStep, page_next, &place);
+            page_next = page_of(k0 + 2 * kStep);
+            load(place, raw);
+        }
+        f32x4 s[RT][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                s[rt][x] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int c = 0; c < NS; ++c)
+#pragma unroll
+                    for (int y = PARTS - 1; y >= 0; --y) s[rt][x] = P::mma(kf[x][c], q[rt][c].w[y], s[rt][x]);
+            }
+        const bool masked = k0 + TK > min_lim || now != 0xffffffffu;
+        bool apart = false;  // a value that is not finite beside a mask: 0 * it would not be 0
+        if (masked) {
+            asm volatile("");  // (a branch, no selections)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int at = x * 16 + g * 4 + j;
+                        if (k0 + at >= lim[rt] || !(now >> at & 1)) s[rt][x][j] = kNoMax;
+                    }
+            apart = __any(v.any_not_finite());
+        }
+        float top[RT];
+        bool raise = false;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float t = s[rt][0][0];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) t = fmaxf(t, s[rt][x][j]);
+            t = fmaxf(t, __shfl_xor(t, 16, 64));
+            t = fmaxf(t, __shfl_xor(t, 32, 64));
+            top[rt] = t;
+            raise |= (t - m[rt]) * a.scale2 > kLazyMax;
+        }
+        if (__any(raise)) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const float to = fmaxf(m[rt], top[rt]);
+                const float f = __builtin_amdgcn_exp2f((m[rt] - to) * a.scale2);
+                if (m[rt] != kNoMax) {  // (else nothing is kept yet)
+                    l[rt] *= f;
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) acc[rt][i] *= f;
+                }
+                m[rt] = to;
+                far |= fabsf(to) < __builtin_inff() && !(fabsf(to * a.scale2) < __builtin_inff());
+            }
+            far = __any(far);
+        }
+        QuantWeights<ELT> p[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const float zero = m[rt] == kNoMax ? 0.0f : m[rt];
+            const float ref = zero * a.scale2 - E::kBias;
+            float sum = 0.0f;
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float e = __builtin_amdgcn_exp2f(far ? fmaf(s[rt][x][j] - zero, a.scale2, E::kBias) : fmaf(s[rt][x][j], a.scale2, -ref));
+                    s[rt][x][j] = e;
+                    sum += e;
+                }
+            l[rt] += sum;
+            p[rt].set(s[rt]);
+        }
+        if (!apart) {
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                const u32x4 vi = v.operand(i);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int y = PARTS - 1; y >= 0; --y) acc[rt][i] = P::mma(vi, p[rt].p[y].w, acc[rt][i]);
+            }
+        } else {
+            // query by query, with the values it does not see at 0; a product's columns are queries of their own
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+                for (int c = 0; c < 16; ++c) {
+                    const int limit = __shfl(lim[rt], c, 64);
+                    VRows<PE, DP> u = v;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int at = (j / 4) * 16 + g * 4 + j % 4;
+                        if (k0 + at >= limit || !(now >> at & 1))
+#pragma unroll
+                            for (int x = 0; x < VRows<PE, DP>::kWords; ++x) u.w[j][x] = 0;
+                    }
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) {
+                        f32x4 t = acc[rt][i];
+#pragma unroll
+                        for (int y = PARTS - 1; y >= 0; --y) t = P::mma(u.operand(i), p[rt].p[y].w, t);
+                        if (n == c) acc[rt][i] = t;
+                    }
+                }
+        }
+    }
+    const int bad = (bad_page ? ATK_STATUS_BAD_PAGE : 0) | (bad_seq ? ATK_STATUS_BAD_SEQ : 0) | (bad_len ? ATK_STATUS_BAD_LEN : 0);
+    if (bad && a.status) atomicOr(a.status, bad);
+
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        l[rt] += __shfl_xor(l[rt], 16, 64);
+        l[rt] += __shfl_xor(l[rt], 32, 64);
+    }
+    if constexpr (JOIN) {
+        // the wavefronts' ranges join in LDS, in their order
+        constexpr int kPitch = DP + 4;
+        __shared__ float ls_m[NW * RT * 16], ls_l[NW * RT * 16], ls_o[RT * 16 * kPitch];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+            if (g == 0) ls_m[(wave * RT + rt) * 16 + n] = m[rt], ls_l[(wave * RT + rt) * 16 + n] = l[rt];
+        __syncthreads();
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float to = kNoMax;
+            for (int w = 0; w < NW; ++w) to = fmaxf(to, ls_m[(w * RT + rt) * 16 + n]);
+            l[rt] = 0.0f;
+            for (int w = 0; w < NW; ++w) {
+                const float mw = ls_m[(w * RT + rt) * 16 + n];
+                l[rt] += ls_l[(w * RT + rt) * 16 + n] * (mw == kNoMax ? 1.0f : __builtin_amdgcn_exp2f((mw - to) * a.scale2));
+            }
+            if (m[rt] != kNoMax) {
+                const float f = __builtin_amdgcn_exp2f((m[rt] - to) * a.scale2);
+#pragma unroll
+                for (int i = 0; i < NT; ++i) acc[rt][i] *= f;
+            }
+            m[rt] = to;
+        }
+        for (int w = 0; w < NW; ++w) {
+            if (wave == w) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int i = 0; i < NT; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            float *o = ls_o + (rt * 16 + n) * kPitch + (g * 4 + j) * NT + i;
+                            if (w > 0) acc[rt][i][j] += *o;
+                            if (w < NW - 1) *o = acc[rt][i][j];
+                        }
+            }
+            __syncthreads();
+        }
+        if (wave != NW - 1) return;
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = r0 + rt * 16 + n;
+        if (r >= n_rows) continue;
+        const AttnRow x = attn_row(a, h, r, b);
+        const int64_t row = ((int64_t)x.b * a.tokens + x.t) * a.heads + x.head;
+        if (a.direct) {  // nothing to join
+            if (g == 0 && a.lse) a.lse[row] = row_lse<ELT>(a, m[rt], l[rt]);
+            const float f = 1.0f / l[rt];
+            const bool none = l[rt] == 0.0f;  // no key, or scores of -inf alone, whose values do not count even if they are NaN
+            char *out = (char *)a.out + (x.b * a.os[0] + x.t * a.os[1] + x.head * a.os[2]) * E::kBytes;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < NT; i += 4) {
+                    const int dim = (g * 4 + j) * NT + i;
+                    f32x4 o = f32x4{acc[rt][i][j] * f, acc[rt][i + 1][j] * f, acc[rt][i + 2][j] * f, acc[rt][i + 3][j] * f};
+                    if (none) o = f32x4{0, 0, 0, 0};
+                    if (dim < a.dim) store_out<ELT>(out + dim * E::kBytes, o);
+                }
+            continue;
+        }
+        if (g == 0) a.parts_ml[row * a.parts + split] = float2{m[rt], l[rt]};
+        float *o = a.parts_o + (row * a.parts + split) * a.dim;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < NT; i += 4) {
+                const int dim = (g * 4 + j) * NT + i;
+                if (dim < a.dim) *(f32x4 *)(o + dim) = f32x4{acc[rt][i][j], acc[rt][i + 1][j], acc[rt][i + 2][j], acc[rt][i + 3][j]};
+            }
+    }
+}
+
+// Row tiles of a wavefront at most: f32's queries are three operands each.
+constexpr int quant_max_rt(int elt, int dp) { return dp == 256 ? (elt == ATK_F32 ? 1 : 2) : elt == ATK_F32 ? 2 : 4; }
+
+template <int ELT, int BITS, int DP, int RT, bool JOIN>
+static hipError_t launch_quant(const QuantAttnDev &d, hipStream_t stream) {
+    const int64_t groups = JOIN ? d.units : ((int64_t)d.units + kQuantWaves - 1) / kQuantWaves, whole = 8 * (int64_t)d.chunk;
+    hipLaunchKernelGGL((quant_attn_kernel<ELT, BITS, DP, RT, JOIN>), dim3((uint32_t)((groups + whole - 1) / whole * whole)), dim3(64 * kQuantWaves), 0, stream, d);
+    return hipGetLastError();
+}
+template <int ELT, int BITS, int DP>
+static hipError_t launch_quant_rt(const QuantAttnDev &d, int rt, bool join, hipStream_t stream) {
+    if (rt == 1) return join ? launch_quant<ELT, BITS, DP, 1, true>(d, stream) : launch_quant<ELT, BITS, DP, 1, false>(d, stream);
+    if constexpr (quant_max_rt(ELT, DP) >= 4)
+        if (rt == 4) return launch_quant<ELT, BITS, DP, 4, false>(d, stream);
+    if constexpr (quant_max_rt(ELT, DP) >= 2) return launch_quant<ELT, BITS, DP, 2, false>(d, stream);
+    return hipErrorInvalidValue;
+}
+template <int ELT>
+static hipError_t launch_quant_elt(const QuantAttnDev &d, int bits, int dp, int rt, bool join, hipStream_t stream) {
+    hipError_t e = bits == 4 ? (dp == 64 ? launch_quant_rt<ELT, 4, 64>(d, rt, join, stream) : dp == 128 ? launch_quant_rt<ELT, 4, 128>(d, rt, join, stream) : launch_quant_rt<ELT, 4, 256>(d, rt, join, stream))
+                             : (dp == 64 ? launch_quant_rt<ELT, 8, 64>(d, rt, join, stream) : dp == 128 ? launch_quant_rt<ELT, 8, 128>(d, rt, join, stream) : launch_quant_rt<ELT, 8, 256>(d, rt, join, stream));
+    if (e == hipSuccess && !d.a.direct) e = launch_join<ELT>(d.a, dp, stream);
+    return e;
+}
+
+hipError_t launch_quant_f32(const QuantAttnDev &d, int bits, int dp, int rt, bool join, hipStream_t stream);
+hipError_t launch_quant_bf16(const QuantAttnDev &d, int bits, int dp, int rt, bool join, hipStream_t stream);
+hipError_t launch_quant_f16(const QuantAttnDev &d, int bits, int dp, int rt, bool join, hipStream_t stream);
+
+}  // namespace atk

@@ -1,0 +1,250 @@
+"""quantized_attention against its definition in 64 bits on the values that the codes stand for.
+
+The tolerance counts roundings as the test of shared_prefix_attention does, with h half a step of the type and e = 2^-24: a weight is rounded to the type (h, against the
+sum of weight * |v|), so is the result (h of it); a score is a sum of dim products in f32 (f32: of three for each), off by (3 dim + 4) e of scale * sum |q k|, and a weight by as much
+relatively, in the sum of weights too; 2^x is good to 4 e; sums over n keys add n e (f32: 3 n).  f16 weights have steps of 2^-31 of the largest at the least."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2412_04358_amd as atk
+from oracle import decode as plain
+from oracle import quant as oracle
+
+pytestmark = pytest.mark.gpu
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+TYPES = [torch.bfloat16, torch.float16, torch.float32]
+E = 2.0 ** -24
+
+
+def make(B, T, H, Hk, D, lens, ps, dtype, bits, seed=0, spare=2, rows=None, scale_q=1.0, scale_kv=1.0):
+    """q, k, v, table, lens; unused pages, unused slots and padding hold bytes of NaN, and entries past a row's pages are -1."""
+    g = np.random.default_rng(seed)
+    rows = B if rows is None else rows
+    M = max(1, max(-(-n // ps) for n in lens) + spare)
+    P = rows * M + 1
+    table = g.permutation(P)[:rows * M].reshape(rows, M)
+    pools = []
+    for _ in range(2):
+        pool = np.full((P, ps, oracle.token_bytes(Hk, D, bits)), 0xFF, np.uint8)
+        for r in range(rows):
+            at = np.arange(lens[r])
+            if lens[r]:
+                pool[table[r, at // ps], at % ps] = oracle.encode(scale_kv * g.standard_normal((lens[r], Hk, D)), bits)
+        pools.append(torch.from_numpy(pool).cuda())
+    for r in range(rows):
+        table[r, -(-lens[r] // ps):] = -1
+    q = torch.from_numpy(scale_q * g.standard_normal((B, T, H, D))).to(dtype).cuda()
+    return [q, *pools, torch.from_numpy(table).int().cuda(), torch.tensor(lens, dtype=torch.int32).cuda()]
+
+
+def wider(table, ps, keys):
+    """The table with room for more pages: the host plans for longer sequences."""
+    wide = torch.full((table.shape[0], table.shape[1] + keys // ps), -1, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = table
+    return wide
+
+
+def check(q, k, v, table, lens, Hk, bits, seqs=None, scale=None):
+    want = None
+    for keys in (0, 3000, 40000):
+        want, got = _check(q, k, v, wider(table, k.shape[1], keys), lens, Hk, bits, seqs, scale, want)
+    return got
+
+
+def _check(q, k, v, table, lens, Hk, bits, seqs, scale, expected):
+    D = q.shape[3]
+    status = torch.zeros((1,), dtype=torch.int32, device="cuda")
+    out, lse = atk.quantized_attention(q, k, v, table, lens, Hk, bits=bits, seqs=seqs, scale=scale, return_lse=True, status=status)
+    torch.cuda.synchronize()
+    if expected is None:
+        kv = []
+        for pool in (k, v):
+            with np.errstate(over="ignore"):
+                x = torch.from_numpy(oracle.decode(pool.cpu().numpy(), Hk, D, bits)).to(q.dtype).double().numpy()
+            kv.append(x)
+        expected = plain.attention(q.double().cpu().numpy(), *kv, table.cpu().numpy(), lens.cpu().numpy(), 0, None if seqs is None else seqs.cpu().numpy(), D ** -0.5 if scale is None else scale)
+    want, wlse, mass, size, count, top = expected
+    h, f32 = HALF[q.dtype], 3 if q.dtype == torch.float32 else 1
+    weight = 2 * (f32 * D + 4) * E * size + (4 + f32 * count) * E     # relative, of a weight or of their sum
+    tol = mass * (h + 2 * weight)[..., None] + h * np.abs(want)
+    if q.dtype == torch.float16:
+        tol = tol + 2 * (count * top * 2.0 ** -31)[..., None] + 2.0 ** -24  # (and outputs have subnormal steps)
+    got_out, got_lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    assert status.item() == 0
+    assert np.array_equal(np.isnan(got_out), np.isnan(want)) and np.array_equal(np.isnan(got_lse), np.isnan(wlse))
+    finite = np.isfinite(want)
+    assert (np.abs(got_out - want)[finite] <= tol[finite]).all(), np.nanmax((np.abs(got_out - want) / tol)[finite & (tol > 0)])
+    live = np.isfinite(wlse)
+    assert np.array_equal(got_lse[~live & ~np.isnan(wlse)], wlse[~live & ~np.isnan(wlse)])
+    with np.errstate(invalid="ignore"):
+        off = np.abs(got_lse - wlse)
+    assert (off[live] <= (weight + 4 * E * (1 + np.abs(wlse)))[live]).all()
+    return expected, (out, lse)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("B,T,H,Hk,D,lens,ps", [
+    (1, 1, 1, 1, 32, [1], 16),                       # one key
+    (2, 1, 8, 2, 64, [50, 41], 16),
+    (3, 1, 4, 4, 128, [64, 0, 200], 16),             # every head its own keys; a sequence of none
+    (2, 5, 8, 1, 128, [105, 3], 8),                  # drafts; queries that see no key
+    (4, 3, 10, 2, 96, [36, 90, 35, 33], 24),         # dim and page size that are no powers of two, rows with padding
+    (2, 2, 6, 2, 160, [2, 77], 1),                   # pages of one token
+    (2, 1, 16, 1, 192, [129, 260], 32),
+    (1, 17, 5, 1, 256, [48], 7),                     # more rows than one tile; long heads
+    (1, 9, 4, 1, 224, [100], 16),
+    (2, 40, 8, 2, 64, [40, 333], 16),                # many rows
+    (1, 70, 2, 1, 128, [97], 5),
+    (5, 1, 20, 5, 128, [1500 + 40 * i + 1 for i in range(5)], 64),
+    (1, 1, 6, 3, 64, [4100], 16),                    # a long one by itself: heads that are no multiple of four
+], ids=lambda v: str(len(v)) if isinstance(v, list) else str(v))
+def test_shapes(bits, dtype, B, T, H, Hk, D, lens, ps):
+    check(*make(B, T, H, Hk, D, lens, ps, dtype, bits, seed=B * 100 + D), Hk, bits)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("length", [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 160, 255, 1024, 1025])
+def test_lengths(bits, dtype, length):
+    check(*make(2, 1, 4, 2, 64, [length, max(0, length - 5)], 16, dtype, bits, seed=length), 2, bits)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_scales_and_sizes(dtype):
+    big = 2.0 ** 7 if dtype == torch.float16 else 2.0 ** 40
+    for scale_q, scale_kv, scale in ((30.0, 1.0, None), (1.0, big, 1e-3 / big), (1e-3, 1e-3, 50.0), (1.0, 1.0, 1e-6)):
+        check(*make(2, 2, 4, 2, 64, [70, 300], 16, dtype, 4, seed=3, scale_q=scale_q, scale_kv=scale_kv), 2, 4, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_rows_of_the_table_and_strides(dtype):
+    B, T, H, Hk, D = 3, 2, 8, 2, 64
+    q, k, v, table, lens = make(B, T, H, Hk, D, [100, 50, 75, 20, 33], 16, dtype, 4, seed=5, rows=5)
+    seqs = torch.tensor([4, 0, 4], dtype=torch.int32, device="cuda")
+    check(q, k, v, table, lens, Hk, 4, seqs=seqs)
+    out = atk.quantized_attention(q, k, v, table, lens, Hk, seqs=seqs)   # (the same plan: the same bits)
+    wide = torch.full((T, B, H + 3, D + 16), float("nan"), dtype=dtype, device="cuda")
+    view = wide[:, :, 1:H + 1, 16:].transpose(0, 1)
+    view.copy_(q)
+    wide_out = torch.zeros((B, T, 2 * H, D), dtype=dtype, device="cuda")
+    table2 = torch.full((5, table.shape[1] + 7), -1, dtype=torch.int32, device="cuda")[:, 3:3 + table.shape[1]]
+    table2.copy_(table)
+    got = atk.quantized_attention(view, k, v, table2, lens, Hk, seqs=seqs, out=wide_out[:, :, ::2])
+    assert torch.equal(got, out) and (wide_out[:, :, 1::2] == 0).all()
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_what_is_not_visible_has_no_influence(bits, dtype):
+    """Keys and values of NaN and infinity that only the later of a sequence's queries see."""
+    B, T, H, Hk, D, ps = 2, 6, 4, 1, 64, 16
+    q, k, v, table, lens = make(B, T, H, Hk, D, [45, 37], ps, dtype, bits, seed=7)
+    codes = Hk * D * bits // 8
+    t = table.cpu().numpy()
+    for b, n in ((0, 45), (1, 37)):
+        for j, byte in ((n - 1, 255), (n - 3, 254)):         # NaN; numbers that no type but f32 has (some past it)
+            v[t[b, j // ps], j % ps, codes:] = byte
+    k[t[0, 44 // ps], 44 % ps, codes:] = 255
+    q[:, 4:] = 0    # (scores of the sequences' last queries are finite, but for those with a key of NaN)
+    kv = [torch.from_numpy(oracle.decode(p.cpu().numpy(), Hk, D, bits)).to(dtype).double().numpy() for p in (k, v)]
+    want = plain.attention(q.double().cpu().numpy(), *kv, t, lens.cpu().numpy(), 0, None, D ** -0.5)[0]
+    for keys in (0, 3000):
+        out = atk.quantized_attention(q, k, v, wider(table, ps, keys), lens, Hk, bits=bits).double().cpu().numpy()
+        # (f32 weights are sums of three, one of which may be 0: units that are never written stand for infinities, for which the header allows NaN in f32)
+        assert np.array_equal(np.isfinite(out), np.isfinite(want))
+        assert dtype == torch.float32 or np.array_equal(out[np.isinf(want)], want[np.isinf(want)])
+        assert np.isfinite(out[:, :3]).all() and np.isnan(out[:, 5]).all()
+        fine = np.isfinite(want)
+        tol = 2.0 ** -6 if dtype != torch.float32 else 2.0 ** -16   # (that they are not touched is the point)
+        assert (np.abs(out - want)[fine] <= tol * np.maximum(1, np.abs(want[fine]))).all()
+
+
+def test_reports_and_bad_pages():
+    q, k, v, table, lens = make(2, 1, 4, 2, 64, [60, 40], 16, torch.bfloat16, 4, seed=9)
+    for keys in (0, 3000):
+        wide = wider(table, 16, keys)
+        status = torch.zeros((1,), dtype=torch.int32, device="cuda")
+        bad = wide.clone()
+        bad[0, 1] = 1 << 30
+        out, lse = atk.quantized_attention(q, k, v, bad, lens, 2, status=status, return_lse=True)
+        assert status.item() == atk.ATK_STATUS_BAD_PAGE
+        # the same as without that page's keys
+        less = wide.clone()
+        less[0, 1:3] = wide[0, 2:4]
+        less[0, 3] = -1
+        want, wlse = atk.quantized_attention(q, k, v, less, torch.tensor([44, 40], dtype=torch.int32, device="cuda"), 2, return_lse=True)
+        assert torch.allclose(out.float(), want.float(), atol=2.0 ** -6, rtol=2.0 ** -6) and torch.allclose(lse, wlse, atol=1e-5)
+        for seqs, lengths, told in (([0, 7], [60, 40], atk.ATK_STATUS_BAD_SEQ), ([0, 1], [60, -3], atk.ATK_STATUS_BAD_LEN)):
+            status.zero_()
+            out, lse = atk.quantized_attention(q, k, v, wide, torch.tensor(lengths, dtype=torch.int32, device="cuda"), 2, seqs=torch.tensor(seqs, dtype=torch.int32, device="cuda"),
+                                               return_lse=True, status=status)
+            assert status.item() == told and (out[1] == 0).all() and (lse[1] == -float("inf")).all() and torch.isfinite(lse[0]).all()
+    # a length past the row's pages counts as all of them
+    full = make(1, 1, 4, 2, 64, [64], 16, torch.bfloat16, 4, seed=10, spare=0)
+    status = torch.zeros((1,), dtype=torch.int32, device="cuda")
+    want = atk.quantized_attention(*full, 2)
+    got = atk.quantized_attention(*full[:4], torch.tensor([1 << 29], dtype=torch.int32, device="cuda"), 2, status=status)
+    assert torch.equal(got, want) and status.item() == atk.ATK_STATUS_BAD_LEN
+
+
+def test_far_pages():
+    """A pool of more than 2^32 bytes, whose last pages are read."""
+    Hk, D, ps = 8, 256, 64
+    size = atk.quantized_token_bytes(Hk, D, 8)
+    pages = (1 << 32) // (size * ps) + 40
+    lens = [150]
+    q, k, v, table, n = make(1, 1, 16, Hk, D, lens, ps, torch.bfloat16, 8, seed=11)
+    want = atk.quantized_attention(q, k, v, table, n, Hk, bits=8)
+    far = []
+    for pool in (k, v):
+        x = torch.empty((pages, ps, size), dtype=torch.uint8, device="cuda")
+        x[-pool.shape[0]:] = pool
+        far.append(x)
+    moved = torch.where(table >= 0, table + (pages - k.shape[0]), table).int()
+    assert torch.equal(atk.quantized_attention(q, *far, moved, n, Hk, bits=8), want)
+
+
+def test_nothing_and_refusals():
+    q, k, v, table, lens = make(2, 1, 4, 2, 64, [60, 40], 16, torch.bfloat16, 4, seed=12)
+    assert atk.quantized_attention(q[:0], k, v, table, lens, 2).shape == (0, 1, 4, 64)
+    out, lse = atk.quantized_attention(q, k[:0], v[:0], table, lens, 2, return_lse=True)
+    assert (out == 0).all() and (lse == -float("inf")).all()
+    for args, kw, error in (((q, k, v, table, lens, 3), {}, ValueError), ((q, k, v, table, lens, 2), dict(bits=8), ValueError), ((q, k, v[:1], table, lens, 2), {}, ValueError),
+                            ((q, k.view(torch.int8), v, table, lens, 2), {}, TypeError), ((q, k, v, table.long(), lens, 2), {}, ValueError), ((q, k, v, table, lens.long(), 2), {}, TypeError),
+                            ((q, k, v, table, lens, 2), dict(scale=0.0), atk.ApproxTopkError), ((q, k, v, table, lens, 2), dict(scale=-1.0), atk.ApproxTopkError),
+                            ((q, k, v, table, lens, 2), dict(out=torch.empty_like(q).float()), ValueError), ((q.cpu(), k, v, table, lens, 2), {}, ValueError),
+                            ((q, k, v, table[:1], lens[:1], 2), {}, ValueError), ((q, k, v, table, lens, 0), {}, atk.ApproxTopkError)):
+        with pytest.raises(error):
+            atk.quantized_attention(*args, **kw)
+
+
+def test_captured_streams_and_order():
+    """The same bits from every call: replayed with other inputs, on another stream, twice at once."""
+    B, T, H, Hk, D = 4, 2, 8, 2, 128
+    q, k, v, table, lens = make(B, T, H, Hk, D, [900, 1300, 64, 7], 16, torch.bfloat16, 4, seed=13)
+    table = wider(table, 16, 8000)
+    q2 = torch.flip(q, (0,)).contiguous()
+    want, want2 = atk.quantized_attention(q, k, v, table, lens, Hk), atk.quantized_attention(q2, k, v, table, lens, Hk)
+    graphs, inputs, outs = [], [], []
+    for _ in range(2):
+        x = q.clone()
+        atk.quantized_attention(x, k, v, table, lens, Hk)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(atk.quantized_attention(x, k, v, table, lens, Hk))
+        graphs.append(graph)
+        inputs.append(x)
+    side = torch.cuda.Stream()
+    for step in range(4):
+        inputs[0].copy_(q2 if step % 2 else q)
+        graphs[0].replay()
+        graphs[1].replay()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            other = atk.quantized_attention(q, k, v, table, lens, Hk)
+        here = atk.quantized_attention(q2, k, v, table, lens, Hk)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], want2 if step % 2 else want) and torch.equal(outs[1], want) and torch.equal(other, want) and torch.equal(here, want2)
