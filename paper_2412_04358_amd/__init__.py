@@ -48,3 +48,4 @@ from .quantized import (  # noqa: F401
     quantized_token_bytes,
     read_quantized,
 )
+from .scores import token_logprobs, token_logprobs_grad  # noqa: F401

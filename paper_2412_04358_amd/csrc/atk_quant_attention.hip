@@ -32,6 +32,7 @@ static int check_quant(const atk_quant_attention_args *p, bool pointers) {
     for (int i = 0; i < 3; ++i) {
         if (p->q_stride[i] < 0 || p->out_stride[i] < 0) return ATK_ERR_ARGS;
         if (rows[i] > 1 && (p->q_stride[i] % piece || p->out_stride[i] % piece)) return ATK_ERR_ALIGN;
+        if (rows[i] > 1 && p->out_stride[i] < p->dim) return ATK_ERR_ARGS;  // (rows over each other)
     }
     if (pointers) {
         if (!p->q || !p->k || !p->v || !p->out || !p->page_table || !p->lens) return ATK_ERR_NULL_PTR;
