@@ -97,8 +97,12 @@ struct QuantRaw {
     uint32_t k[2][NC][kPieceWords], ku[2][NC], v[8][kVWords], vu[8];
 };
 
-template <int ELT, int BITS, int DP, int RT, bool JOIN>
-__global__ __launch_bounds__(64 * kQuantWaves) void quant_attn_kernel(const QuantAttnDev d) {
+// Wavefronts of a SIMD, which share its registers.
+constexpr int quant_waves(int elt, int dp, int rt) { return rt == 1 ? (dp == 64 ? 4 : dp == 128 ? (elt == ATK_F32 ? 2 : 3) : 2) : rt == 2 && dp <= 128 ? 2 : 1; }
+
+// FULL: heads of DP elements.  Shorter ones: what lies behind them is read at their first elements, and counts as 0 in keys; of values it goes into sums that are not written.
+template <int ELT, int BITS, int DP, int RT, bool JOIN, bool FULL>
+__global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void quant_attn_kernel(const QuantAttnDev d) {
     typedef AttnElt<ELT> E;
     constexpr int PE = quant_products(ELT), PARTS = quant_parts(ELT);
     typedef AttnElt<PE> P;
@@ -106,7 +110,7 @@ __global__ __launch_bounds__(64 * kQuantWaves) void quant_attn_kernel(const Quan
     constexpr int NT = DP / 16, NS = DP / 32;       // products along d of the second product, of the first
     constexpr int TK = 32, NW = kQuantWaves;
     const AttnDev &a = d.a;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, g = lane >> 4;
 
     // workgroups of a chunk are 8 apart, which is how they come to one XCD
@@ -130,6 +134,12 @@ __global__ __launch_bounds__(64 * kQuantWaves) void quant_attn_kernel(const Quan
     const int ka = (int)min((int64_t)end, (int64_t)split * range), kb = min(end, ka + range);
     const int32_t *table_row = a.table + max(s_row, 0) * a.table_stride;
 
+    // first what the keys' addresses wait for.  lane j (and the one 32 behind it) looks key k0 + j up; keys past the end are read as the last one and masked
+    constexpr int kStep = JOIN ? NW * TK : TK;
+    const int first = ka + (JOIN ? wave * TK : 0);
+    auto page_of = [&](int k0) { return table_row[a.page.div(min(k0 + (lane & 31), kb - 1))]; };
+    int page_next = first < kb ? page_of(first) : 0;
+
     QuantQuery<ELT> q[RT][NS];
     int lim[RT];
     int min_lim = kb;
@@ -145,7 +155,7 @@ __global__ __launch_bounds__(64 * kQuantWaves) void quant_attn_kernel(const Quan
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             const int dim = (s / Raw::kPieceSteps * 4 + g) * Raw::kPieceDims + s % Raw::kPieceSteps * 8;
-            if (dim < a.dim)
+            if (FULL || dim < a.dim)
                 q[rt][s].load(p + dim * E::kBytes);
             else
                 q[rt][s].clear();
@@ -162,91 +172,129 @@ __global__ __launch_bounds__(64 * kQuantWaves) void quant_attn_kernel(const Quan
 #pragma unroll
         for (int i = 0; i < NT; ++i) acc[rt][i] = f32x4{0, 0, 0, 0};
     }
-    const char *kc = (const char *)a.k + h * d.head_codes, *vc = (const char *)a.v + h * d.head_codes;
-    const char *ku = (const char *)a.k + d.code_bytes + h * d.head_units, *vu = (const char *)a.v + d.code_bytes + h * d.head_units;
 
-    // lane j (and the one 32 behind it) looks key k0 + j up; keys past the end are read as the last one and masked
-    constexpr int kStep = JOIN ? NW * TK : TK;
-    auto page_of = [&](int k0) { return table_row[a.page.div(min(k0 + (lane & 31), kb - 1))]; };
+    // a lane's places in a row: of its pieces of a key, of its elements of a value
+    const int v_dim = FULL || n * (DP / 16) < a.dim ? n * (DP / 16) : 0;
+    const char *kc[Raw::NC], *ku[Raw::NC];
+    bool inside[Raw::NC];
+#pragma unroll
+    for (int c = 0; c < Raw::NC; ++c) {
+        int dim = (c * 4 + g) * Raw::kPieceDims;
+        inside[c] = FULL || dim < a.dim;
+        if (!inside[c]) dim = 0;
+        kc[c] = (const char *)a.k + h * d.head_codes + dim * BITS / 8, ku[c] = (const char *)a.k + d.code_bytes + h * d.head_units + dim / kMxBlock;
+    }
+    const char *vc = (const char *)a.v + h * d.head_codes + v_dim * BITS / 8, *vu = (const char *)a.v + d.code_bytes + h * d.head_units + v_dim / kMxBlock;
+
     uint32_t valid = 0;
-    auto places = [&](int k0, int page, uint32_t *place) {
+    auto places = [&](int k0, int page) {  // a key's row in 16 bytes
         const bool good = (unsigned)page < (unsigned)a.n_pages;
         bad_page |= !good;
         valid = (uint32_t)__ballot(good);
-        *place = ((uint32_t)(good ? page : 0) * a.page.d + (uint32_t)a.page.mod(min(k0 + (lane & 31), kb - 1))) * d.row16;
+        return ((uint32_t)(good ? page : 0) * a.page.d + (uint32_t)a.page.mod(min(k0 + (lane & 31), kb - 1))) * d.row16;
     };
-    auto load = [&](uint32_t place, Raw &x) {
+    Raw raw;
+    auto load_k = [&](uint32_t place) {
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
             const uint64_t row = (uint64_t)(uint32_t)__shfl((int)place, y * 16 + n, 64) << 4;
 #pragma unroll
             for (int c = 0; c < Raw::NC; ++c) {
-                const int dim = (c * 4 + g) * Raw::kPieceDims;
-                if (dim < a.dim) {
-                    const char *p = kc + row + dim * BITS / 8;
-                    if constexpr (Raw::kPieceWords == 4) {
-                        const u32x4 t = *(const u32x4 *)p;
+                if constexpr (Raw::kPieceWords == 4) {
+                    const u32x4 t = *(const u32x4 *)(kc[c] + row);
 #pragma unroll
-                        for (int z = 0; z < 4; ++z) x.k[y][c][z] = t[z];
-                    } else {
-                        const u32x2 t = *(const u32x2 *)p;
-                        x.k[y][c][0] = t[0], x.k[y][c][1] = t[1];
-                    }
-                    x.ku[y][c] = (uint8_t)ku[row + dim / kMxBlock];
+                    for (int z = 0; z < 4; ++z) raw.k[y][c][z] = t[z];
                 } else {
-                    x.ku[y][c] = 0;
-#pragma unroll
-                    for (int z = 0; z < Raw::kPieceWords; ++z) x.k[y][c][z] = 0;
+                    const u32x2 t = *(const u32x2 *)(kc[c] + row);
+                    raw.k[y][c][0] = t[0], raw.k[y][c][1] = t[1];
                 }
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint64_t row = (uint64_t)(uint32_t)__shfl((int)place, (j / 4) * 16 + g * 4 + j % 4, 64) << 4;
-            const int dim = n * (DP / 16);
-            if (dim < a.dim) {
-                const char *p = vc + row + n * Raw::kVBytes;
-                if constexpr (Raw::kVBytes == 2) {
-                    x.v[j][0] = *(const uint16_t *)p;
-                } else if constexpr (Raw::kVBytes == 4) {
-                    x.v[j][0] = *(const uint32_t *)p;
-                } else if constexpr (Raw::kVBytes == 8) {
-                    const u32x2 t = *(const u32x2 *)p;
-                    x.v[j][0] = t[0], x.v[j][1] = t[1];
-                } else {
-                    const u32x4 t = *(const u32x4 *)p;
-#pragma unroll
-                    for (int z = 0; z < 4; ++z) x.v[j][z] = t[z];
-                }
-                x.vu[j] = (uint8_t)vu[row + dim / kMxBlock];
-            } else {
-                x.vu[j] = 0;
-#pragma unroll
-                for (int z = 0; z < Raw::kVWords; ++z) x.v[j][z] = 0;
+                raw.ku[y][c] = *(const uint8_t *)(ku[c] + row);
             }
         }
     };
-
-    const int first = ka + (JOIN ? wave * TK : 0);
-    Raw raw;
-    int page_next = 0;
-    if (first < kb) {
-        uint32_t place;
-        places(first, page_of(first), &place);
-        page_next = page_of(first + kStep);
-        load(place, raw);
-    }
-    for (int k0 = first; k0 < kb; k0 += kStep) {
-        // operands, and then the next tile's loads into the registers that they came from
-        u32x4 kf[2][NS];
+    auto load_v = [&](uint32_t place) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int j = 0; j < 8; ++j) {
+            const uint64_t row = (uint64_t)(uint32_t)__shfl((int)place, (j / 4) * 16 + g * 4 + j % 4, 64) << 4;
+            const char *p = vc + row;
+            if constexpr (Raw::kVBytes == 2) {
+                raw.v[j][0] = *(const uint16_t *)p;
+            } else if constexpr (Raw::kVBytes == 4) {
+                raw.v[j][0] = *(const uint32_t *)p;
+            } else if constexpr (Raw::kVBytes == 8) {
+                const u32x2 t = *(const u32x2 *)p;
+                raw.v[j][0] = t[0], raw.v[j][1] = t[1];
+            } else {
+                const u32x4 t = *(const u32x4 *)p;
 #pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const int c = s / Raw::kPieceSteps;
-                kf[x][s] = __builtin_bit_cast(u32x4, mx_eight<PE, BITS>(&raw.k[x][c][s % Raw::kPieceSteps * Raw::kStepWords], mx_unit(raw.ku[x][c])));
+                for (int z = 0; z < 4; ++z) raw.v[j][z] = t[z];
             }
-        VRows<PE, DP> v;
+            raw.vu[j] = *(const uint8_t *)(vu + row);
+        }
+    };
+
+    // S^T of a tile
+    f32x4 s[RT][2];
+    auto scores = [&]() {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) s[rt][x] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < NS; ++c) {
+                const int piece = c / Raw::kPieceSteps;
+                u32x4 kf = __builtin_bit_cast(u32x4, mx_eight<PE, BITS>(&raw.k[x][piece][c % Raw::kPieceSteps * Raw::kStepWords], mx_unit(raw.ku[x][piece])));
+                if (!FULL && !inside[piece]) kf = u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int y = PARTS - 1; y >= 0; --y) s[rt][x] = P::mma(kf, q[rt][c].w[y], s[rt][x]);
+            }
+        }
+    };
+    auto hide = [&](int k0, uint32_t now) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int at = x * 16 + g * 4 + j;
+                    if (k0 + at >= lim[rt] || !(now >> at & 1)) s[rt][x][j] = kNoMax;
+                }
+    };
+    // weights, and their sums
+    auto weigh = [&](QuantWeights<ELT> *p, float *sums) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const float zero = m[rt] == kNoMax ? 0.0f : m[rt];
+            const float ref = zero * a.scale2 - E::kBias;
+            if (far) {
+                asm volatile("");  // (a branch, no selections)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[rt][x][j] = fmaf(s[rt][x][j] - zero, a.scale2, E::kBias);
+            } else {
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[rt][x][j] = fmaf(s[rt][x][j], a.scale2, -ref);
+            }
+            float sum = 0.0f;
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[rt][x][j] = __builtin_amdgcn_exp2f(s[rt][x][j]);
+                    sum += s[rt][x][j];
+                }
+            sums[rt] = sum;
+            p[rt].set(s[rt]);
+        }
+    };
+    VRows<PE, DP> v;
+    auto values = [&]() {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float unit = mx_unit(raw.vu[j]);
@@ -262,38 +310,49 @@ __global__ __launch_bounds__(64 * kQuantWaves) void quant_attn_kernel(const Quan
                 v.w[j][1] = mx_pair<PE, BITS, 1>(raw.v[j], unit);
             }
         }
-        const uint32_t now = valid;
-        if (k0 + kStep < kb) {
-            uint32_t place;
-            places(k0 + kStep, page_next, &place);
-            page_next = page_of(k0 + 2 * kStep);
-            load(place, raw);
-        }
-        f32x4 s[RT][2];
+    };
+    // Whether row j of a lane's values may hold a number that is not finite: by the unit, or e4m3's NaN.
+    auto odd_row = [&](int j) {
+        bool odd = raw.vu[j] >= (PE == ATK_F16 ? 141u : 253u) - (BITS == 8 ? 6u : 0u);
+        if constexpr (BITS == 8) {
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                s[rt][x] = f32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int c = 0; c < NS; ++c)
-#pragma unroll
-                    for (int y = PARTS - 1; y >= 0; --y) s[rt][x] = P::mma(kf[x][c], q[rt][c].w[y], s[rt][x]);
+            for (int z = 0; z < Raw::kVWords; ++z) {
+                const uint32_t x = ~raw.v[j][z] & 0x7f7f7f7fu;  // a byte of 0: NaN
+                odd |= ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
             }
-        const bool masked = k0 + TK > min_lim || now != 0xffffffffu;
-        bool apart = false;  // a value that is not finite beside a mask: 0 * it would not be 0
-        if (masked) {
+        }
+        return odd;
+    };
+    auto drop_row = [&](int j) {
+        raw.vu[j] = kMxLeast;
+#pragma unroll
+        for (int z = 0; z < Raw::kVWords; ++z) raw.v[j][z] = 0;
+    };
+
+    bool apart = false;  // rows of values that are not finite were left out, as 0 * them would not be 0 for queries that do not see them
+    if (first < kb) {
+        const uint32_t place = places(first, page_next);
+        page_next = page_of(first + kStep);
+        load_k(place);
+        load_v(place);
+    }
+    for (int k0 = first; k0 < kb; k0 += kStep) {
+        // a tile's loads go out when the registers that they come to are free, a tile ahead
+        const bool more = k0 + kStep < kb;
+        const uint32_t now = valid;
+        uint32_t place = 0;
+        if (more) {
+            place = places(k0 + kStep, page_next);
+            page_next = page_of(k0 + 2 * kStep);
+        }
+        scores();
+        if (more) load_k(place);
+        if (k0 + TK > min_lim || now != 0xffffffffu) {
             asm volatile("");  // (a branch, no selections)
+            hide(k0, now);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int at = x * 16 + g * 4 + j;
-                        if (k0 + at >= lim[rt] || !(now >> at & 1)) s[rt][x][j] = kNoMax;
-                    }
-            apart = __any(v.any_not_finite());
+            for (int j = 0; j < 8; ++j)
+                if (odd_row(j)) apart = true, drop_row(j);
         }
         float top[RT];
         bool raise = false;
@@ -313,62 +372,63 @@ __global__ __launch_bounds__(64 * kQuantWaves) void quant_attn_kernel(const Quan
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 const float to = fmaxf(m[rt], top[rt]);
-                const float f = __builtin_amdgcn_exp2f((m[rt] - to) * a.scale2);
-                if (m[rt] != kNoMax) {  // (else nothing is kept yet)
-                    l[rt] *= f;
+                const float f = m[rt] == kNoMax ? 1.0f : __builtin_amdgcn_exp2f((m[rt] - to) * a.scale2);  // (nothing is kept yet where there was no maximum)
+                l[rt] *= f;
 #pragma unroll
-                    for (int i = 0; i < NT; ++i) acc[rt][i] *= f;
-                }
+                for (int i = 0; i < NT; ++i) acc[rt][i] *= f;
                 m[rt] = to;
                 far |= fabsf(to) < __builtin_inff() && !(fabsf(to * a.scale2) < __builtin_inff());
             }
             far = __any(far);
         }
         QuantWeights<ELT> p[RT];
+        float sums[RT];
+        weigh(p, sums);
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            const float zero = m[rt] == kNoMax ? 0.0f : m[rt];
-            const float ref = zero * a.scale2 - E::kBias;
-            float sum = 0.0f;
+        for (int rt = 0; rt < RT; ++rt) l[rt] += sums[rt];
+        values();
+        if (more) load_v(place);
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+        for (int i = 0; i < NT; ++i) {
+            const u32x4 vi = v.operand(i);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float e = __builtin_amdgcn_exp2f(far ? fmaf(s[rt][x][j] - zero, a.scale2, E::kBias) : fmaf(s[rt][x][j], a.scale2, -ref));
-                    s[rt][x][j] = e;
-                    sum += e;
-                }
-            l[rt] += sum;
-            p[rt].set(s[rt]);
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int y = PARTS - 1; y >= 0; --y) acc[rt][i] = P::mma(vi, p[rt].p[y].w, acc[rt][i]);
         }
-        if (!apart) {
+    }
+    if (__any(apart)) {
+        // what was left out, query by query with what it does not see at 0 (a product's columns are queries of their own)
+        for (int k0 = first; k0 < kb; k0 += kStep) {
+            const uint32_t place = places(k0, page_of(k0)), now = valid;
+            if (!(k0 + TK > min_lim || now != 0xffffffffu)) continue;
+            load_k(place);
+            load_v(place);
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                const u32x4 vi = v.operand(i);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                    for (int y = PARTS - 1; y >= 0; --y) acc[rt][i] = P::mma(vi, p[rt].p[y].w, acc[rt][i]);
-            }
-        } else {
-            // query by query, with the values it does not see at 0; a product's columns are queries of their own
+            for (int j = 0; j < 8; ++j)
+                if (!odd_row(j)) drop_row(j);
+            scores();
+            hide(k0, now);
+            QuantWeights<ELT> p[RT];
+            float sums[RT];
+            weigh(p, sums);
+            values();
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
                 for (int c = 0; c < 16; ++c) {
                     const int limit = __shfl(lim[rt], c, 64);
-                    VRows<PE, DP> u = v;
+                    u32x4 seen;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int at = (j / 4) * 16 + g * 4 + j % 4;
-                        if (k0 + at >= limit || !(now >> at & 1))
-#pragma unroll
-                            for (int x = 0; x < VRows<PE, DP>::kWords; ++x) u.w[j][x] = 0;
+                    for (int y = 0; y < 4; ++y) {
+                        const int at = (y / 2) * 16 + g * 4 + y % 2 * 2;
+                        seen[y] = (k0 + at < limit && (now >> at & 1) ? 0xffffu : 0u) | (k0 + at + 1 < limit && (now >> (at + 1) & 1) ? 0xffff0000u : 0u);
                     }
 #pragma unroll
                     for (int i = 0; i < NT; ++i) {
+                        const u32x4 vi = v.operand(i) & seen;
                         f32x4 t = acc[rt][i];
 #pragma unroll
-                        for (int y = PARTS - 1; y >= 0; --y) t = P::mma(u.operand(i), p[rt].p[y].w, t);
+                        for (int y = PARTS - 1; y >= 0; --y) t = P::mma(vi, p[rt].p[y].w, t);
                         if (n == c) acc[rt][i] = t;
                     }
                 }
@@ -441,7 +501,7 @@ __global__ __launch_bounds__(64 * kQuantWaves) void quant_attn_kernel(const Quan
                     const int dim = (g * 4 + j) * NT + i;
                     f32x4 o = f32x4{acc[rt][i][j] * f, acc[rt][i + 1][j] * f, acc[rt][i + 2][j] * f, acc[rt][i + 3][j] * f};
                     if (none) o = f32x4{0, 0, 0, 0};
-                    if (dim < a.dim) store_out<ELT>(out + dim * E::kBytes, o);
+                    if (FULL || dim < a.dim) store_out<ELT>(out + dim * E::kBytes, o);
                 }
             continue;
         }
@@ -452,7 +512,7 @@ __global__ __launch_bounds__(64 * kQuantWaves) void quant_attn_kernel(const Quan
 #pragma unroll
             for (int i = 0; i < NT; i += 4) {
                 const int dim = (g * 4 + j) * NT + i;
-                if (dim < a.dim) *(f32x4 *)(o + dim) = f32x4{acc[rt][i][j], acc[rt][i + 1][j], acc[rt][i + 2][j], acc[rt][i + 3][j]};
+                if (FULL || dim < a.dim) *(f32x4 *)(o + dim) = f32x4{acc[rt][i][j], acc[rt][i + 1][j], acc[rt][i + 2][j], acc[rt][i + 3][j]};
             }
     }
 }
@@ -460,11 +520,15 @@ __global__ __launch_bounds__(64 * kQuantWaves) void quant_attn_kernel(const Quan
 // Row tiles of a wavefront at most: f32's queries are three operands each.
 constexpr int quant_max_rt(int elt, int dp) { return dp == 256 ? (elt == ATK_F32 ? 1 : 2) : elt == ATK_F32 ? 2 : 4; }
 
+template <int ELT, int BITS, int DP, int RT, bool JOIN, bool FULL>
+static hipError_t launch_quant_as(const QuantAttnDev &d, hipStream_t stream) {
+    const int64_t groups = JOIN ? d.units : ((int64_t)d.units + kQuantWaves - 1) / kQuantWaves, whole = 8 * (int64_t)d.chunk;
+    hipLaunchKernelGGL((quant_attn_kernel<ELT, BITS, DP, RT, JOIN, FULL>), dim3((uint32_t)((groups + whole - 1) / whole * whole)), dim3(64 * kQuantWaves), 0, stream, d);
+    return hipGetLastError();
+}
 template <int ELT, int BITS, int DP, int RT, bool JOIN>
 static hipError_t launch_quant(const QuantAttnDev &d, hipStream_t stream) {
-    const int64_t groups = JOIN ? d.units : ((int64_t)d.units + kQuantWaves - 1) / kQuantWaves, whole = 8 * (int64_t)d.chunk;
-    hipLaunchKernelGGL((quant_attn_kernel<ELT, BITS, DP, RT, JOIN>), dim3((uint32_t)((groups + whole - 1) / whole * whole)), dim3(64 * kQuantWaves), 0, stream, d);
-    return hipGetLastError();
+    return d.a.dim == DP ? launch_quant_as<ELT, BITS, DP, RT, JOIN, true>(d, stream) : launch_quant_as<ELT, BITS, DP, RT, JOIN, false>(d, stream);
 }
 template <int ELT, int BITS, int DP>
 static hipError_t launch_quant_rt(const QuantAttnDev &d, int rt, bool join, hipStream_t stream) {
