@@ -8,9 +8,9 @@ namespace atk {
 static int64_t quant_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 struct QuantPlan {
-    int dp, rt, row_blocks, splits, chunk;
+    int dp, rt, row_blocks, ranges, chunk, pitch;
     bool join;
-    int64_t units, rows, o_bytes, bytes;
+    int64_t units, rows, o_bytes, ml_bytes, bytes;
 };
 
 static int check_quant(const atk_quant_attention_args *p, bool pointers) {
@@ -51,14 +51,17 @@ static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
     const int64_t base = p->batch * p->kv_heads * pl->row_blocks, tiles = quant_ceil(all, 32);
     // few keys: a workgroup's wavefronts share them
     pl->join = pl->rt == 1 && tiles <= 32;
-    const int64_t wanted = 16 * kNumCU;
-    pl->splits = pl->join ? 1 : (int)std::max<int64_t>(1, std::min(quant_ceil(tiles, 4), wanted / base));
-    pl->units = base * pl->splits;
+    // ranges for wavefronts that fill the chip once, if that is more than one for each sequence
+    const int64_t per_range = p->kv_heads * pl->row_blocks, wanted = 4 * kNumCU * quant_waves(p->dtype, pl->dp, pl->rt) / per_range;
+    pl->ranges = pl->join || wanted < p->batch + (p->batch + 1) / 2 || tiles <= 4 ? 0 : (int)std::min(wanted, p->batch * (1 + quant_ceil(tiles, 4)));
+    pl->units = pl->ranges ? pl->ranges * per_range : base;
     const int64_t per = pl->join ? 1 : kQuantWaves;
     pl->chunk = (int)(p->kv_heads % per ? 1 : std::min<int64_t>(p->kv_heads / per, 16));
+    pl->pitch = (int)std::min<int64_t>(rows, 16 * pl->rt);
     pl->rows = p->batch * p->tokens * p->heads;
-    pl->o_bytes = pl->splits > 1 ? pl->rows * pl->splits * p->dim * 4 : 0;
-    pl->bytes = pl->splits > 1 ? pl->o_bytes + pl->rows * pl->splits * 8 : 16;
+    pl->o_bytes = pl->ranges ? pl->units * pl->pitch * p->dim * 4 : 0;
+    pl->ml_bytes = pl->ranges ? pl->units * pl->pitch * 8 : 0;
+    pl->bytes = pl->o_bytes + pl->ml_bytes + (pl->ranges ? p->batch * 8 : 16);
     const bool fit = pl->units < (INT64_C(1) << 31) && launches(quant_ceil(pl->units, per) + 8 * pl->chunk, 64 * kQuantWaves) && launches(quant_ceil(pl->rows, 4), 256);
     return fit ? ATK_OK : ATK_ERR_ARGS;
 }
@@ -89,19 +92,18 @@ int atk_quant_attention(const atk_quant_attention_args *p, void *work, int64_t w
     a.q = p->q, a.k = p->k, a.v = p->v, a.out = p->out, a.lse = p->lse;
     a.table = p->page_table, a.lens = p->lens, a.seqs = p->seqs, a.status = p->status;
     a.parts_o = (float *)work, a.parts_ml = (float2 *)((char *)work + pl.o_bytes);
+    d.shares = (int2 *)((char *)work + pl.o_bytes + pl.ml_bytes);
     a.table_stride = p->table_stride;
     for (int i = 0; i < 3; ++i) a.qs[i] = p->q_stride[i], a.os[i] = p->out_stride[i];
     a.batch = (int)p->batch, a.tokens = (int)p->tokens, a.heads = (int)p->heads, a.kv_heads = (int)p->kv_heads;
     a.group = a.heads / a.kv_heads, a.dim = (int)p->dim;
     a.rows = (int)p->rows, a.row_pages = (int)p->row_pages, a.n_pages = (int)p->n_pages;
-    a.parts = pl.splits;
-    a.direct = pl.splits == 1;
     a.page.set((uint32_t)p->page_size);
     a.scale = (float)p->scale;
     a.scale2 = (float)(p->scale * 1.4426950408889634);
     d.row16 = (uint32_t)(mx_token_bytes(p->kv_heads, p->dim, p->bits) / 16);
     d.head_codes = (uint32_t)(p->dim * p->bits / 8), d.head_units = (uint32_t)(p->dim / kMxBlock), d.code_bytes = (uint32_t)p->kv_heads * d.head_codes;
-    d.row_blocks = pl.row_blocks, d.splits = pl.splits, d.units = (int)pl.units, d.chunk = pl.chunk;
+    d.row_blocks = pl.row_blocks, d.ranges = pl.ranges, d.units = (int)pl.units, d.chunk = pl.chunk, d.pitch = pl.pitch;
     hipStream_t s = (hipStream_t)stream;
     const hipError_t e = p->dtype == ATK_F32    ? launch_quant_f32(d, p->bits, pl.dp, pl.rt, pl.join, s)
                          : p->dtype == ATK_BF16 ? launch_quant_bf16(d, p->bits, pl.dp, pl.rt, pl.join, s)

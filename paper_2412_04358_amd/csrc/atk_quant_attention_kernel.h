@@ -9,7 +9,7 @@
 // with keys and values, which are bf16 numbers, are summed up in f32.  (f32 products take eight times as long as bf16 ones.)
 #pragma once
 
-#include "atk_attention_join.h"
+#include "atk_attention_kernel.h"
 #include "atk_mx.h"
 
 namespace atk {
@@ -17,12 +17,51 @@ namespace atk {
 constexpr int kQuantWaves = 4;
 
 struct QuantAttnDev {
-    AttnDev a;              // (of its key fields only those that the join needs)
+    AttnDev a;              // (not its plan)
     uint32_t row16;         // a token's row in 16 bytes
     uint32_t head_codes, head_units, code_bytes;
-    int row_blocks, splits, units;
+    int row_blocks, units, pitch;  // pitch: rows of a part
+    int ranges;             // of all sequences together, at most; 0: one each, and no parts
+    int2 *shares;           // [sequence]: its first range, and how many it has
     int chunk;              // workgroups next to each other that read the same keys: they go to one XCD
 };
+
+// Range `which` of all sequences': their tiles are cut into equally many for each range, so that wavefronts that all fit the chip end together whatever the lengths are (64 sequences of
+// 4096 to 8192 keys: with equally many ranges for each of them 160 us).  Every wavefront finds its own by the lengths; B sequences have at most all tiles / R + B of them.
+struct QuantRange {
+    int b, split, tiles;    // b: -1 where there are fewer ranges
+};
+__device__ __forceinline__ QuantRange quant_range(const AttnDev &a, int2 *shares, int ranges, int which, bool *bad_len, bool *bad_seq) {
+    const int lane = threadIdx.x & 63;
+    auto tiles_of = [&](int b) {
+        if (b >= a.batch) return 0;
+        return (seq_len(a, seq_row(a, b, bad_seq), bad_len) + 31) / 32;
+    };
+    int64_t total = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 64) total += tiles_of(b0 + lane);
+    for (int w = 1; w < 64; w <<= 1) total += __shfl_xor(total, w, 64);
+    const int spare = ranges - a.batch, each = (int)max((int64_t)4, (total + spare - 1) / spare);
+    QuantRange r{-1, 0, each};
+    int before = 0;
+    for (int b0 = 0; b0 < a.batch && r.b < 0; b0 += 64) {
+        const int n = b0 + lane < a.batch ? max(1, (tiles_of(b0 + lane) + each - 1) / each) : 0;
+        int up = n;
+        for (int w = 1; w < 64; w <<= 1) {
+            const int o = __shfl_up(up, w, 64);
+            if (lane >= w) up += o;
+        }
+        const int front = before + up - n;
+        const uint64_t mine = __ballot(which >= front && which < front + n);
+        if (mine) {
+            const int at = __builtin_ctzll(mine);
+            r.b = b0 + at, r.split = which - __builtin_amdgcn_readlane(front, at);
+            if (lane == at && r.split == 0) shares[r.b] = int2{front, n};  // (from one wavefront for each head and row block, all alike)
+        }
+        before = __builtin_amdgcn_readlane(front + n, 63);
+    }
+    r.b = __builtin_amdgcn_readfirstlane(r.b), r.split = __builtin_amdgcn_readfirstlane(r.split), r.tiles = __builtin_amdgcn_readfirstlane(each);
+    return r;
+}
 
 constexpr int quant_products(int elt) { return elt == ATK_F32 ? ATK_BF16 : elt; }  // type of the products' operands
 constexpr int quant_parts(int elt) { return elt == ATK_F32 ? 3 : 1; }              // operands that a number of q or a weight is the sum of
@@ -118,20 +157,23 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
     const uint32_t unit = JOIN ? block : block * NW + wave;
     if (unit >= (uint32_t)d.units) return;
     const int h = (int)(unit % (uint32_t)a.kv_heads);
-    uint32_t rest = unit / (uint32_t)a.kv_heads;
-    const int split = (int)(rest % (uint32_t)d.splits);
-    rest /= (uint32_t)d.splits;
-    const int block_of = (int)(rest % (uint32_t)d.row_blocks), b = (int)(rest / (uint32_t)d.row_blocks);
-    const int n_rows = a.tokens * a.group, r0 = block_of * 16 * RT;
-
+    const uint32_t rest = unit / (uint32_t)a.kv_heads;
+    const int block_of = (int)(rest % (uint32_t)d.row_blocks);
     bool bad_len = false, bad_seq = false, bad_page = false;
+    int b = (int)(rest / (uint32_t)d.row_blocks), split = 0, each = 0;
+    if (!JOIN && d.ranges) {
+        const QuantRange r = quant_range(a, d.shares, d.ranges, b, &bad_len, &bad_seq);
+        if (r.b < 0) return;
+        b = r.b, split = r.split, each = r.tiles;
+    }
+    const int n_rows = a.tokens * a.group, r0 = block_of * 16 * RT;
     const int s_row = seq_row(a, b, &bad_seq);
     const int len = seq_len(a, s_row, &bad_len);
-    // the keys that the block's last query sees, in ranges of whole tiles
+    // the keys that the block's last query sees
     const int last_t = (min(r0 + 16 * RT, n_rows) - 1) / a.group;
     const int end = max(0, len - (a.tokens - 1 - last_t));
-    const int range = ((end + TK - 1) / TK + d.splits - 1) / d.splits * TK;
-    const int ka = (int)min((int64_t)end, (int64_t)split * range), kb = min(end, ka + range);
+    const bool whole = JOIN || !d.ranges;
+    const int ka = whole ? 0 : (int)min((int64_t)end, (int64_t)split * each * TK), kb = whole ? end : (int)min((int64_t)end, (int64_t)ka + (int64_t)each * TK);
     const int32_t *table_row = a.table + max(s_row, 0) * a.table_stride;
 
     // first what the keys' addresses wait for.  lane j (and the one 32 behind it) looks key k0 + j up; keys past the end are read as the last one and masked
@@ -489,7 +531,7 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
         if (r >= n_rows) continue;
         const AttnRow x = attn_row(a, h, r, b);
         const int64_t row = ((int64_t)x.b * a.tokens + x.t) * a.heads + x.head;
-        if (a.direct) {  // nothing to join
+        if (whole) {  // nothing to join
             if (g == 0 && a.lse) a.lse[row] = row_lse<ELT>(a, m[rt], l[rt]);
             const float f = 1.0f / l[rt];
             const bool none = l[rt] == 0.0f;  // no key, or scores of -inf alone, whose values do not count even if they are NaN
@@ -505,8 +547,9 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
                 }
             continue;
         }
-        if (g == 0) a.parts_ml[row * a.parts + split] = float2{m[rt], l[rt]};
-        float *o = a.parts_o + (row * a.parts + split) * a.dim;
+        const int64_t part = (int64_t)unit * d.pitch + (r - r0);
+        if (g == 0) a.parts_ml[part] = float2{m[rt], l[rt]};
+        float *o = a.parts_o + part * a.dim;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -515,6 +558,74 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
                 if (FULL || dim < a.dim) *(f32x4 *)(o + dim) = f32x4{acc[rt][i][j], acc[rt][i + 1][j], acc[rt][i + 2][j], acc[rt][i + 3][j]};
             }
     }
+}
+
+// Joins the parts of a row: one wavefront, LPR lanes have four elements each, 64 / LPR parts at a time and four of those on their way.
+template <int ELT, int LPR>
+__global__ __launch_bounds__(256) void quant_join_kernel(const QuantAttnDev d, int rows_of) {
+    const AttnDev &a = d.a;
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= (int64_t)a.batch * a.tokens * a.heads) return;
+    const int head = (int)(row % a.heads);
+    const int64_t bt = row / a.heads;
+    const int b = (int)(bt / a.tokens), t = (int)(bt % a.tokens);
+    const int r = t * a.group + head % a.group, block = r / rows_of;
+    const int2 share = d.shares[b];
+    // a sequence's parts are so far apart
+    const int64_t first = (((int64_t)share.x * d.row_blocks + block) * a.kv_heads + head / a.group) * d.pitch + r % rows_of, step = (int64_t)d.row_blocks * a.kv_heads * d.pitch;
+    const float2 *ml = a.parts_ml + first;
+    float m = kNoMax;
+    for (int p = lane; p < share.y; p += 64) m = fmaxf(m, ml[p * step].x);
+    for (int w = 1; w < 64; w <<= 1) m = fmaxf(m, __shfl_xor(m, w, 64));
+    float l = 0.0f;
+    for (int p = lane; p < share.y; p += 64) {
+        const float2 x = ml[p * step];
+        l += x.y * (x.x == kNoMax ? 1.0f : __builtin_amdgcn_exp2f((x.x - m) * a.scale2));
+    }
+    for (int w = 1; w < 64; w <<= 1) l += __shfl_xor(l, w, 64);
+    const int dim = lane % LPR * 4;
+    f32x4 o = {0, 0, 0, 0};
+    if (dim < a.dim) {
+        constexpr int kStep = 64 / LPR;
+        const float *from = a.parts_o + first * a.dim + dim;
+        for (int p0 = lane / LPR; p0 < share.y; p0 += 4 * kStep) {
+            float2 x[4];
+            f32x4 v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int p = min(p0 + j * kStep, share.y - 1);
+                x[j] = ml[p * step];
+                v[j] = *(const f32x4 *)(from + p * step * a.dim);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (p0 + j * kStep >= share.y) continue;
+                const float f = x[j].x == kNoMax ? 1.0f : __builtin_amdgcn_exp2f((x[j].x - m) * a.scale2);
+                o += f * v[j];
+            }
+        }
+    }
+#pragma unroll
+    for (int w = LPR; w < 64; w <<= 1)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], w, 64);
+    if (l == 0.0f) o = f32x4{0, 0, 0, 0};  // no key, or scores of -inf alone, whose values do not count even if they are NaN
+    const float f = l == 0.0f ? 0.0f : 1.0f / l;
+    if (lane < LPR && dim < a.dim) store_out<ELT>((char *)a.out + (b * a.os[0] + t * a.os[1] + head * a.os[2] + dim) * AttnElt<ELT>::kBytes, o * f);
+    if (a.lse && lane == 0) a.lse[row] = row_lse<ELT>(a, m, l);
+}
+template <int ELT>
+static hipError_t launch_quant_join(const QuantAttnDev &d, int dp, int rt, hipStream_t stream) {
+    const int64_t rows = (int64_t)d.a.batch * d.a.tokens * d.a.heads;
+    const dim3 grid((uint32_t)((rows + 3) / 4)), threads(256);
+    if (dp == 64)
+        hipLaunchKernelGGL((quant_join_kernel<ELT, 16>), grid, threads, 0, stream, d, 16 * rt);
+    else if (dp == 128)
+        hipLaunchKernelGGL((quant_join_kernel<ELT, 32>), grid, threads, 0, stream, d, 16 * rt);
+    else
+        hipLaunchKernelGGL((quant_join_kernel<ELT, 64>), grid, threads, 0, stream, d, 16 * rt);
+    return hipGetLastError();
 }
 
 // Row tiles of a wavefront at most: f32's queries are three operands each.
@@ -542,7 +653,7 @@ template <int ELT>
 static hipError_t launch_quant_elt(const QuantAttnDev &d, int bits, int dp, int rt, bool join, hipStream_t stream) {
     hipError_t e = bits == 4 ? (dp == 64 ? launch_quant_rt<ELT, 4, 64>(d, rt, join, stream) : dp == 128 ? launch_quant_rt<ELT, 4, 128>(d, rt, join, stream) : launch_quant_rt<ELT, 4, 256>(d, rt, join, stream))
                              : (dp == 64 ? launch_quant_rt<ELT, 8, 64>(d, rt, join, stream) : dp == 128 ? launch_quant_rt<ELT, 8, 128>(d, rt, join, stream) : launch_quant_rt<ELT, 8, 256>(d, rt, join, stream));
-    if (e == hipSuccess && !d.a.direct) e = launch_join<ELT>(d.a, dp, stream);
+    if (e == hipSuccess && d.ranges) e = launch_quant_join<ELT>(d, dp, rt, stream);
     return e;
 }
 
