@@ -103,7 +103,7 @@ int atk_quant_attention(const atk_quant_attention_args *p, void *work, int64_t w
     a.scale2 = (float)(p->scale * 1.4426950408889634);
     d.row16 = (uint32_t)(mx_token_bytes(p->kv_heads, p->dim, p->bits) / 16);
     d.head_codes = (uint32_t)(p->dim * p->bits / 8), d.head_units = (uint32_t)(p->dim / kMxBlock), d.code_bytes = (uint32_t)p->kv_heads * d.head_codes;
-    d.row_blocks = pl.row_blocks, d.ranges = pl.ranges, d.units = (int)pl.units, d.chunk = pl.chunk, d.pitch = pl.pitch;
+    d.row_blocks = pl.row_blocks, d.ranges = pl.ranges, d.units = (int)pl.units, d.chunk = pl.chunk, d.pitch = pl.pitch, d.by_four = p->page_size % 4 == 0;
     hipStream_t s = (hipStream_t)stream;
     const hipError_t e = p->dtype == ATK_F32    ? launch_quant_f32(d, p->bits, pl.dp, pl.rt, pl.join, s)
                          : p->dtype == ATK_BF16 ? launch_quant_bf16(d, p->bits, pl.dp, pl.rt, pl.join, s)

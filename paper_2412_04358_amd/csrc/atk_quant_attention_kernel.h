@@ -23,6 +23,7 @@ struct QuantAttnDev {
     int row_blocks, units, pitch;  // pitch: rows of a part
     int ranges;             // of all sequences together, at most; 0: one each, and no parts
     int2 *shares;           // [sequence]: its first range, and how many it has
+    bool by_four;           // pages are whole fours of tokens
     int chunk;              // workgroups next to each other that read the same keys: they go to one XCD
 };
 
@@ -133,11 +134,15 @@ struct QuantRaw {
     static constexpr int kVBytes = DP / 16 * BITS / 8;                      // bytes of V's row
     static constexpr int kVWords = (kVBytes + 3) / 4;
     static constexpr int kPieceDims = 8 * kPieceSteps;
-    uint32_t k[2][NC][kPieceWords], ku[2][NC], v[8][kVWords], vu[8];
+    uint32_t k[2][NC][kPieceWords], ku[2][NC], v[8][kVWords], vu[8];  // ku, vu: words that the exponents lie in (bytes that go round a loop are cleared above them where they arrive, which is a wait)
 };
 
 // Wavefronts of a SIMD, which share its registers.
 constexpr int quant_waves(int elt, int dp, int rt) { return rt == 1 ? (dp == 64 ? 4 : dp == 128 ? (elt == ATK_F32 ? 2 : 3) : 2) : rt == 2 && dp <= 128 ? 2 : 1; }
+
+// Loads stay on their sides of this.  A wait for one is a number of later ones, the least over all ways to it, so page numbers, keys and values have to be asked for in one order in front of the
+// loop and in it: with page numbers last in front of it each tile waited for the next one's values (64 sequences of 4096 to 8192 keys: XXX).
+__device__ __forceinline__ void keep_loads() { __builtin_amdgcn_sched_barrier(0x78f); }
 
 // FULL: heads of DP elements.  Shorter ones: what lies behind them is read at their first elements, and counts as 0 in keys; of values it goes into sums that are not written.
 template <int ELT, int BITS, int DP, int RT, bool JOIN, bool FULL>
@@ -180,6 +185,7 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
     constexpr int kStep = JOIN ? NW * TK : TK;
     const int first = ka + (JOIN ? wave * TK : 0);
     auto page_of = [&](int k0) { return table_row[a.page.div(min(k0 + (lane & 31), kb - 1))]; };
+    const int last = first + (kb - 1 - first) / kStep * kStep;  // (of this wavefront's tiles)
     int page_next = first < kb ? page_of(first) : 0;
 
     QuantQuery<ELT> q[RT][NS];
@@ -218,28 +224,36 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
     // a lane's places in a row: of its pieces of a key, of its elements of a value
     const int v_dim = FULL || n * (DP / 16) < a.dim ? n * (DP / 16) : 0;
     const char *kc[Raw::NC], *ku[Raw::NC];
+    int ku_bit[Raw::NC];
     bool inside[Raw::NC];
+    auto unit_at = [&](int dim) { return d.code_bytes + h * d.head_units + dim / kMxBlock; };
 #pragma unroll
     for (int c = 0; c < Raw::NC; ++c) {
         int dim = (c * 4 + g) * Raw::kPieceDims;
         inside[c] = FULL || dim < a.dim;
         if (!inside[c]) dim = 0;
-        kc[c] = (const char *)a.k + h * d.head_codes + dim * BITS / 8, ku[c] = (const char *)a.k + d.code_bytes + h * d.head_units + dim / kMxBlock;
+        kc[c] = (const char *)a.k + h * d.head_codes + dim * BITS / 8, ku[c] = (const char *)a.k + (unit_at(dim) & ~3u), ku_bit[c] = 8 * (unit_at(dim) & 3);
     }
-    const char *vc = (const char *)a.v + h * d.head_codes + v_dim * BITS / 8, *vu = (const char *)a.v + d.code_bytes + h * d.head_units + v_dim / kMxBlock;
+    const char *vc = (const char *)a.v + h * d.head_codes + (v_dim * BITS / 8 & ~(Raw::kVBytes < 4 ? 3 : 0)), *vu = (const char *)a.v + (unit_at(v_dim) & ~3u);
+    const int vu_bit = 8 * (unit_at(v_dim) & 3), v_bit = Raw::kVBytes < 4 ? 8 * ((v_dim * BITS / 8) & 3) : 0;
 
     uint32_t valid = 0;
     auto places = [&](int k0, int page) {  // a key's row in 16 bytes
         const bool good = (unsigned)page < (unsigned)a.n_pages;
         bad_page |= !good;
         valid = (uint32_t)__ballot(good);
-        return ((uint32_t)(good ? page : 0) * a.page.d + (uint32_t)a.page.mod(min(k0 + (lane & 31), kb - 1))) * d.row16;
+        // (by four: a lane whose key is behind the last one may be asked for the first of four)
+        const int key = d.by_four ? k0 + (lane & 31) : min(k0 + (lane & 31), kb - 1);
+        uint32_t first_of = (uint32_t)((good ? page : 0) - a.page.div(key)) * (a.page.d * d.row16);
+        asm volatile("" : "+v"(first_of));  // (a product and a sum in one instruction of 64 bits would wait for whatever its unused half is being loaded with)
+        return first_of + (uint32_t)key * d.row16;
     };
     Raw raw;
     auto load_k = [&](uint32_t place) {
+        const uint32_t rows[2] = {(uint32_t)__shfl((int)place, n, 64), (uint32_t)__shfl((int)place, 16 + n, 64)};
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-            const uint64_t row = (uint64_t)(uint32_t)__shfl((int)place, y * 16 + n, 64) << 4;
+            const uint64_t row = (uint64_t)rows[y] << 4;
 #pragma unroll
             for (int c = 0; c < Raw::NC; ++c) {
                 if constexpr (Raw::kPieceWords == 4) {
@@ -250,18 +264,28 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
                     const u32x2 t = *(const u32x2 *)(kc[c] + row);
                     raw.k[y][c][0] = t[0], raw.k[y][c][1] = t[1];
                 }
-                raw.ku[y][c] = *(const uint8_t *)(ku[c] + row);
+                raw.ku[y][c] = *(const uint32_t *)(ku[c] + row);
             }
         }
     };
     auto load_v = [&](uint32_t place) {
+        uint32_t rows[8];
+        if (d.by_four) {  // four keys are in one page, one behind the other (those behind the last one, too: of the page, and not visible)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint32_t at = (uint32_t)__shfl((int)place, x * 16 + g * 4, 64);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) rows[x * 4 + j] = at + j * d.row16;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) rows[j] = (uint32_t)__shfl((int)place, (j / 4) * 16 + g * 4 + j % 4, 64);
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const uint64_t row = (uint64_t)(uint32_t)__shfl((int)place, (j / 4) * 16 + g * 4 + j % 4, 64) << 4;
+            const uint64_t row = (uint64_t)rows[j] << 4;
             const char *p = vc + row;
-            if constexpr (Raw::kVBytes == 2) {
-                raw.v[j][0] = *(const uint16_t *)p;
-            } else if constexpr (Raw::kVBytes == 4) {
+            if constexpr (Raw::kVBytes <= 4) {
                 raw.v[j][0] = *(const uint32_t *)p;
             } else if constexpr (Raw::kVBytes == 8) {
                 const u32x2 t = *(const u32x2 *)p;
@@ -271,7 +295,7 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
 #pragma unroll
                 for (int z = 0; z < 4; ++z) raw.v[j][z] = t[z];
             }
-            raw.vu[j] = *(const uint8_t *)(vu + row);
+            raw.vu[j] = *(const uint32_t *)(vu + row);
         }
     };
 
@@ -285,7 +309,7 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
 #pragma unroll
             for (int c = 0; c < NS; ++c) {
                 const int piece = c / Raw::kPieceSteps;
-                u32x4 kf = __builtin_bit_cast(u32x4, mx_eight<PE, BITS>(&raw.k[x][piece][c % Raw::kPieceSteps * Raw::kStepWords], mx_unit(raw.ku[x][piece])));
+                u32x4 kf = __builtin_bit_cast(u32x4, mx_eight<PE, BITS>(&raw.k[x][piece][c % Raw::kPieceSteps * Raw::kStepWords], mx_unit(raw.ku[x][piece] >> ku_bit[piece] & 0xff)));
                 if (!FULL && !inside[piece]) kf = u32x4{0, 0, 0, 0};
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
@@ -339,7 +363,7 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
     auto values = [&]() {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float unit = mx_unit(raw.vu[j]);
+            const float unit = mx_unit(raw.vu[j] >> vu_bit & 0xff);
             if constexpr (NT >= 8) {
 #pragma unroll
                 for (int x = 0; x < NT / 8; ++x) {
@@ -348,14 +372,15 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
                     for (int y = 0; y < 4; ++y) v.w[j][x * 4 + y] = t[y];
                 }
             } else {
-                v.w[j][0] = mx_pair<PE, BITS, 0>(raw.v[j], unit);
-                v.w[j][1] = mx_pair<PE, BITS, 1>(raw.v[j], unit);
+                const uint32_t w = Raw::kVBytes < 4 ? raw.v[j][0] >> v_bit : raw.v[j][0];
+                v.w[j][0] = mx_pair<PE, BITS, 0>(&w, unit);
+                v.w[j][1] = mx_pair<PE, BITS, 1>(&w, unit);
             }
         }
     };
     // Whether row j of a lane's values may hold a number that is not finite: by the unit, or e4m3's NaN.
     auto odd_row = [&](int j) {
-        bool odd = raw.vu[j] >= (PE == ATK_F16 ? 141u : 253u) - (BITS == 8 ? 6u : 0u);
+        bool odd = (raw.vu[j] >> vu_bit & 0xff) >= (PE == ATK_F16 ? 141u : 253u) - (BITS == 8 ? 6u : 0u);
         if constexpr (BITS == 8) {
 #pragma unroll
             for (int z = 0; z < Raw::kVWords; ++z) {
@@ -366,78 +391,88 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
         return odd;
     };
     auto drop_row = [&](int j) {
-        raw.vu[j] = kMxLeast;
+        raw.vu[j] = kMxLeast << vu_bit;
 #pragma unroll
         for (int z = 0; z < Raw::kVWords; ++z) raw.v[j][z] = 0;
     };
 
     bool apart = false;  // rows of values that are not finite were left out, as 0 * them would not be 0 for queries that do not see them
+    keep_loads();
     if (first < kb) {
         const uint32_t place = places(first, page_next);
-        page_next = page_of(first + kStep);
+        page_next = page_of(min(first + kStep, last));
+        keep_loads();
         load_k(place);
+        keep_loads();
         load_v(place);
-    }
-    for (int k0 = first; k0 < kb; k0 += kStep) {
-        // a tile's loads go out when the registers that they come to are free, a tile ahead
-        const bool more = k0 + kStep < kb;
-        const uint32_t now = valid;
-        uint32_t place = 0;
-        if (more) {
-            place = places(k0 + kStep, page_next);
-            page_next = page_of(k0 + 2 * kStep);
-        }
-        scores();
-        if (more) load_k(place);
-        if (k0 + TK > min_lim || now != 0xffffffffu) {
-            asm volatile("");  // (a branch, no selections)
-            hide(k0, now);
+        keep_loads();
+        int k0 = first;
+        do {  // (the one way to it is from here: see keep_loads)
+            // a tile's loads go out when the registers that they come to are free, a tile ahead (behind the last one it once more: a branch around them would cost a wait for them)
+            const uint32_t now = valid;
+            const int next = min(k0 + kStep, last);
+            const uint32_t place = places(next, page_next);
+            page_next = page_of(min(next + kStep, last));
+            keep_loads();
+            scores();
+            load_k(place);
+            keep_loads();
+            if (k0 + TK > min_lim || now != 0xffffffffu) {
+                asm volatile("");  // (a branch, no selections)
+                hide(k0, now);
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (odd_row(j)) apart = true, drop_row(j);
-        }
-        float top[RT];
-        bool raise = false;
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            float t = s[rt][0][0];
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) t = fmaxf(t, s[rt][x][j]);
-            t = fmaxf(t, __shfl_xor(t, 16, 64));
-            t = fmaxf(t, __shfl_xor(t, 32, 64));
-            top[rt] = t;
-            raise |= (t - m[rt]) * a.scale2 > kLazyMax;
-        }
-        if (__any(raise)) {
+                for (int j = 0; j < 8; ++j)
+                    if (odd_row(j)) {
+                        const int at = (j / 4) * 16 + g * 4 + j % 4;
+                        apart |= k0 + at < kb && (now >> at & 1);  // (what no query sees is nothing)
+                        drop_row(j);
+                    }
+            }
+            float top[RT];
+            bool raise = false;
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                const float to = fmaxf(m[rt], top[rt]);
-                const float f = m[rt] == kNoMax ? 1.0f : __builtin_amdgcn_exp2f((m[rt] - to) * a.scale2);  // (nothing is kept yet where there was no maximum)
-                l[rt] *= f;
+                float t = s[rt][0][0];
 #pragma unroll
-                for (int i = 0; i < NT; ++i) acc[rt][i] *= f;
-                m[rt] = to;
-                far |= fabsf(to) < __builtin_inff() && !(fabsf(to * a.scale2) < __builtin_inff());
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) t = fmaxf(t, s[rt][x][j]);
+                t = fmaxf(t, __shfl_xor(t, 16, 64));
+                t = fmaxf(t, __shfl_xor(t, 32, 64));
+                top[rt] = t;
+                raise |= (t - m[rt]) * a.scale2 > kLazyMax;
             }
-            far = __any(far);
-        }
-        QuantWeights<ELT> p[RT];
-        float sums[RT];
-        weigh(p, sums);
+            if (__any(raise)) {
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) l[rt] += sums[rt];
-        values();
-        if (more) load_v(place);
+                for (int rt = 0; rt < RT; ++rt) {
+                    const float to = fmaxf(m[rt], top[rt]);
+                    const float f = m[rt] == kNoMax ? 1.0f : __builtin_amdgcn_exp2f((m[rt] - to) * a.scale2);  // (nothing is kept yet where there was no maximum)
+                    l[rt] *= f;
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            const u32x4 vi = v.operand(i);
+                    for (int i = 0; i < NT; ++i) acc[rt][i] *= f;
+                    m[rt] = to;
+                    far |= fabsf(to) < __builtin_inff() && !(fabsf(to * a.scale2) < __builtin_inff());
+                }
+                far = __any(far);
+            }
+            QuantWeights<ELT> p[RT];
+            float sums[RT];
+            weigh(p, sums);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
+            for (int rt = 0; rt < RT; ++rt) l[rt] += sums[rt];
+            values();
+            load_v(place);
+            keep_loads();
 #pragma unroll
-                for (int y = PARTS - 1; y >= 0; --y) acc[rt][i] = P::mma(vi, p[rt].p[y].w, acc[rt][i]);
-        }
+            for (int i = 0; i < NT; ++i) {
+                const u32x4 vi = v.operand(i);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int y = PARTS - 1; y >= 0; --y) acc[rt][i] = P::mma(vi, p[rt].p[y].w, acc[rt][i]);
+            }
+            k0 += kStep;
+        } while (k0 < kb);
     }
     if (__any(apart)) {
         // what was left out, query by query with what it does not see at 0 (a product's columns are queries of their own)
