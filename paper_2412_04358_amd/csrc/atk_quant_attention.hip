@@ -8,8 +8,7 @@ namespace atk {
 static int64_t quant_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 struct QuantPlan {
-    int dp, rt, row_blocks, ranges, chunk, pitch;
-    bool join;
+    int dp, rt, row_blocks, ranges, chunk, pitch, mode, team, subtiles, row_chunks, code_chunks;
     int64_t units, rows, o_bytes, ml_bytes, bytes;
 };
 
@@ -50,17 +49,40 @@ static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
     pl->row_blocks = (int)quant_ceil(rows, 16 * pl->rt);
     const int64_t base = p->batch * p->kv_heads * pl->row_blocks, tiles = quant_ceil(all, 32);
     // few keys: a workgroup's wavefronts share them
-    pl->join = pl->rt == 1 && tiles <= 32;
+    pl->mode = pl->rt == 1 && tiles <= 32 ? kJoin : kApart;
+    pl->team = pl->subtiles = 1, pl->row_chunks = pl->code_chunks = 0;
+    const int64_t head_codes = p->dim * p->bits / 8, head_units = p->dim / kMxBlock;
+    constexpr int64_t kScan = 8192;  // sequences up to which every workgroup looks its range up among all of them
+    if (pl->mode == kApart && pl->dp * p->bits / 8 < 128 && pl->rt <= 2 && p->batch <= kScan) {
+        // heads of less than a line: rows by way of LDS
+        const int64_t teams = quant_ceil(p->kv_heads, kStagedWaves);
+        pl->mode = kStaged;
+        pl->team = (int)quant_ceil(p->kv_heads, teams);
+        pl->subtiles = kStagedWaves / pl->team;
+        pl->code_chunks = (int)(pl->team * head_codes / 16);
+        int64_t units = 1;  // pieces that a team's exponents lie in, at most
+        for (int64_t t = 0; t < teams; ++t) {
+            const int64_t from = t * pl->team * head_units, to = from + pl->team * head_units;
+            units = std::max(units, (std::min(to, p->kv_heads * head_units) + 15) / 16 - from / 16);
+        }
+        pl->row_chunks = pl->code_chunks + (int)units;
+        if (pl->row_chunks * 32 > kStagedPieces * 64 * pl->team || quant_stage_bytes(pl->row_chunks, pl->subtiles) > kStagedLds) pl->mode = kApart, pl->team = pl->subtiles = 1;
+    }
     // ranges for wavefronts that fill the chip once, if that is more than one for each sequence
-    const int64_t per_range = p->kv_heads * pl->row_blocks, wanted = 4 * kNumCU * quant_waves(p->dtype, pl->dp, pl->rt) / per_range;
-    pl->ranges = pl->join || wanted < p->batch + (p->batch + 1) / 2 || tiles <= 4 ? 0 : (int)std::min(wanted, p->batch * (1 + quant_ceil(tiles, 4)));
-    pl->units = pl->ranges ? pl->ranges * per_range : base;
-    const int64_t per = pl->join ? 1 : kQuantWaves;
-    pl->chunk = (int)(p->kv_heads % per ? 1 : std::min<int64_t>(p->kv_heads / per, 16));
+    const int64_t per_range = (pl->mode == kStaged ? quant_ceil(p->kv_heads, pl->team) : p->kv_heads) * pl->row_blocks;
+    const int64_t slots = 4 * kNumCU * quant_waves(p->dtype, pl->dp, pl->rt, pl->mode) / (pl->mode == kStaged ? pl->team * pl->subtiles : 1);
+    const int64_t wanted = slots / per_range, range_tiles = quant_ceil(tiles, pl->subtiles);
+    pl->ranges = pl->mode == kJoin || p->batch > kScan || (wanted < p->batch + (p->batch + 1) / 2 && pl->subtiles == 1) || range_tiles <= 4
+                     ? 0
+                     : (int)std::max<int64_t>(2 * p->batch, std::min(wanted, p->batch * (1 + quant_ceil(range_tiles, 4))));
+    if (pl->mode == kStaged && pl->ranges == 0 && pl->subtiles > 1) pl->ranges = (int)(2 * p->batch);
+    pl->units = pl->ranges ? pl->ranges * per_range : p->batch * per_range;
+    const int64_t per = pl->mode == kApart ? kQuantWaves : 1;
+    pl->chunk = (int)(pl->mode == kStaged ? std::min<int64_t>(quant_ceil(p->kv_heads, pl->team), 16) : p->kv_heads % per ? 1 : std::min<int64_t>(p->kv_heads / per, 16));
     pl->pitch = (int)std::min<int64_t>(rows, 16 * pl->rt);
     pl->rows = p->batch * p->tokens * p->heads;
-    pl->o_bytes = pl->ranges ? pl->units * pl->pitch * p->dim * 4 : 0;
-    pl->ml_bytes = pl->ranges ? pl->units * pl->pitch * 8 : 0;
+    const int64_t parts = (int64_t)pl->ranges * pl->subtiles * pl->row_blocks * p->kv_heads * pl->pitch;
+    pl->o_bytes = parts * p->dim * 4, pl->ml_bytes = parts * 8;
     pl->bytes = pl->o_bytes + pl->ml_bytes + (pl->ranges ? p->batch * 8 : 16);
     const bool fit = pl->units < (INT64_C(1) << 31) && launches(quant_ceil(pl->units, per) + 8 * pl->chunk, 64 * kQuantWaves) && launches(quant_ceil(pl->rows, 4), 256);
     return fit ? ATK_OK : ATK_ERR_ARGS;
@@ -104,10 +126,11 @@ int atk_quant_attention(const atk_quant_attention_args *p, void *work, int64_t w
     d.row16 = (uint32_t)(mx_token_bytes(p->kv_heads, p->dim, p->bits) / 16);
     d.head_codes = (uint32_t)(p->dim * p->bits / 8), d.head_units = (uint32_t)(p->dim / kMxBlock), d.code_bytes = (uint32_t)p->kv_heads * d.head_codes;
     d.row_blocks = pl.row_blocks, d.ranges = pl.ranges, d.units = (int)pl.units, d.chunk = pl.chunk, d.pitch = pl.pitch, d.by_four = p->page_size % 4 == 0;
+    d.team = pl.team, d.subtiles = pl.subtiles, d.row_chunks = pl.row_chunks, d.unit_from = pl.code_chunks;
     hipStream_t s = (hipStream_t)stream;
-    const hipError_t e = p->dtype == ATK_F32    ? launch_quant_f32(d, p->bits, pl.dp, pl.rt, pl.join, s)
-                         : p->dtype == ATK_BF16 ? launch_quant_bf16(d, p->bits, pl.dp, pl.rt, pl.join, s)
-                                                : launch_quant_f16(d, p->bits, pl.dp, pl.rt, pl.join, s);
+    const hipError_t e = p->dtype == ATK_F32    ? launch_quant_f32(d, p->bits, pl.dp, pl.rt, pl.mode, s)
+                         : p->dtype == ATK_BF16 ? launch_quant_bf16(d, p->bits, pl.dp, pl.rt, pl.mode, s)
+                                                : launch_quant_f16(d, p->bits, pl.dp, pl.rt, pl.mode, s);
     return e == hipSuccess ? ATK_OK : set_hip_error(e);
 }
 

@@ -1,5 +1,5 @@
 #include "atk_quant_attention_kernel.h"
 
 namespace atk {
-hipError_t launch_quant_bf16(const QuantAttnDev &d, int bits, int dp, int rt, bool join, hipStream_t stream) { return launch_quant_elt<ATK_BF16>(d, bits, dp, rt, join, stream); }
+hipError_t launch_quant_bf16(const QuantAttnDev &d, int bits, int dp, int rt, int mode, hipStream_t stream) { return launch_quant_elt<ATK_BF16>(d, bits, dp, rt, mode, stream); }
 }  // namespace atk

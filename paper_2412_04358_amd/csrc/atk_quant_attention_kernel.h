@@ -24,19 +24,21 @@ struct QuantAttnDev {
     int ranges;             // of all sequences together, at most; 0: one each, and no parts
     int2 *shares;           // [sequence]: its first range, and how many it has
     bool by_four;           // pages are whole fours of tokens
+    int team, subtiles;     // MODE kStaged: heads of a workgroup, 32 keys that it takes at a time for each of them
+    int row_chunks, unit_from;  // ... pieces of 16 bytes of a token that it brings in, how many of those are codes (behind them: the exponents)
     int chunk;              // workgroups next to each other that read the same keys: they go to one XCD
 };
 
 // Range `which` of all sequences': their tiles are cut into equally many for each range, so that wavefronts that all fit the chip end together whatever the lengths are (64 sequences of
 // 4096 to 8192 keys: with equally many ranges for each of them 160 us).  Every wavefront finds its own by the lengths; B sequences have at most all tiles / R + B of them.
 struct QuantRange {
-    int b, split, tiles;    // b: -1 where there are fewer ranges
+    int b, split, tiles;    // b: -1 where there are fewer ranges; tiles of 32 * subtiles keys
 };
-__device__ __forceinline__ QuantRange quant_range(const AttnDev &a, int2 *shares, int ranges, int which, bool *bad_len, bool *bad_seq) {
+__device__ __forceinline__ QuantRange quant_range(const AttnDev &a, int2 *shares, int ranges, int which, int subtiles, bool *bad_len, bool *bad_seq) {
     const int lane = threadIdx.x & 63;
     auto tiles_of = [&](int b) {
         if (b >= a.batch) return 0;
-        return (seq_len(a, seq_row(a, b, bad_seq), bad_len) + 31) / 32;
+        return (seq_len(a, seq_row(a, b, bad_seq), bad_len) + 32 * subtiles - 1) / (32 * subtiles);
     };
     int64_t total = 0;
     for (int b0 = 0; b0 < a.batch; b0 += 64) total += tiles_of(b0 + lane);
@@ -56,13 +58,21 @@ __device__ __forceinline__ QuantRange quant_range(const AttnDev &a, int2 *shares
         if (mine) {
             const int at = __builtin_ctzll(mine);
             r.b = b0 + at, r.split = which - __builtin_amdgcn_readlane(front, at);
-            if (lane == at && r.split == 0) shares[r.b] = int2{front, n};  // (from one wavefront for each head and row block, all alike)
+            if (lane == at && r.split == 0) shares[r.b] = int2{front * subtiles, n * subtiles};  // (from one wavefront for each head and row block, all alike)
         }
         before = __builtin_amdgcn_readlane(front + n, 63);
     }
     r.b = __builtin_amdgcn_readfirstlane(r.b), r.split = __builtin_amdgcn_readfirstlane(r.split), r.tiles = __builtin_amdgcn_readfirstlane(each);
     return r;
 }
+
+// How a workgroup's wavefronts share its work.
+enum { kApart = 0,   // each has a range of its own, for a head (workgroups' wavefronts: neighbouring heads)
+       kJoin = 1,    // they take turns at the tiles of one range, for one head, and join through LDS
+       kStaged = 2   // a range for several heads: rows come into LDS whole, a tile ahead, and a wavefront has one head's part of them
+};
+constexpr int kStagedWaves = 4, kStagedPieces = 3, kStagedLds = 80 * 1024;
+constexpr int quant_stage_bytes(int row_chunks, int subtiles) { return 4 * subtiles * 32 * row_chunks * 16; }
 
 constexpr int quant_products(int elt) { return elt == ATK_F32 ? ATK_BF16 : elt; }  // type of the products' operands
 constexpr int quant_parts(int elt) { return elt == ATK_F32 ? 3 : 1; }              // operands that a number of q or a weight is the sum of
@@ -124,6 +134,15 @@ struct QuantQuery {
     }
 };
 
+// f(0), f(1), ... f(N - 1), each number a type's.
+template <int N, int X = 0, typename F>
+__device__ __forceinline__ void each_of(F f) {
+    if constexpr (X < N) {
+        f(std::integral_constant<int, X>{});
+        each_of<N, X + 1>(f);
+    }
+}
+
 // What a lane holds of 32 keys as it lies in memory.
 template <int BITS, int DP>
 struct QuantRaw {
@@ -138,15 +157,18 @@ struct QuantRaw {
 };
 
 // Wavefronts of a SIMD, which share its registers.
-constexpr int quant_waves(int elt, int dp, int rt) { return rt == 1 ? (dp == 64 ? 4 : dp == 128 ? (elt == ATK_F32 ? 2 : 3) : 2) : rt == 2 && dp <= 128 ? 2 : 1; }
+constexpr int quant_waves(int elt, int dp, int rt, int mode) {
+    if (mode == kStaged) return rt == 1 ? (dp == 64 ? 4 : 3) - (elt == ATK_F32 ? 1 : 0) : 2;
+    return rt == 1 ? (dp == 64 ? 4 : dp == 128 ? (elt == ATK_F32 ? 2 : 3) : 2) : rt == 2 && dp <= 128 ? 2 : 1;
+}
 
 // Loads stay on their sides of this.  A wait for one is a number of later ones, the least over all ways to it, so page numbers, keys and values have to be asked for in one order in front of the
 // loop and in it: with page numbers last in front of it each tile waited for the next one's values (64 sequences of 4096 to 8192 keys: XXX).
 __device__ __forceinline__ void keep_loads() { __builtin_amdgcn_sched_barrier(0x78f); }
 
 // FULL: heads of DP elements.  Shorter ones: what lies behind them is read at their first elements, and counts as 0 in keys; of values it goes into sums that are not written.
-template <int ELT, int BITS, int DP, int RT, bool JOIN, bool FULL>
-__global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void quant_attn_kernel(const QuantAttnDev d) {
+template <int ELT, int BITS, int DP, int RT, int MODE, bool FULL>
+__global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : kQuantWaves), quant_waves(ELT, DP, RT, MODE)) void quant_attn_kernel(const QuantAttnDev d) {
     typedef AttnElt<ELT> E;
     constexpr int PE = quant_products(ELT), PARTS = quant_parts(ELT);
     typedef AttnElt<PE> P;
@@ -159,15 +181,21 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
 
     // workgroups of a chunk are 8 apart, which is how they come to one XCD
     const uint32_t at8 = blockIdx.x / 8, block = (at8 / d.chunk * 8 + blockIdx.x % 8) * d.chunk + at8 % d.chunk;
-    const uint32_t unit = JOIN ? block : block * NW + wave;
+    const uint32_t unit = MODE == kApart ? block * NW + wave : block;
     if (unit >= (uint32_t)d.units) return;
-    const int h = (int)(unit % (uint32_t)a.kv_heads);
-    const uint32_t rest = unit / (uint32_t)a.kv_heads;
+    // of a staged workgroup: the heads from h0 on, a wavefront has one of them and 32 keys of a tile
+    const int teams = MODE == kStaged ? (a.kv_heads + d.team - 1) / d.team : a.kv_heads;
+    const int h0 = (int)(unit % (uint32_t)teams) * (MODE == kStaged ? d.team : 1);
+    const int sub = MODE == kStaged ? wave / d.team : 0, member = MODE == kStaged ? wave % d.team : 0;
+    const int h = MODE == kStaged ? min(h0 + member, a.kv_heads - 1) : h0;
+    const bool idle = MODE == kStaged && h0 + member >= a.kv_heads;  // (one head too many for the last team: it helps with the loads)
+    const uint32_t rest = unit / (uint32_t)teams;
     const int block_of = (int)(rest % (uint32_t)d.row_blocks);
     bool bad_len = false, bad_seq = false, bad_page = false;
     int b = (int)(rest / (uint32_t)d.row_blocks), split = 0, each = 0;
-    if (!JOIN && d.ranges) {
-        const QuantRange r = quant_range(a, d.shares, d.ranges, b, &bad_len, &bad_seq);
+    const int range_at = b;
+    if (MODE != kJoin && d.ranges) {
+        const QuantRange r = quant_range(a, d.shares, d.ranges, b, MODE == kStaged ? d.subtiles : 1, &bad_len, &bad_seq);
         if (r.b < 0) return;
         b = r.b, split = r.split, each = r.tiles;
     }
@@ -177,13 +205,14 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
     // the keys that the block's last query sees
     const int last_t = (min(r0 + 16 * RT, n_rows) - 1) / a.group;
     const int end = max(0, len - (a.tokens - 1 - last_t));
-    const bool whole = JOIN || !d.ranges;
-    const int ka = whole ? 0 : (int)min((int64_t)end, (int64_t)split * each * TK), kb = whole ? end : (int)min((int64_t)end, (int64_t)ka + (int64_t)each * TK);
+    const bool whole = MODE == kJoin || !d.ranges;
+    const int tile = MODE == kStaged ? TK * d.subtiles : TK;
+    const int ka = whole ? 0 : (int)min((int64_t)end, (int64_t)split * each * tile), kb = whole ? end : (int)min((int64_t)end, (int64_t)ka + (int64_t)each * tile);
     const int32_t *table_row = a.table + max(s_row, 0) * a.table_stride;
 
     // first what the keys' addresses wait for.  lane j (and the one 32 behind it) looks key k0 + j up; keys past the end are read as the last one and masked
-    constexpr int kStep = JOIN ? NW * TK : TK;
-    const int first = ka + (JOIN ? wave * TK : 0);
+    const int kStep = MODE == kApart ? TK : MODE == kJoin ? NW * TK : tile;
+    const int first = ka + (MODE == kApart ? 0 : MODE == kJoin ? wave * TK : sub * TK);
     auto page_of = [&](int k0) { return table_row[a.page.div(min(k0 + (lane & 31), kb - 1))]; };
     const int last = first + (kb - 1 - first) / kStep * kStep;  // (of this wavefront's tiles)
     int page_next = first < kb ? page_of(first) : 0;
@@ -319,6 +348,7 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
         }
     };
     auto hide = [&](int k0, uint32_t now) {
+        asm volatile("");  // (a branch, no selections)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -328,6 +358,35 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
                     const int at = x * 16 + g * 4 + j;
                     if (k0 + at >= lim[rt] || !(now >> at & 1)) s[rt][x][j] = kNoMax;
                 }
+    };
+    auto raise_max = [&]() {
+        float top[RT];
+        bool raise = false;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float t = s[rt][0][0];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) t = fmaxf(t, s[rt][x][j]);
+            t = fmaxf(t, __shfl_xor(t, 16, 64));
+            t = fmaxf(t, __shfl_xor(t, 32, 64));
+            top[rt] = t;
+            raise |= (t - m[rt]) * a.scale2 > kLazyMax;
+        }
+        if (__any(raise)) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const float to = fmaxf(m[rt], top[rt]);
+                const float f = m[rt] == kNoMax ? 1.0f : __builtin_amdgcn_exp2f((m[rt] - to) * a.scale2);  // (nothing is kept yet where there was no maximum)
+                l[rt] *= f;
+#pragma unroll
+                for (int i = 0; i < NT; ++i) acc[rt][i] *= f;
+                m[rt] = to;
+                far |= fabsf(to) < __builtin_inff() && !(fabsf(to * a.scale2) < __builtin_inff());
+            }
+            far = __any(far);
+        }
     };
     // weights, and their sums
     auto weigh = [&](QuantWeights<ELT> *p, float *sums) {
@@ -359,23 +418,24 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
             p[rt].set(s[rt]);
         }
     };
-    VRows<PE, DP> v;
-    auto values = [&]() {
+    // V^T's operands of products 2 * X and 2 * X + 1: elements 2 * X and 2 * X + 1 of all eight keys, by two conversions' worth of registers at a time
+    auto operands = [&](auto x, u32x4 *o) {
+        constexpr int X = decltype(x)::value;
+        uint32_t w[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float unit = mx_unit(raw.vu[j] >> vu_bit & 0xff);
-            if constexpr (NT >= 8) {
-#pragma unroll
-                for (int x = 0; x < NT / 8; ++x) {
-                    const u32x4 t = __builtin_bit_cast(u32x4, mx_eight<PE, BITS>(&raw.v[j][x * Raw::kStepWords], unit));
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) v.w[j][x * 4 + y] = t[y];
-                }
+            if constexpr (Raw::kVBytes < 4) {
+                const uint32_t two = raw.v[j][0] >> v_bit;
+                w[j] = mx_pair<PE, BITS, X % 4>(&two, unit);
             } else {
-                const uint32_t w = Raw::kVBytes < 4 ? raw.v[j][0] >> v_bit : raw.v[j][0];
-                v.w[j][0] = mx_pair<PE, BITS, 0>(&w, unit);
-                v.w[j][1] = mx_pair<PE, BITS, 1>(&w, unit);
+                w[j] = mx_pair<PE, BITS, X % 4>(&raw.v[j][X / 4 * Raw::kStepWords], unit);
             }
+        }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            o[0][y] = __builtin_amdgcn_perm(w[2 * y + 1], w[2 * y], 0x05040100u);
+            o[1][y] = __builtin_amdgcn_perm(w[2 * y + 1], w[2 * y], 0x07060302u);
         }
     };
     // Whether row j of a lane's values may hold a number that is not finite: by the unit, or e4m3's NaN.
@@ -397,6 +457,127 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
     };
 
     bool apart = false;  // rows of values that are not finite were left out, as 0 * them would not be 0 for queries that do not see them
+    auto drop = [&](int k0, uint32_t now) {  // in tiles with a mask
+        asm volatile("");  // (a branch, no selections)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (odd_row(j)) {
+                const int at = (j / 4) * 16 + g * 4 + j % 4;
+                apart |= k0 + at < kb && (now >> at & 1);  // (what no query sees is nothing)
+                drop_row(j);
+            }
+    };
+    auto products = [&](const QuantWeights<ELT> *p) {
+        each_of<NT / 2>([&](auto x) {
+            u32x4 o[2];
+            operands(x, o);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int y = PARTS - 1; y >= 0; --y) acc[rt][2 * decltype(x)::value + i] = P::mma(o[i], p[rt].p[y].w, acc[rt][2 * decltype(x)::value + i]);
+        });
+    };
+
+    if constexpr (MODE == kStaged) {
+        // Two slots of a tile's rows, keys' and values'.  The team's wavefronts bring their 32 keys in, 16 bytes a lane, the lane's pieces of all tiles being the same ones of a row; in
+        // LDS they lie as they are counted, a row's pieces next to each other.
+        extern __shared__ char stage[];
+        const int row_bytes = d.row_chunks * 16, sub_bytes = TK * row_bytes, slot_bytes = 2 * d.subtiles * sub_bytes;
+        const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)stage;
+        int token[kStagedPieces];
+        uint32_t from[kStagedPieces];
+        bool there[kStagedPieces];
+#pragma unroll
+        for (int k = 0; k < kStagedPieces; ++k) {
+            const int i = (k * d.team + member) * 64 + lane, c = i % d.row_chunks;
+            token[k] = i / d.row_chunks & 31, there[k] = i < TK * d.row_chunks;
+            from[k] = min(d.row16 * 16 - 16, c < d.unit_from ? (uint32_t)h0 * d.head_codes + c * 16 : ((d.code_bytes + h0 * d.head_units) & ~15u) + (c - d.unit_from) * 16);  // (a last team may have fewer heads)
+        }
+        auto bring = [&](int slot, uint32_t place) {
+#pragma unroll
+            for (int k = 0; k < kStagedPieces; ++k) {
+                const uint64_t at = ((uint64_t)(uint32_t)__shfl((int)place, token[k], 64) << 4) + from[k];
+                const uint32_t to = __builtin_amdgcn_readfirstlane(lds + slot * slot_bytes + sub * sub_bytes + (k * d.team + member) * 1024);
+                if (there[k]) {
+                    load_to_lds((const char *)a.k + at, to);
+                    load_to_lds((const char *)a.v + at, to + d.subtiles * sub_bytes);
+                }
+            }
+        };
+        // a wavefront's own places in a slot
+        const char *lk[Raw::NC], *lu[Raw::NC];
+        const int unit_at0 = d.unit_from * 16 + ((d.code_bytes + h0 * d.head_units) & 15) + (h - h0) * d.head_units;
+        const char *mine = stage + sub * sub_bytes + (h - h0) * (int)d.head_codes;
+#pragma unroll
+        for (int c = 0; c < Raw::NC; ++c) {
+            const int dim = inside[c] ? (c * 4 + g) * Raw::kPieceDims : 0;
+            lk[c] = mine + n * row_bytes + dim * BITS / 8;
+            lu[c] = stage + sub * sub_bytes + n * row_bytes + ((unit_at0 + dim / kMxBlock) & ~3);
+        }
+        const char *lv = mine + d.subtiles * sub_bytes + g * 4 * row_bytes + (v_dim * BITS / 8 & ~(Raw::kVBytes < 4 ? 3 : 0)),
+                   *lvu = stage + (sub + d.subtiles) * sub_bytes + g * 4 * row_bytes + ((unit_at0 + v_dim / kMxBlock) & ~3);
+        auto read_k = [&](int slot) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int c = 0; c < Raw::NC; ++c) {
+                    const int at = slot * slot_bytes + y * 16 * row_bytes;
+                    if constexpr (Raw::kPieceWords == 4) {
+                        const u32x4 t = *(const u32x4 *)(lk[c] + at);
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) raw.k[y][c][z] = t[z];
+                    } else {
+                        const u32x2 t = *(const u32x2 *)(lk[c] + at);
+                        raw.k[y][c][0] = t[0], raw.k[y][c][1] = t[1];
+                    }
+                    raw.ku[y][c] = *(const uint32_t *)(lu[c] + at);
+                }
+        };
+        auto read_v = [&](int slot) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int at = slot * slot_bytes + (j / 4 * 16 + j % 4) * row_bytes;
+#pragma unroll
+                for (int z = 0; z < Raw::kVWords; ++z) raw.v[j][z] = ((const uint32_t *)(lv + at))[z];
+                raw.vu[j] = *(const uint32_t *)(lvu + at);
+            }
+        };
+        if (ka < kb) {
+            bring(0, places(first, page_next));
+            uint32_t now = valid;
+            page_next = page_of(min(first + kStep, kb - 1));
+            int slot = 0;
+            for (int t0 = ka; t0 < kb; t0 += kStep, slot ^= 1) {
+                const int k0 = t0 + sub * TK;
+                wait_loads<0>();
+                __syncthreads();  // the tile is there, and the other slot has been read
+                uint32_t next = 0;
+                if (t0 + kStep < kb) {
+                    bring(slot ^ 1, places(min(k0 + kStep, kb - 1), page_next));
+                    next = valid;
+                    page_next = page_of(min(k0 + 2 * kStep, kb - 1));
+                }
+                if (k0 < kb && !idle) {
+                    read_k(slot);
+                    scores();
+                    const bool masked = k0 + TK > min_lim || now != 0xffffffffu;
+                    if (masked) hide(k0, now);
+                    raise_max();
+                    QuantWeights<ELT> p[RT];
+                    float sums[RT];
+                    weigh(p, sums);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) l[rt] += sums[rt];
+                    read_v(slot);
+                    if (masked) drop(k0, now);
+                    products(p);
+                }
+                now = next;
+            }
+        }
+    } else {
     keep_loads();
     if (first < kb) {
         const uint32_t place = places(first, page_next);
@@ -417,62 +598,20 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
             scores();
             load_k(place);
             keep_loads();
-            if (k0 + TK > min_lim || now != 0xffffffffu) {
-                asm volatile("");  // (a branch, no selections)
-                hide(k0, now);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (odd_row(j)) {
-                        const int at = (j / 4) * 16 + g * 4 + j % 4;
-                        apart |= k0 + at < kb && (now >> at & 1);  // (what no query sees is nothing)
-                        drop_row(j);
-                    }
-            }
-            float top[RT];
-            bool raise = false;
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                float t = s[rt][0][0];
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) t = fmaxf(t, s[rt][x][j]);
-                t = fmaxf(t, __shfl_xor(t, 16, 64));
-                t = fmaxf(t, __shfl_xor(t, 32, 64));
-                top[rt] = t;
-                raise |= (t - m[rt]) * a.scale2 > kLazyMax;
-            }
-            if (__any(raise)) {
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    const float to = fmaxf(m[rt], top[rt]);
-                    const float f = m[rt] == kNoMax ? 1.0f : __builtin_amdgcn_exp2f((m[rt] - to) * a.scale2);  // (nothing is kept yet where there was no maximum)
-                    l[rt] *= f;
-#pragma unroll
-                    for (int i = 0; i < NT; ++i) acc[rt][i] *= f;
-                    m[rt] = to;
-                    far |= fabsf(to) < __builtin_inff() && !(fabsf(to * a.scale2) < __builtin_inff());
-                }
-                far = __any(far);
-            }
+            if (k0 + TK > min_lim || now != 0xffffffffu) hide(k0, now);
+            raise_max();
             QuantWeights<ELT> p[RT];
             float sums[RT];
             weigh(p, sums);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) l[rt] += sums[rt];
-            values();
+            if (k0 + TK > min_lim || now != 0xffffffffu) drop(k0, now);
+            products(p);
             load_v(place);
             keep_loads();
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                const u32x4 vi = v.operand(i);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                    for (int y = PARTS - 1; y >= 0; --y) acc[rt][i] = P::mma(vi, p[rt].p[y].w, acc[rt][i]);
-            }
             k0 += kStep;
         } while (k0 < kb);
+    }
     }
     if (__any(apart)) {
         // what was left out, query by query with what it does not see at 0 (a product's columns are queries of their own)
@@ -489,7 +628,6 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
             QuantWeights<ELT> p[RT];
             float sums[RT];
             weigh(p, sums);
-            values();
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
                 for (int c = 0; c < 16; ++c) {
@@ -500,17 +638,22 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
                         const int at = (y / 2) * 16 + g * 4 + y % 2 * 2;
                         seen[y] = (k0 + at < limit && (now >> at & 1) ? 0xffffu : 0u) | (k0 + at + 1 < limit && (now >> (at + 1) & 1) ? 0xffff0000u : 0u);
                     }
+                    each_of<NT / 2>([&](auto x) {
+                        u32x4 o[2];
+                        operands(x, o);
 #pragma unroll
-                    for (int i = 0; i < NT; ++i) {
-                        const u32x4 vi = v.operand(i) & seen;
-                        f32x4 t = acc[rt][i];
+                        for (int i = 0; i < 2; ++i) {
+                            constexpr int at = 2 * decltype(x)::value;
+                            f32x4 t = acc[rt][at + i];
 #pragma unroll
-                        for (int y = PARTS - 1; y >= 0; --y) t = P::mma(vi, p[rt].p[y].w, t);
-                        if (n == c) acc[rt][i] = t;
-                    }
+                            for (int y = PARTS - 1; y >= 0; --y) t = P::mma(o[i] & seen, p[rt].p[y].w, t);
+                            if (n == c) acc[rt][at + i] = t;
+                        }
+                    });
                 }
         }
     }
+    if (MODE == kStaged && idle) return;
     const int bad = (bad_page ? ATK_STATUS_BAD_PAGE : 0) | (bad_seq ? ATK_STATUS_BAD_SEQ : 0) | (bad_len ? ATK_STATUS_BAD_LEN : 0);
     if (bad && a.status) atomicOr(a.status, bad);
 
@@ -519,7 +662,7 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
         l[rt] += __shfl_xor(l[rt], 16, 64);
         l[rt] += __shfl_xor(l[rt], 32, 64);
     }
-    if constexpr (JOIN) {
+    if constexpr (MODE == kJoin) {
         // the wavefronts' ranges join in LDS, in their order
         constexpr int kPitch = DP + 4;
         __shared__ float ls_m[NW * RT * 16], ls_l[NW * RT * 16], ls_o[RT * 16 * kPitch];
@@ -582,7 +725,7 @@ __global__ __launch_bounds__(64 * kQuantWaves, quant_waves(ELT, DP, RT)) void qu
                 }
             continue;
         }
-        const int64_t part = (int64_t)unit * d.pitch + (r - r0);
+        const int64_t part = (((int64_t)range_at * (MODE == kStaged ? d.subtiles : 1) + sub) * d.row_blocks + block_of) * a.kv_heads * d.pitch + (int64_t)h * d.pitch + (r - r0);
         if (g == 0) a.parts_ml[part] = float2{m[rt], l[rt]};
         float *o = a.parts_o + part * a.dim;
 #pragma unroll
@@ -666,34 +809,49 @@ static hipError_t launch_quant_join(const QuantAttnDev &d, int dp, int rt, hipSt
 // Row tiles of a wavefront at most: f32's queries are three operands each.
 constexpr int quant_max_rt(int elt, int dp) { return dp == 256 ? (elt == ATK_F32 ? 1 : 2) : elt == ATK_F32 ? 2 : 4; }
 
-template <int ELT, int BITS, int DP, int RT, bool JOIN, bool FULL>
+template <int ELT, int BITS, int DP, int RT, int MODE, bool FULL>
 static hipError_t launch_quant_as(const QuantAttnDev &d, hipStream_t stream) {
-    const int64_t groups = JOIN ? d.units : ((int64_t)d.units + kQuantWaves - 1) / kQuantWaves, whole = 8 * (int64_t)d.chunk;
-    hipLaunchKernelGGL((quant_attn_kernel<ELT, BITS, DP, RT, JOIN, FULL>), dim3((uint32_t)((groups + whole - 1) / whole * whole)), dim3(64 * kQuantWaves), 0, stream, d);
+    const int64_t groups = MODE == kApart ? ((int64_t)d.units + kQuantWaves - 1) / kQuantWaves : d.units, whole = 8 * (int64_t)d.chunk;
+    const int threads = MODE == kStaged ? 64 * d.team * d.subtiles : 64 * kQuantWaves;
+    const size_t lds = MODE == kStaged ? (size_t)quant_stage_bytes(d.row_chunks, d.subtiles) : 0;
+    if (lds > 65536) {
+        static const hipError_t e = hipFuncSetAttribute((const void *)&quant_attn_kernel<ELT, BITS, DP, RT, MODE, FULL>, hipFuncAttributeMaxDynamicSharedMemorySize, kStagedLds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((quant_attn_kernel<ELT, BITS, DP, RT, MODE, FULL>), dim3((uint32_t)((groups + whole - 1) / whole * whole)), dim3(threads), lds, stream, d);
     return hipGetLastError();
 }
-template <int ELT, int BITS, int DP, int RT, bool JOIN>
+template <int ELT, int BITS, int DP, int RT, int MODE>
 static hipError_t launch_quant(const QuantAttnDev &d, hipStream_t stream) {
-    return d.a.dim == DP ? launch_quant_as<ELT, BITS, DP, RT, JOIN, true>(d, stream) : launch_quant_as<ELT, BITS, DP, RT, JOIN, false>(d, stream);
+    return d.a.dim == DP ? launch_quant_as<ELT, BITS, DP, RT, MODE, true>(d, stream) : launch_quant_as<ELT, BITS, DP, RT, MODE, false>(d, stream);
 }
-template <int ELT, int BITS, int DP>
-static hipError_t launch_quant_rt(const QuantAttnDev &d, int rt, bool join, hipStream_t stream) {
-    if (rt == 1) return join ? launch_quant<ELT, BITS, DP, 1, true>(d, stream) : launch_quant<ELT, BITS, DP, 1, false>(d, stream);
-    if constexpr (quant_max_rt(ELT, DP) >= 4)
-        if (rt == 4) return launch_quant<ELT, BITS, DP, 4, false>(d, stream);
-    if constexpr (quant_max_rt(ELT, DP) >= 2) return launch_quant<ELT, BITS, DP, 2, false>(d, stream);
+template <int ELT, int BITS, int DP, int MODE>
+static hipError_t launch_quant_rt(const QuantAttnDev &d, int rt, hipStream_t stream) {
+    if (rt == 1) return launch_quant<ELT, BITS, DP, 1, MODE>(d, stream);
+    if constexpr (MODE != kJoin) {
+        if constexpr (quant_max_rt(ELT, DP) >= 4 && MODE != kStaged)
+            if (rt == 4) return launch_quant<ELT, BITS, DP, 4, MODE>(d, stream);
+        if constexpr (quant_max_rt(ELT, DP) >= 2) return launch_quant<ELT, BITS, DP, 2, MODE>(d, stream);
+    }
     return hipErrorInvalidValue;
 }
+template <int ELT, int BITS, int DP>
+static hipError_t launch_quant_mode(const QuantAttnDev &d, int rt, int mode, hipStream_t stream) {
+    if (mode == kJoin) return launch_quant_rt<ELT, BITS, DP, kJoin>(d, rt, stream);
+    if constexpr (DP * BITS / 8 < 128)
+        if (mode == kStaged) return launch_quant_rt<ELT, BITS, DP, kStaged>(d, rt, stream);
+    return launch_quant_rt<ELT, BITS, DP, kApart>(d, rt, stream);
+}
 template <int ELT>
-static hipError_t launch_quant_elt(const QuantAttnDev &d, int bits, int dp, int rt, bool join, hipStream_t stream) {
-    hipError_t e = bits == 4 ? (dp == 64 ? launch_quant_rt<ELT, 4, 64>(d, rt, join, stream) : dp == 128 ? launch_quant_rt<ELT, 4, 128>(d, rt, join, stream) : launch_quant_rt<ELT, 4, 256>(d, rt, join, stream))
-                             : (dp == 64 ? launch_quant_rt<ELT, 8, 64>(d, rt, join, stream) : dp == 128 ? launch_quant_rt<ELT, 8, 128>(d, rt, join, stream) : launch_quant_rt<ELT, 8, 256>(d, rt, join, stream));
+static hipError_t launch_quant_elt(const QuantAttnDev &d, int bits, int dp, int rt, int mode, hipStream_t stream) {
+    hipError_t e = bits == 4 ? (dp == 64 ? launch_quant_mode<ELT, 4, 64>(d, rt, mode, stream) : dp == 128 ? launch_quant_mode<ELT, 4, 128>(d, rt, mode, stream) : launch_quant_mode<ELT, 4, 256>(d, rt, mode, stream))
+                             : (dp == 64 ? launch_quant_mode<ELT, 8, 64>(d, rt, mode, stream) : dp == 128 ? launch_quant_mode<ELT, 8, 128>(d, rt, mode, stream) : launch_quant_mode<ELT, 8, 256>(d, rt, mode, stream));
     if (e == hipSuccess && d.ranges) e = launch_quant_join<ELT>(d, dp, rt, stream);
     return e;
 }
 
-hipError_t launch_quant_f32(const QuantAttnDev &d, int bits, int dp, int rt, bool join, hipStream_t stream);
-hipError_t launch_quant_bf16(const QuantAttnDev &d, int bits, int dp, int rt, bool join, hipStream_t stream);
-hipError_t launch_quant_f16(const QuantAttnDev &d, int bits, int dp, int rt, bool join, hipStream_t stream);
+hipError_t launch_quant_f32(const QuantAttnDev &d, int bits, int dp, int rt, int mode, hipStream_t stream);
+hipError_t launch_quant_bf16(const QuantAttnDev &d, int bits, int dp, int rt, int mode, hipStream_t stream);
+hipError_t launch_quant_f16(const QuantAttnDev &d, int bits, int dp, int rt, int mode, hipStream_t stream);
 
 }  // namespace atk
