@@ -2,13 +2,13 @@
 
 A pool is a contiguous uint8 tensor (pages, page_size, quantized_token_bytes(kv_heads, dim, bits)): rows of e2m1 (bits 4) or e4m3 (bits 8) codes with
 a power of two for each 32 elements of a head (include/atk_quant.h has the layout and the rounding).  fork_sequences, compact_pages and copy_pages move such pools as
-they are.  Argument marshalling only, with decode.py's conventions: torch's current stream of the tensors' device, no synchronising, every call may be captured.
+they are.  Argument marshalling only (calls on plain tensors by the extension module of csrc/atk_quant_torch.cpp), with decode.py's conventions: torch's current stream of the tensors' device, no synchronising, every call may be captured.
 """
 from __future__ import annotations
 
 import ctypes
 
-from . import binding, decode
+from . import binding, decode, plain
 from .decode import _call, _ci, _dtype, _i64, _ints, _on_gpu, _seqs, _vp
 
 _lib = None
@@ -62,6 +62,8 @@ def append_quantized(tables, pools, seqs, values, bits=4):
     and float16, is quantised as it goes into pools[p] behind what the rows hold.  A token's values are contiguous, tokens and sequences strided as they like (by whole 16 bytes).
 
     Fresh pages, copies of shared pages, and all or nothing are as for append_tokens."""
+    if plain.call("append", tables._address, tables._device, pools, seqs, values, bits) is not None:
+        return
     n = _seqs(tables, seqs, None, "seqs")
     a = tables._args
     if len(values) != len(pools):
@@ -85,7 +87,7 @@ def append_quantized(tables, pools, seqs, values, bits=4):
         strides += [s[0] * v.element_size(), s[1] * v.element_size()]
     if n and tokens:
         k = len(values)
-        _call(tables.device, _lib.atk_append_quantized, a, (_vp * k)(*ptrs), (_vp * k)(*[v.data_ptr() for v in values]), (_i64 * (2 * k))(*strides), k, heads, dim, bits, code,
+        _call(tables.device, _library().atk_append_quantized, a, (_vp * k)(*ptrs), (_vp * k)(*[v.data_ptr() for v in values]), (_i64 * (2 * k))(*strides), k, heads, dim, bits, code,
               seqs.data_ptr(), n, tokens)
 
 
@@ -99,6 +101,9 @@ def read_quantized(tables, pools, seqs, starts, tokens, kv_heads, dim, bits=4, d
     code = {torch.float32: decode.ATK_F32, torch.bfloat16: decode.ATK_BF16, torch.float16: decode.ATK_F16}.get(dtype)
     if code is None:
         raise TypeError("dtype must be float32, bfloat16 or float16")
+    got = plain.call("read", tables._address, tables._device, pools, seqs, starts, tokens, kv_heads, dim, bits, code)
+    if got is not None:
+        return got
     _on_gpu(tables.device, seqs=seqs, starts=starts)
     if seqs.dim() != 1:
         raise ValueError("seqs must have one dimension")
@@ -114,7 +119,7 @@ def read_quantized(tables, pools, seqs, starts, tokens, kv_heads, dim, bits=4, d
     outs = [torch.empty((n, tokens, kv_heads, dim), dtype=dtype, device=tables.device) for _ in pools]
     if n and tokens and outs:
         k = len(outs)
-        _call(tables.device, _lib.atk_read_quantized, a, (_vp * k)(*ptrs), (_vp * k)(*[o.data_ptr() for o in outs]), k, kv_heads, dim, bits, code, seqs.data_ptr(),
+        _call(tables.device, _library().atk_read_quantized, a, (_vp * k)(*ptrs), (_vp * k)(*[o.data_ptr() for o in outs]), k, kv_heads, dim, bits, code, seqs.data_ptr(),
               None if starts is None else starts.data_ptr(), n, tokens)
     return outs
 
@@ -128,6 +133,10 @@ def quantized_attention(q, k_pages, v_pages, page_table, lens, kv_heads, bits=4,
 
     Returns out (B, T, heads, dim), with return_lse also the log of the sum of exp of the scaled scores (B, T, heads) f32: what shared_prefix_attention gives on the
     values that read_quantized gives in q's type.  A token that sees no key gets 0 and -inf."""
+    if out is None:
+        got = plain.call("attention", q, k_pages, v_pages, page_table, lens, kv_heads, bits, seqs, scale, return_lse, status)
+        if got is not None:
+            return got
     import torch
 
     if q.dim() != 4 or k_pages.dim() != 3:

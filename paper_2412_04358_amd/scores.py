@@ -1,11 +1,11 @@
 """The scores of tokens that a decoder chose: their log probabilities with the entropy and the likeliest alternatives, and the gradient of the first two.
 
-Argument marshalling only, with decode.py's conventions (include/atk_scores.h): torch's current stream of the tensors' device, no synchronising, every call may be captured.
+Argument marshalling only (calls on plain tensors by the extension module of csrc/atk_quant_torch.cpp), with decode.py's conventions (include/atk_scores.h): torch's current stream of the tensors' device, no synchronising, every call may be captured.
 There is no autograd here: the gradient is a call of its own.
 """
 from __future__ import annotations
 
-from . import binding, decode
+from . import binding, decode, plain
 from .decode import _call, _ci, _dtype, _i64, _ints, _on_gpu, _vp
 
 _lib = None
@@ -54,6 +54,9 @@ def token_logprobs(logits, tokens, top=0):
     logits (B, T, vocab) of float32, bfloat16 or float16, strided as they like but for a contiguous vocab; tokens (B, T) int32, outside of the vocabulary where there is none
     (its log probability is -inf).  Returns logprobs (B, T), entropy (B, T), lse (B, T), the log of the sum of exp of the logits, top_logprobs (B, T, top), all f32, and
     top_tokens (B, T, top) int32: the likeliest first, equally likely ones by their numbers."""
+    got = plain.call("logprobs", logits, tokens, top)
+    if got is not None:
+        return got
     import torch
 
     code, strides = _rows(logits, "logits")
@@ -82,6 +85,10 @@ def token_logprobs_grad(logits, tokens, lse, entropy, grad_logprobs, grad_entrop
 
     lse, entropy as that call gave them (entropy may be None where grad_entropy is), grad_logprobs (None: 0) and grad_entropy (B, T) float32.  Returns a tensor like logits, in `out` if given:
     of their shape and type, strided as it likes but for a contiguous vocab, the logits themselves if they are not needed any more."""
+    if out is None:
+        got = plain.call("grad", logits, tokens, lse, entropy, grad_logprobs, grad_entropy)
+        if got is not None:
+            return got
     import torch
 
     code, strides = _rows(logits, "logits")
