@@ -41,15 +41,19 @@ static int check_quant(const atk_quant_attention_args *p, bool pointers) {
     return ATK_OK;
 }
 
+constexpr int64_t kSharedRows = 97;
+
 static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
     const int64_t group = p->heads / p->kv_heads, rows = p->tokens * group, all = p->row_pages * p->page_size;
     pl->dp = p->dim <= 64 ? 64 : p->dim <= 128 ? 128 : 256;
     pl->rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     pl->rt = std::min(pl->rt, quant_max_rt(p->dtype, pl->dp));
-    pl->row_blocks = (int)quant_ceil(rows, 16 * pl->rt);
-    const int64_t base = p->batch * p->kv_heads * pl->row_blocks, tiles = quant_ceil(all, 32);
+    const int64_t tiles = quant_ceil(all, 32);
     // few keys: a workgroup's wavefronts share them
     pl->mode = pl->rt == 1 && tiles <= 32 ? kJoin : kApart;
+    if (rows >= kSharedRows && pl->dp <= 128) pl->mode = kShared, pl->rt = quant_shared_rt(p->dtype);
+    const int block_rows = 16 * pl->rt * (pl->mode == kShared ? kSharedWaves : 1);
+    pl->row_blocks = (int)quant_ceil(rows, block_rows);
     pl->team = pl->subtiles = 1, pl->row_chunks = pl->code_chunks = 0;
     const int64_t head_codes = p->dim * p->bits / 8, head_units = p->dim / kMxBlock;
     constexpr int64_t kScan = 8192;  // sequences up to which every workgroup looks its range up among all of them
@@ -70,8 +74,8 @@ static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
     }
     // ranges for wavefronts that fill the chip once, if that is more than one for each sequence
     const int64_t per_range = (pl->mode == kStaged ? quant_ceil(p->kv_heads, pl->team) : p->kv_heads) * pl->row_blocks;
-    const int64_t slots = 4 * kNumCU * quant_waves(p->dtype, pl->dp, pl->rt, pl->mode) / (pl->mode == kStaged ? pl->team * pl->subtiles : 1);
-    const int64_t wanted = slots / per_range, range_tiles = quant_ceil(tiles, pl->subtiles);
+    const int64_t slots = 4 * kNumCU * quant_waves(p->dtype, pl->dp, pl->rt, pl->mode) / (pl->mode == kStaged ? pl->team * pl->subtiles : pl->mode == kShared ? kSharedWaves : 1);
+    const int64_t wanted = (pl->mode == kShared ? 2 : 1) * slots / per_range, range_tiles = quant_ceil(tiles, pl->mode == kShared ? kSharedSubs : pl->subtiles);
     pl->ranges = pl->mode == kJoin || p->batch > kScan || (wanted < p->batch + (p->batch + 1) / 2 && pl->subtiles == 1) || range_tiles <= 4
                      ? 0
                      : (int)std::max<int64_t>(2 * p->batch, std::min(wanted, p->batch * (1 + quant_ceil(range_tiles, 4))));
@@ -79,12 +83,12 @@ static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
     pl->units = pl->ranges ? pl->ranges * per_range : p->batch * per_range;
     const int64_t per = pl->mode == kApart ? kQuantWaves : 1;
     pl->chunk = (int)(pl->mode == kStaged ? std::min<int64_t>(quant_ceil(p->kv_heads, pl->team), 16) : p->kv_heads % per ? 1 : std::min<int64_t>(p->kv_heads / per, 16));
-    pl->pitch = (int)std::min<int64_t>(rows, 16 * pl->rt);
+    pl->pitch = (int)std::min<int64_t>(rows, block_rows);
     pl->rows = p->batch * p->tokens * p->heads;
     const int64_t parts = (int64_t)pl->ranges * pl->subtiles * pl->row_blocks * p->kv_heads * pl->pitch;
     pl->o_bytes = parts * p->dim * 4, pl->ml_bytes = parts * 8;
     pl->bytes = pl->o_bytes + pl->ml_bytes + (pl->ranges ? p->batch * 8 : 16);
-    const bool fit = pl->units < (INT64_C(1) << 31) && launches(quant_ceil(pl->units, per) + 8 * pl->chunk, 64 * kQuantWaves) && launches(quant_ceil(pl->rows, 4), 256);
+    const bool fit = pl->units < (INT64_C(1) << 31) && launches(quant_ceil(pl->units, per) + 8 * pl->chunk, 64 * kSharedWaves) && launches(quant_ceil(pl->rows, 4), 256);
     return fit ? ATK_OK : ATK_ERR_ARGS;
 }
 

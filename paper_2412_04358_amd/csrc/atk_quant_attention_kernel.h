@@ -34,7 +34,7 @@ struct QuantAttnDev {
 struct QuantRange {
     int b, split, tiles;    // b: -1 where there are fewer ranges; tiles of 32 * subtiles keys
 };
-__device__ __forceinline__ QuantRange quant_range(const AttnDev &a, int2 *shares, int ranges, int which, int subtiles, bool *bad_len, bool *bad_seq) {
+__device__ __forceinline__ QuantRange quant_range(const AttnDev &a, int2 *shares, int ranges, int which, int subtiles, int parts, bool *bad_len, bool *bad_seq) {
     const int lane = threadIdx.x & 63;
     auto tiles_of = [&](int b) {
         if (b >= a.batch) return 0;
@@ -44,10 +44,10 @@ __device__ __forceinline__ QuantRange quant_range(const AttnDev &a, int2 *shares
     for (int b0 = 0; b0 < a.batch; b0 += 64) total += tiles_of(b0 + lane);
     for (int w = 1; w < 64; w <<= 1) total += __shfl_xor(total, w, 64);
     const int spare = ranges - a.batch, each = (int)max((int64_t)4, (total + spare - 1) / spare);
-    QuantRange r{-1, 0, each};
+    QuantRange r{-1, 0, 0};
     int before = 0;
     for (int b0 = 0; b0 < a.batch && r.b < 0; b0 += 64) {
-        const int n = b0 + lane < a.batch ? max(1, (tiles_of(b0 + lane) + each - 1) / each) : 0;
+        const int tiles = tiles_of(b0 + lane), n = b0 + lane < a.batch ? max(1, (tiles + each - 1) / each) : 0;
         int up = n;
         for (int w = 1; w < 64; w <<= 1) {
             const int o = __shfl_up(up, w, 64);
@@ -58,19 +58,23 @@ __device__ __forceinline__ QuantRange quant_range(const AttnDev &a, int2 *shares
         if (mine) {
             const int at = __builtin_ctzll(mine);
             r.b = b0 + at, r.split = which - __builtin_amdgcn_readlane(front, at);
-            if (lane == at && r.split == 0) shares[r.b] = int2{front * subtiles, n * subtiles};  // (from one wavefront for each head and row block, all alike)
+            r.tiles = __builtin_amdgcn_readlane(n > 0 ? (tiles + n - 1) / n : 0, at);
+            if (lane == at && r.split == 0) shares[r.b] = int2{front * parts, n * parts};  // (from one wavefront for each head and row block, all alike)
         }
         before = __builtin_amdgcn_readlane(front + n, 63);
     }
-    r.b = __builtin_amdgcn_readfirstlane(r.b), r.split = __builtin_amdgcn_readfirstlane(r.split), r.tiles = __builtin_amdgcn_readfirstlane(each);
+    r.b = __builtin_amdgcn_readfirstlane(r.b), r.split = __builtin_amdgcn_readfirstlane(r.split), r.tiles = __builtin_amdgcn_readfirstlane(r.tiles);
     return r;
 }
 
 // How a workgroup's wavefronts share its work.
 enum { kApart = 0,   // each has a range of its own, for a head (workgroups' wavefronts: neighbouring heads)
        kJoin = 1,    // they take turns at the tiles of one range, for one head, and join through LDS
-       kStaged = 2   // a range for several heads: rows come into LDS whole, a tile ahead, and a wavefront has one head's part of them
+       kStaged = 2,  // a range for several heads: rows come into LDS whole, a tile ahead, and a wavefront has one head's part of them
+       kShared = 3   // a range for one head and many queries: operands are made once, go through LDS, and each wavefront has queries of its own
 };
+constexpr int kSharedWaves = 8, kSharedSubs = 4;  // of kShared: each wavefront makes keys' or values' operands of 32 of a tile's 128 keys
+constexpr int quant_shared_bytes(int dp) { return 2 * kSharedSubs * (2 * (dp / 32) + dp / 16) * 1024 + 64; }
 constexpr int kStagedWaves = 4, kStagedPieces = 3, kStagedLds = 80 * 1024;
 constexpr int quant_stage_bytes(int row_chunks, int subtiles) { return 4 * subtiles * 32 * row_chunks * 16; }
 
@@ -158,6 +162,7 @@ struct QuantRaw {
 
 // Wavefronts of a SIMD, which share its registers.
 constexpr int quant_waves(int elt, int dp, int rt, int mode) {
+    if (mode == kShared) return 2;
     if (mode == kStaged) return rt == 1 ? (dp == 64 ? 4 : 3) - (elt == ATK_F32 ? 1 : 0) : 2;
     return rt == 1 ? (dp == 64 ? 4 : dp == 128 ? (elt == ATK_F32 ? 2 : 3) : 2) : rt == 2 && dp <= 128 ? 2 : 1;
 }
@@ -168,7 +173,7 @@ __device__ __forceinline__ void keep_loads() { __builtin_amdgcn_sched_barrier(0x
 
 // FULL: heads of DP elements.  Shorter ones: what lies behind them is read at their first elements, and counts as 0 in keys; of values it goes into sums that are not written.
 template <int ELT, int BITS, int DP, int RT, int MODE, bool FULL>
-__global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : kQuantWaves), quant_waves(ELT, DP, RT, MODE)) void quant_attn_kernel(const QuantAttnDev d) {
+__global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : MODE == kShared ? kSharedWaves : kQuantWaves), quant_waves(ELT, DP, RT, MODE)) void quant_attn_kernel(const QuantAttnDev d) {
     typedef AttnElt<ELT> E;
     constexpr int PE = quant_products(ELT), PARTS = quant_parts(ELT);
     typedef AttnElt<PE> P;
@@ -195,27 +200,29 @@ __global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : kQuantWaves)
     int b = (int)(rest / (uint32_t)d.row_blocks), split = 0, each = 0;
     const int range_at = b;
     if (MODE != kJoin && d.ranges) {
-        const QuantRange r = quant_range(a, d.shares, d.ranges, b, MODE == kStaged ? d.subtiles : 1, &bad_len, &bad_seq);
+        const QuantRange r = quant_range(a, d.shares, d.ranges, b, MODE == kStaged ? d.subtiles : MODE == kShared ? kSharedSubs : 1, MODE == kStaged ? d.subtiles : 1, &bad_len, &bad_seq);
         if (r.b < 0) return;
         b = r.b, split = r.split, each = r.tiles;
     }
-    const int n_rows = a.tokens * a.group, r0 = block_of * 16 * RT;
+    constexpr int kBlockRows = 16 * RT * (MODE == kShared ? kSharedWaves : 1);
+    const int n_rows = a.tokens * a.group, block_r0 = block_of * kBlockRows, r0 = block_r0 + (MODE == kShared ? wave * 16 * RT : 0);
     const int s_row = seq_row(a, b, &bad_seq);
     const int len = seq_len(a, s_row, &bad_len);
     // the keys that the block's last query sees
-    const int last_t = (min(r0 + 16 * RT, n_rows) - 1) / a.group;
+    const int last_t = (min(block_r0 + kBlockRows, n_rows) - 1) / a.group;
     const int end = max(0, len - (a.tokens - 1 - last_t));
     const bool whole = MODE == kJoin || !d.ranges;
-    const int tile = MODE == kStaged ? TK * d.subtiles : TK;
+    const int tile = MODE == kStaged ? TK * d.subtiles : MODE == kShared ? TK * kSharedSubs : TK;
     const int ka = whole ? 0 : (int)min((int64_t)end, (int64_t)split * each * tile), kb = whole ? end : (int)min((int64_t)end, (int64_t)ka + (int64_t)each * tile);
     const int32_t *table_row = a.table + max(s_row, 0) * a.table_stride;
 
     // first what the keys' addresses wait for.  lane j (and the one 32 behind it) looks key k0 + j up; keys past the end are read as the last one and masked
     const int kStep = MODE == kApart ? TK : MODE == kJoin ? NW * TK : tile;
-    const int first = ka + (MODE == kApart ? 0 : MODE == kJoin ? wave * TK : sub * TK);
+    const int first = ka + (MODE == kApart ? 0 : MODE == kJoin ? wave * TK : MODE == kStaged ? sub * TK : (wave % kSharedSubs) * TK);
     auto page_of = [&](int k0) { return table_row[a.page.div(min(k0 + (lane & 31), kb - 1))]; };
     const int last = first + (kb - 1 - first) / kStep * kStep;  // (of this wavefront's tiles)
-    int page_next = first < kb ? page_of(first) : 0;
+    const int last_tile = (kb - 1) & ~(TK - 1);  // (ranges begin at whole tiles)
+    int page_next = MODE == kShared ? (ka < kb ? page_of(min(first, last_tile)) : 0) : first < kb ? page_of(first) : 0;
 
     QuantQuery<ELT> q[RT][NS];
     int lim[RT];
@@ -252,19 +259,30 @@ __global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : kQuantWaves)
 
     // a lane's places in a row: of its pieces of a key, of its elements of a value
     const int v_dim = FULL || n * (DP / 16) < a.dim ? n * (DP / 16) : 0;
-    const char *kc[Raw::NC], *ku[Raw::NC];
-    int ku_bit[Raw::NC];
+    int ku_bit[Raw::NC], k_dim[Raw::NC];
     bool inside[Raw::NC];
     auto unit_at = [&](int dim) { return d.code_bytes + h * d.head_units + dim / kMxBlock; };
 #pragma unroll
     for (int c = 0; c < Raw::NC; ++c) {
-        int dim = (c * 4 + g) * Raw::kPieceDims;
-        inside[c] = FULL || dim < a.dim;
-        if (!inside[c]) dim = 0;
-        kc[c] = (const char *)a.k + h * d.head_codes + dim * BITS / 8, ku[c] = (const char *)a.k + (unit_at(dim) & ~3u), ku_bit[c] = 8 * (unit_at(dim) & 3);
+        k_dim[c] = (c * 4 + g) * Raw::kPieceDims;
+        inside[c] = FULL || k_dim[c] < a.dim;
+        if (!inside[c]) k_dim[c] = 0;
+        ku_bit[c] = 8 * (unit_at(k_dim[c]) & 3);
     }
-    const char *vc = (const char *)a.v + h * d.head_codes + (v_dim * BITS / 8 & ~(Raw::kVBytes < 4 ? 3 : 0)), *vu = (const char *)a.v + (unit_at(v_dim) & ~3u);
     const int vu_bit = 8 * (unit_at(v_dim) & 3), v_bit = Raw::kVBytes < 4 ? 8 * ((v_dim * BITS / 8) & 3) : 0;
+    // ... in memory
+    struct {
+        const char *kc[Raw::NC], *ku[Raw::NC], *vc, *vu;
+    } row_of;
+    auto find_rows = [&]() {
+#pragma unroll
+        for (int c = 0; c < Raw::NC; ++c) {
+            row_of.kc[c] = (const char *)a.k + h * d.head_codes + k_dim[c] * BITS / 8;
+            row_of.ku[c] = (const char *)a.k + (unit_at(k_dim[c]) & ~3u);
+        }
+        row_of.vc = (const char *)a.v + h * d.head_codes + (v_dim * BITS / 8 & ~(Raw::kVBytes < 4 ? 3 : 0));
+        row_of.vu = (const char *)a.v + (unit_at(v_dim) & ~3u);
+    };
 
     uint32_t valid = 0;
     auto places = [&](int k0, int page) {  // a key's row in 16 bytes
@@ -286,14 +304,14 @@ __global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : kQuantWaves)
 #pragma unroll
             for (int c = 0; c < Raw::NC; ++c) {
                 if constexpr (Raw::kPieceWords == 4) {
-                    const u32x4 t = *(const u32x4 *)(kc[c] + row);
+                    const u32x4 t = *(const u32x4 *)(row_of.kc[c] + row);
 #pragma unroll
                     for (int z = 0; z < 4; ++z) raw.k[y][c][z] = t[z];
                 } else {
-                    const u32x2 t = *(const u32x2 *)(kc[c] + row);
+                    const u32x2 t = *(const u32x2 *)(row_of.kc[c] + row);
                     raw.k[y][c][0] = t[0], raw.k[y][c][1] = t[1];
                 }
-                raw.ku[y][c] = *(const uint32_t *)(ku[c] + row);
+                raw.ku[y][c] = *(const uint32_t *)(row_of.ku[c] + row);
             }
         }
     };
@@ -313,7 +331,7 @@ __global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : kQuantWaves)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const uint64_t row = (uint64_t)rows[j] << 4;
-            const char *p = vc + row;
+            const char *p = row_of.vc + row;
             if constexpr (Raw::kVBytes <= 4) {
                 raw.v[j][0] = *(const uint32_t *)p;
             } else if constexpr (Raw::kVBytes == 8) {
@@ -324,10 +342,17 @@ __global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : kQuantWaves)
 #pragma unroll
                 for (int z = 0; z < 4; ++z) raw.v[j][z] = t[z];
             }
-            raw.vu[j] = *(const uint32_t *)(vu + row);
+            raw.vu[j] = *(const uint32_t *)(row_of.vu + row);
         }
     };
 
+    // K's operand of product c for 16 of the keys
+    auto key_operand = [&](int x, int c) {
+        const int piece = c / Raw::kPieceSteps;
+        u32x4 kf = __builtin_bit_cast(u32x4, mx_eight<PE, BITS>(&raw.k[x][piece][c % Raw::kPieceSteps * Raw::kStepWords], mx_unit(raw.ku[x][piece] >> ku_bit[piece] & 0xff)));
+        if (!FULL && !inside[piece]) kf = u32x4{0, 0, 0, 0};
+        return kf;
+    };
     // S^T of a tile
     f32x4 s[RT][2];
     auto scores = [&]() {
@@ -337,9 +362,7 @@ __global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : kQuantWaves)
             for (int rt = 0; rt < RT; ++rt) s[rt][x] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int c = 0; c < NS; ++c) {
-                const int piece = c / Raw::kPieceSteps;
-                u32x4 kf = __builtin_bit_cast(u32x4, mx_eight<PE, BITS>(&raw.k[x][piece][c % Raw::kPieceSteps * Raw::kStepWords], mx_unit(raw.ku[x][piece] >> ku_bit[piece] & 0xff)));
-                if (!FULL && !inside[piece]) kf = u32x4{0, 0, 0, 0};
+                const u32x4 kf = key_operand(x, c);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -480,7 +503,103 @@ __global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : kQuantWaves)
         });
     };
 
-    if constexpr (MODE == kStaged) {
+    int apart_lim = min_lim;  // tiles up to it have no mask for whoever made their operands
+    if constexpr (MODE == kShared) {
+        // Two slots of a tile's operands as the products take them, 16 bytes a lane.  A wavefront makes those of the next tile (from rows that it asked for a tile before), asks for the rows of
+        // the one behind it, and then has this one's products: 16 KB from LDS for 32 keys and its 32 queries (heads of 128), a third of what LDS has for the time that they take.
+        extern __shared__ char stage[];
+        constexpr int kKey = 2 * NS * 1024, kSub = kKey + NT * 1024, kSlot = kSharedSubs * kSub;
+        uint32_t *const masks = (uint32_t *)(stage + 2 * kSlot), *const any_apart = masks + 2 * kSharedSubs;
+        const int mine = wave % kSharedSubs;
+        const bool makes_values = wave >= kSharedSubs;
+        apart_lim = min(kb, len - (a.tokens - 1 - block_r0 / a.group));
+        if (threadIdx.x == 0) *any_apart = 0;
+        find_rows();
+        auto ask = [&](int t0) {
+            const uint32_t place = places(min(t0 + mine * TK, last_tile), page_next);
+            page_next = page_of(min(t0 + tile + mine * TK, last_tile));
+            if (makes_values)
+                load_v(place);
+            else
+                load_k(place);
+        };
+        auto make = [&](int t0, int slot, uint32_t now) {
+            char *const to = stage + slot * kSlot + mine * kSub + lane * 16;
+            const int k0 = t0 + mine * TK;
+            if (makes_values) {
+                if (k0 + TK > apart_lim || now != 0xffffffffu) drop(k0, now);
+                each_of<NT / 2>([&](auto x) {
+                    u32x4 o[2];
+                    operands(x, o);
+                    *(u32x4 *)(to + kKey + (2 * decltype(x)::value) * 1024) = o[0];
+                    *(u32x4 *)(to + kKey + (2 * decltype(x)::value + 1) * 1024) = o[1];
+                });
+            } else {
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int c = 0; c < NS; ++c) *(u32x4 *)(to + (x * NS + c) * 1024) = key_operand(x, c);
+                if (lane == 0) masks[slot * kSharedSubs + mine] = now;
+            }
+        };
+        const int my_end = min(kb, len - (a.tokens - 1 - (min(r0 + 16 * RT, n_rows) - 1) / a.group));
+        const bool idle_rows = r0 >= n_rows;
+        if (ka < kb) {
+            ask(ka);
+            uint32_t now = valid;
+            make(ka, 0, now);
+            ask(ka + tile);
+            now = valid;
+            __syncthreads();
+            int slot = 0;
+            for (int t0 = ka; t0 < kb; t0 += tile, slot ^= 1) {
+                if (t0 + tile < kb) {
+                    make(t0 + tile, slot ^ 1, now);
+                    ask(t0 + 2 * tile);
+                    now = valid;
+                }
+                if (!idle_rows)
+                    for (int st = 0; st < kSharedSubs; ++st) {
+                        const int k0 = t0 + st * TK;
+                        if (k0 >= my_end) break;
+                        const char *const from = stage + slot * kSlot + st * kSub + lane * 16;
+                        const uint32_t seen = masks[slot * kSharedSubs + st];
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+#pragma unroll
+                            for (int rt = 0; rt < RT; ++rt) s[rt][x] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                            for (int c = 0; c < NS; ++c) {
+                                const u32x4 kf = *(const u32x4 *)(from + (x * NS + c) * 1024);
+#pragma unroll
+                                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                                    for (int y = PARTS - 1; y >= 0; --y) s[rt][x] = P::mma(kf, q[rt][c].w[y], s[rt][x]);
+                            }
+                        }
+                        if (k0 + TK > min_lim || seen != 0xffffffffu) hide(k0, seen);
+                        raise_max();
+                        QuantWeights<ELT> p[RT];
+                        float sums[RT];
+                        weigh(p, sums);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) l[rt] += sums[rt];
+#pragma unroll
+                        for (int i = 0; i < NT; ++i) {
+                            const u32x4 vi = *(const u32x4 *)(from + kKey + i * 1024);
+#pragma unroll
+                            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                                for (int y = PARTS - 1; y >= 0; --y) acc[rt][i] = P::mma(vi, p[rt].p[y].w, acc[rt][i]);
+                        }
+                    }
+                __syncthreads();
+            }
+        }
+        if (__any(apart) && lane == 0) *any_apart = 1;
+        __syncthreads();
+        apart = *any_apart && !idle_rows;
+    } else if constexpr (MODE == kStaged) {
         // Two slots of a tile's rows, keys' and values'.  The team's wavefronts bring their 32 keys in, 16 bytes a lane, the lane's pieces of all tiles being the same ones of a row; in
         // LDS they lie as they are counted, a row's pieces next to each other.
         extern __shared__ char stage[];
@@ -512,9 +631,8 @@ __global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : kQuantWaves)
         const char *mine = stage + sub * sub_bytes + (h - h0) * (int)d.head_codes;
 #pragma unroll
         for (int c = 0; c < Raw::NC; ++c) {
-            const int dim = inside[c] ? (c * 4 + g) * Raw::kPieceDims : 0;
-            lk[c] = mine + n * row_bytes + dim * BITS / 8;
-            lu[c] = stage + sub * sub_bytes + n * row_bytes + ((unit_at0 + dim / kMxBlock) & ~3);
+            lk[c] = mine + n * row_bytes + k_dim[c] * BITS / 8;
+            lu[c] = stage + sub * sub_bytes + n * row_bytes + ((unit_at0 + k_dim[c] / kMxBlock) & ~3);
         }
         const char *lv = mine + d.subtiles * sub_bytes + g * 4 * row_bytes + (v_dim * BITS / 8 & ~(Raw::kVBytes < 4 ? 3 : 0)),
                    *lvu = stage + (sub + d.subtiles) * sub_bytes + g * 4 * row_bytes + ((unit_at0 + v_dim / kMxBlock) & ~3);
@@ -578,6 +696,7 @@ __global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : kQuantWaves)
             }
         }
     } else {
+    find_rows();
     keep_loads();
     if (first < kb) {
         const uint32_t place = places(first, page_next);
@@ -615,9 +734,10 @@ __global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : kQuantWaves)
     }
     if (__any(apart)) {
         // what was left out, query by query with what it does not see at 0 (a product's columns are queries of their own)
-        for (int k0 = first; k0 < kb; k0 += kStep) {
+        if (MODE == kStaged) find_rows();
+        for (int k0 = MODE == kShared ? ka : first; k0 < kb; k0 += MODE == kShared ? TK : kStep) {
             const uint32_t place = places(k0, page_of(k0)), now = valid;
-            if (!(k0 + TK > min_lim || now != 0xffffffffu)) continue;
+            if (!(k0 + TK > apart_lim || now != 0xffffffffu)) continue;
             load_k(place);
             load_v(place);
 #pragma unroll
@@ -725,7 +845,7 @@ __global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : kQuantWaves)
                 }
             continue;
         }
-        const int64_t part = (((int64_t)range_at * (MODE == kStaged ? d.subtiles : 1) + sub) * d.row_blocks + block_of) * a.kv_heads * d.pitch + (int64_t)h * d.pitch + (r - r0);
+        const int64_t part = (((int64_t)range_at * (MODE == kStaged ? d.subtiles : 1) + sub) * d.row_blocks + block_of) * a.kv_heads * d.pitch + (int64_t)h * d.pitch + (r - block_r0);
         if (g == 0) a.parts_ml[part] = float2{m[rt], l[rt]};
         float *o = a.parts_o + part * a.dim;
 #pragma unroll
@@ -806,16 +926,17 @@ static hipError_t launch_quant_join(const QuantAttnDev &d, int dp, int rt, hipSt
     return hipGetLastError();
 }
 
+constexpr int quant_shared_rt(int elt) { return elt == ATK_F32 ? 1 : 2; }
 // Row tiles of a wavefront at most: f32's queries are three operands each.
 constexpr int quant_max_rt(int elt, int dp) { return dp == 256 ? (elt == ATK_F32 ? 1 : 2) : elt == ATK_F32 ? 2 : 4; }
 
 template <int ELT, int BITS, int DP, int RT, int MODE, bool FULL>
 static hipError_t launch_quant_as(const QuantAttnDev &d, hipStream_t stream) {
     const int64_t groups = MODE == kApart ? ((int64_t)d.units + kQuantWaves - 1) / kQuantWaves : d.units, whole = 8 * (int64_t)d.chunk;
-    const int threads = MODE == kStaged ? 64 * d.team * d.subtiles : 64 * kQuantWaves;
-    const size_t lds = MODE == kStaged ? (size_t)quant_stage_bytes(d.row_chunks, d.subtiles) : 0;
+    const int threads = MODE == kStaged ? 64 * d.team * d.subtiles : MODE == kShared ? 64 * kSharedWaves : 64 * kQuantWaves;
+    const size_t lds = MODE == kStaged ? (size_t)quant_stage_bytes(d.row_chunks, d.subtiles) : MODE == kShared ? (size_t)quant_shared_bytes(DP) : 0;
     if (lds > 65536) {
-        static const hipError_t e = hipFuncSetAttribute((const void *)&quant_attn_kernel<ELT, BITS, DP, RT, MODE, FULL>, hipFuncAttributeMaxDynamicSharedMemorySize, kStagedLds);
+        static const hipError_t e = hipFuncSetAttribute((const void *)&quant_attn_kernel<ELT, BITS, DP, RT, MODE, FULL>, hipFuncAttributeMaxDynamicSharedMemorySize, MODE == kShared ? quant_shared_bytes(DP) : kStagedLds);
         if (e != hipSuccess) return e;
     }
     hipLaunchKernelGGL((quant_attn_kernel<ELT, BITS, DP, RT, MODE, FULL>), dim3((uint32_t)((groups + whole - 1) / whole * whole)), dim3(threads), lds, stream, d);
@@ -838,6 +959,8 @@ static hipError_t launch_quant_rt(const QuantAttnDev &d, int rt, hipStream_t str
 template <int ELT, int BITS, int DP>
 static hipError_t launch_quant_mode(const QuantAttnDev &d, int rt, int mode, hipStream_t stream) {
     if (mode == kJoin) return launch_quant_rt<ELT, BITS, DP, kJoin>(d, rt, stream);
+    if constexpr (DP <= 128)
+        if (mode == kShared) return launch_quant<ELT, BITS, DP, quant_shared_rt(ELT), kShared>(d, stream);
     if constexpr (DP * BITS / 8 < 128)
         if (mode == kStaged) return launch_quant_rt<ELT, BITS, DP, kStaged>(d, rt, stream);
     return launch_quant_rt<ELT, BITS, DP, kApart>(d, rt, stream);
@@ -846,7 +969,7 @@ template <int ELT>
 static hipError_t launch_quant_elt(const QuantAttnDev &d, int bits, int dp, int rt, int mode, hipStream_t stream) {
     hipError_t e = bits == 4 ? (dp == 64 ? launch_quant_mode<ELT, 4, 64>(d, rt, mode, stream) : dp == 128 ? launch_quant_mode<ELT, 4, 128>(d, rt, mode, stream) : launch_quant_mode<ELT, 4, 256>(d, rt, mode, stream))
                              : (dp == 64 ? launch_quant_mode<ELT, 8, 64>(d, rt, mode, stream) : dp == 128 ? launch_quant_mode<ELT, 8, 128>(d, rt, mode, stream) : launch_quant_mode<ELT, 8, 256>(d, rt, mode, stream));
-    if (e == hipSuccess && d.ranges) e = launch_quant_join<ELT>(d, dp, rt, stream);
+    if (e == hipSuccess && d.ranges) e = launch_quant_join<ELT>(d, dp, rt * (mode == kShared ? kSharedWaves : 1), stream);
     return e;
 }
 

@@ -161,6 +161,43 @@ def test_what_is_not_visible_has_no_influence(bits, dtype):
         assert (np.abs(out - want)[fine] <= tol * np.maximum(1, np.abs(want[fine]))).all()
 
 
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("Hk,D", [(2, 64), (1, 128), (1, 96)], ids=str)
+def test_what_is_not_visible_has_no_influence_on_many_queries(bits, dtype, Hk, D):
+    B, T, H, ps = 2, 70, 2 * Hk, 8
+    q, k, v, table, lens = make(B, T, H, Hk, D, [300, 75], ps, dtype, bits, seed=8)
+    codes = Hk * D * bits // 8
+    t = table.cpu().numpy()
+    hidden = {0: [299, 290, 250], 1: [74, 40]}
+    for b, keys in hidden.items():
+        for j in keys:
+            v[t[b, j // ps], j % ps, codes:codes + D // 32] = 255     # (head 0)
+    q[:] = 0   # (weights that are exact: what is tested is who sees what)
+    kv = [torch.from_numpy(oracle.decode(p.cpu().numpy(), Hk, D, bits)).to(dtype).double().numpy() for p in (k, v)]
+    want = plain.attention(q.double().cpu().numpy(), *kv, t, lens.cpu().numpy(), 0, None, D ** -0.5)[0]
+    for keys in (0, 5000):
+        out = atk.quantized_attention(q, k, v, wider(table, ps, keys), lens, Hk, bits=bits).double().cpu().numpy()
+        assert np.array_equal(np.isnan(out), np.isnan(want))
+        fine = np.isfinite(want)
+        # weights of 1, their sum and the result's rounding: no score has an error here
+        assert (np.abs(out - want)[fine] <= HALF[dtype] * np.abs(want[fine]) + 300 * 3 * E * np.nanmax(np.abs(kv[1])) + (2.0 ** -24 if dtype == torch.float16 else 0)).all()
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("Hk,D", [(6, 64), (7, 32), (9, 64), (11, 128), (16, 64), (13, 96)], ids=str)
+def test_teams_of_heads(bits, Hk, D):
+    """Heads that do not come out even over workgroups, and exponents that lie over several pieces of a row."""
+    check(*make(2, 1, 2 * Hk, Hk, D, [70, 1100], 16, torch.bfloat16, bits, seed=Hk), Hk, bits)
+
+
+def test_many_sequences():
+    """More sequences than ranges that fill the chip: none of them is cut."""
+    lens = [(37 * i) % 50 + (1100 if i == 5 else 1) for i in range(700)]
+    for Hk, D, bits in ((4, 64, 4), (2, 64, 4), (2, 128, 8)):
+        check(*make(700, 1, 2 * Hk, Hk, D, lens, 64, torch.bfloat16, bits, seed=Hk, spare=0), Hk, bits)
+
+
 def test_reports_and_bad_pages():
     q, k, v, table, lens = make(2, 1, 4, 2, 64, [60, 40], 16, torch.bfloat16, 4, seed=9)
     for keys in (0, 3000):
