@@ -392,15 +392,15 @@ __global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : MODE == kSha
             for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) t = fmaxf(t, s[rt][x][j]);
-            t = fmaxf(t, __shfl_xor(t, 16, 64));
-            t = fmaxf(t, __shfl_xor(t, 32, 64));
             top[rt] = t;
             raise |= (t - m[rt]) * a.scale2 > kLazyMax;
         }
-        if (__any(raise)) {
+        if (__any(raise)) {  // (a query's lanes find out what they have in common when one of them has to know, and not for every tile)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                const float to = fmaxf(m[rt], top[rt]);
+                float t = fmaxf(top[rt], __shfl_xor(top[rt], 16, 64));
+                t = fmaxf(t, __shfl_xor(t, 32, 64));
+                const float to = fmaxf(m[rt], t);
                 const float f = m[rt] == kNoMax ? 1.0f : __builtin_amdgcn_exp2f((m[rt] - to) * a.scale2);  // (nothing is kept yet where there was no maximum)
                 l[rt] *= f;
 #pragma unroll
