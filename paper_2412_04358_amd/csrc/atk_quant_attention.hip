@@ -41,7 +41,7 @@ static int check_quant(const atk_quant_attention_args *p, bool pointers) {
     return ATK_OK;
 }
 
-constexpr int64_t kSharedRows = 97;
+constexpr int64_t kSharedRows = 97, kWideParts = 16;
 
 static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
     const int64_t group = p->heads / p->kv_heads, rows = p->tokens * group, all = p->row_pages * p->page_size;
@@ -130,6 +130,7 @@ int atk_quant_attention(const atk_quant_attention_args *p, void *work, int64_t w
     d.row16 = (uint32_t)(mx_token_bytes(p->kv_heads, p->dim, p->bits) / 16);
     d.head_codes = (uint32_t)(p->dim * p->bits / 8), d.head_units = (uint32_t)(p->dim / kMxBlock), d.code_bytes = (uint32_t)p->kv_heads * d.head_codes;
     d.row_blocks = pl.row_blocks, d.ranges = pl.ranges, d.units = (int)pl.units, d.chunk = pl.chunk, d.pitch = pl.pitch, d.by_four = p->page_size % 4 == 0;
+    d.wide_join = pl.ranges > 0 && (int64_t)pl.ranges * pl.subtiles >= kWideParts * p->batch && pl.rows < (INT64_C(1) << 24);
     d.team = pl.team, d.subtiles = pl.subtiles, d.row_chunks = pl.row_chunks, d.unit_from = pl.code_chunks;
     hipStream_t s = (hipStream_t)stream;
     const hipError_t e = p->dtype == ATK_F32    ? launch_quant_f32(d, p->bits, pl.dp, pl.rt, pl.mode, s)

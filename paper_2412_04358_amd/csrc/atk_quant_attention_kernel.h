@@ -24,6 +24,7 @@ struct QuantAttnDev {
     int ranges;             // of all sequences together, at most; 0: one each, and no parts
     int2 *shares;           // [sequence]: its first range, and how many it has
     bool by_four;           // pages are whole fours of tokens
+    bool wide_join;         // a row's parts are joined by four wavefronts
     int team, subtiles;     // MODE kStaged: heads of a workgroup, 32 keys that it takes at a time for each of them
     int row_chunks, unit_from;  // ... pieces of 16 bytes of a token that it brings in, how many of those are codes (behind them: the exponents)
     int chunk;              // workgroups next to each other that read the same keys: they go to one XCD
@@ -858,12 +859,13 @@ __global__ __launch_bounds__(64 * (MODE == kStaged ? kStagedWaves : MODE == kSha
     }
 }
 
-// Joins the parts of a row: one wavefront, LPR lanes have four elements each, 64 / LPR parts at a time and four of those on their way.
-template <int ELT, int LPR>
+// Joins the parts of a row: LPR lanes have four elements each, 64 / LPR parts at a time and four of those on their way; one wavefront, or with many parts four that take turns (one
+// sequence of 100000 keys, which is cut in 380: 70 us -> 46).
+template <int ELT, int LPR, int WAVES>
 __global__ __launch_bounds__(256) void quant_join_kernel(const QuantAttnDev d, int rows_of) {
     const AttnDev &a = d.a;
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = WAVES > 1 ? threadIdx.x >> 6 : 0;
+    const int64_t row = WAVES > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= (int64_t)a.batch * a.tokens * a.heads) return;
     const int head = (int)(row % a.heads);
     const int64_t bt = row / a.heads;
@@ -885,9 +887,9 @@ __global__ __launch_bounds__(256) void quant_join_kernel(const QuantAttnDev d, i
     const int dim = lane % LPR * 4;
     f32x4 o = {0, 0, 0, 0};
     if (dim < a.dim) {
-        constexpr int kStep = 64 / LPR;
+        constexpr int kStep = 64 / LPR * WAVES;
         const float *from = a.parts_o + first * a.dim + dim;
-        for (int p0 = lane / LPR; p0 < share.y; p0 += 4 * kStep) {
+        for (int p0 = wave * (64 / LPR) + lane / LPR; p0 < share.y; p0 += 4 * kStep) {
             float2 x[4];
             f32x4 v[4];
 #pragma unroll
@@ -908,22 +910,32 @@ __global__ __launch_bounds__(256) void quant_join_kernel(const QuantAttnDev d, i
     for (int w = LPR; w < 64; w <<= 1)
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], w, 64);
+    if constexpr (WAVES > 1) {
+        __shared__ f32x4 sums[WAVES][LPR];
+        if (lane < LPR) sums[wave][lane] = o;
+        __syncthreads();
+        if (wave > 0) return;
+        o = sums[0][lane % LPR];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) o += sums[w][lane % LPR];
+    }
     if (l == 0.0f) o = f32x4{0, 0, 0, 0};  // no key, or scores of -inf alone, whose values do not count even if they are NaN
     const float f = l == 0.0f ? 0.0f : 1.0f / l;
     if (lane < LPR && dim < a.dim) store_out<ELT>((char *)a.out + (b * a.os[0] + t * a.os[1] + head * a.os[2] + dim) * AttnElt<ELT>::kBytes, o * f);
     if (a.lse && lane == 0) a.lse[row] = row_lse<ELT>(a, m, l);
 }
-template <int ELT>
-static hipError_t launch_quant_join(const QuantAttnDev &d, int dp, int rt, hipStream_t stream) {
+template <int ELT, int LPR>
+static hipError_t launch_quant_join_of(const QuantAttnDev &d, int rows_of, hipStream_t stream) {
     const int64_t rows = (int64_t)d.a.batch * d.a.tokens * d.a.heads;
-    const dim3 grid((uint32_t)((rows + 3) / 4)), threads(256);
-    if (dp == 64)
-        hipLaunchKernelGGL((quant_join_kernel<ELT, 16>), grid, threads, 0, stream, d, 16 * rt);
-    else if (dp == 128)
-        hipLaunchKernelGGL((quant_join_kernel<ELT, 32>), grid, threads, 0, stream, d, 16 * rt);
+    if (d.wide_join)
+        hipLaunchKernelGGL((quant_join_kernel<ELT, LPR, 4>), dim3((uint32_t)rows), dim3(256), 0, stream, d, rows_of);
     else
-        hipLaunchKernelGGL((quant_join_kernel<ELT, 64>), grid, threads, 0, stream, d, 16 * rt);
+        hipLaunchKernelGGL((quant_join_kernel<ELT, LPR, 1>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, stream, d, rows_of);
     return hipGetLastError();
+}
+template <int ELT>
+static hipError_t launch_quant_join(const QuantAttnDev &d, int dp, int rows_of, hipStream_t stream) {
+    return dp == 64 ? launch_quant_join_of<ELT, 16>(d, rows_of, stream) : dp == 128 ? launch_quant_join_of<ELT, 32>(d, rows_of, stream) : launch_quant_join_of<ELT, 64>(d, rows_of, stream);
 }
 
 constexpr int quant_shared_rt(int elt) { return elt == ATK_F32 ? 1 : 2; }
@@ -969,7 +981,7 @@ template <int ELT>
 static hipError_t launch_quant_elt(const QuantAttnDev &d, int bits, int dp, int rt, int mode, hipStream_t stream) {
     hipError_t e = bits == 4 ? (dp == 64 ? launch_quant_mode<ELT, 4, 64>(d, rt, mode, stream) : dp == 128 ? launch_quant_mode<ELT, 4, 128>(d, rt, mode, stream) : launch_quant_mode<ELT, 4, 256>(d, rt, mode, stream))
                              : (dp == 64 ? launch_quant_mode<ELT, 8, 64>(d, rt, mode, stream) : dp == 128 ? launch_quant_mode<ELT, 8, 128>(d, rt, mode, stream) : launch_quant_mode<ELT, 8, 256>(d, rt, mode, stream));
-    if (e == hipSuccess && d.ranges) e = launch_quant_join<ELT>(d, dp, rt * (mode == kShared ? kSharedWaves : 1), stream);
+    if (e == hipSuccess && d.ranges) e = launch_quant_join<ELT>(d, dp, 16 * rt * (mode == kShared ? kSharedWaves : 1), stream);
     return e;
 }
 
