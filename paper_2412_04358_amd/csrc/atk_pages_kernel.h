@@ -177,7 +177,8 @@ __device__ __forceinline__ AppendSeq append_seq(const PagesDev &t, const int32_t
 // What becomes of the tables when `tokens` tokens have gone to each of the sequences.  By one workgroup, the last to end; n_free: pages of the stack at the call.
 __device__ __forceinline__ void append_tables(const PagesDev &t, const int32_t *seqs, int64_t n, int64_t tokens, int n_free) {
     // Rows, lengths and references, 256 sequences at a time.  Whether a page is copied goes by the references at the call, so the pages that
-    // were copied only lose theirs afterwards.
+    // were copied only lose theirs afterwards.  Pages in their order over all threads: one thread for a sequence's took as long as all the rest of a prompt of 4000 tokens (250 pages).
+    __shared__ int fronts[kThreads], places[kThreads], rows[kThreads];
     int base = n_free;
     bool copied = false;
     for (int64_t j0 = 0; j0 < n; j0 += kThreads) {
@@ -189,21 +190,26 @@ __device__ __forceinline__ void append_tables(const PagesDev &t, const int32_t *
             takes = s.takes();
         }
         const int all = scan_threads(takes, &front);
+        fronts[threadIdx.x] = front;
         if (j < n && !s.bad) {
-            int from = base - 1 - front;
-            int32_t *row = t.table + s.seq * t.row_pages;
+            places[threadIdx.x] = s.copy ? s.used - 1 : s.used, rows[threadIdx.x] = s.seq;
             if (s.copy) {
                 copied = true;
                 atomicOr(&t.left[s.old >> 5], 1u << (s.old & 31));
                 atomicAdd(&t.leaving[s.old], 1);
             }
-            for (int k = s.copy ? s.used - 1 : s.used; k < s.after; ++k) {
-                const int fresh = t.free_at(from--);
-                row[k] = fresh;
-                if (t.is_page(fresh)) atomicAdd(&t.refs[fresh], 1);
-            }
             t.lens[s.seq] = (int)(s.len + tokens);
         }
+        __syncthreads();
+        for (int e = threadIdx.x; e < all; e += kThreads) {
+            int i = 0;  // the last sequence in front of which there are e pages at most: the one that takes page e
+            for (int w = kThreads / 2; w > 0; w /= 2)
+                if (fronts[i + w] <= e) i += w;
+            const int fresh = t.free_at((int64_t)base - 1 - e);
+            t.table[rows[i] * t.row_pages + places[i] + (e - fronts[i])] = fresh;
+            if (t.is_page(fresh)) atomicAdd(&t.refs[fresh], 1);
+        }
+        __syncthreads();
         base -= all;
     }
     if (threadIdx.x == 0) *t.n_free = base;
