@@ -17,7 +17,7 @@ constexpr int kChunk = 512;           // of a wavefront's step
 constexpr int kTop = 32;
 constexpr int kHeld = 16;             // (groups of) minis of a lane of the wavefront that chooses among them
 constexpr int kList = kTop * kMini;   // tokens that may have to be ranked
-constexpr int kSplitThreads = 256, kRowThreads = 1024;
+constexpr int kSplitThreads = 256, kRowThreads = 512;  // (1024 for a row: 2048 rows of 32000 bf16 50 us, 512: 34)
 constexpr int64_t kRowMinis = 2048;   // minis that a workgroup keeps in LDS
 constexpr float kReach = 4.0f;        // how far the largest logit may be above the reference: e^d is off by |d| 2^-24 and more
 constexpr float kLog2e = 1.4426950408889634f;
@@ -115,9 +115,25 @@ struct Logits8 {
     }
 };
 
-__device__ __forceinline__ float wave_max16(float v) {  // over the 16 lanes of a mini
-    for (int w = 1; w < 16; w <<= 1) v = fmaxf(v, __shfl_xor(v, w, 64));
-    return v;
+// Over the 16 lanes of a mini, by rotations of them that cost no LDS.
+template <int N>
+__device__ __forceinline__ float rotated(float v) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x120 + N, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float max_of_16(float v) {
+    v = fmaxf(v, rotated<8>(v));
+    v = fmaxf(v, rotated<4>(v));
+    v = fmaxf(v, rotated<2>(v));
+    return fmaxf(v, rotated<1>(v));
+}
+// Over the wavefront, in a scalar: shifts within 16 lanes, then the last lane of those to the next ones.
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_with(uint32_t v) {
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+    v = max_with<0x142>(max_with<0x118>(max_with<0x114>(max_with<0x112>(max_with<0x111>(v)))));
+    return (uint32_t)__builtin_amdgcn_readlane((int)max_with<0x143>(v), 63);
 }
 
 // Elements from .. to - 1 of a row by the workgroup's wavefronts (from: whole chunks); mini's largest logits to minis[] from `from` / kMini on.
@@ -135,7 +151,7 @@ __device__ __forceinline__ Stats scan_row(const void *row, int from, int to, flo
         for (int j = 2; j < 8; ++j) top = fmaxf(top, x[j]);
         most = fmaxf(most, top);
         if (TOP) {
-            const float m = wave_max16(top);
+            const float m = max_of_16(top);
             if ((lane & 15) == 0 && at < to) minis[at / kMini] = m;
         }
         if (most > s.r + kReach) refer(s, most);
@@ -204,20 +220,22 @@ __device__ __forceinline__ void finish_row(const ScoresDev &a, int64_t r, const 
             const int held = (groups + 63) / 64;
             uint32_t key[kHeld], best = 0;
             int where = 0;
+            float most_of[kHeld];
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) most_of[i] = -__builtin_inff();
+#pragma unroll 1
+            for (int j = 0; j < per; ++j)
+#pragma unroll
+                for (int i = 0; i < kHeld; ++i)
+                    if (i < held) most_of[i] = fmaxf(most_of[i], minis[min((lane * held + i) * per + j, a.n_minis - 1)]);
 #pragma unroll
             for (int i = 0; i < kHeld; ++i) {
-                const int g = lane * held + i;
-                key[i] = 0;  // (below all keys: that of -inf is 0x007fffff)
-                if (i < held && g < groups) {
-                    float m = -__builtin_inff();
-                    for (int j = g * per; j < min(a.n_minis, (g + 1) * per); ++j) m = fmaxf(m, minis[j]);
-                    key[i] = key_of(m);
-                }
+                key[i] = i < held && lane * held + i < groups ? key_of(most_of[i]) : 0;  // (0 is below all keys: that of -inf is 0x007fffff)
                 if (key[i] > best) best = key[i], where = i;
             }
+#pragma unroll 1
             for (int k = 0; k < wanted; ++k) {
-                uint32_t most = best;
-                for (int w = 1; w < 64; w <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, w, 64));
+                const uint32_t most = wave_max(best);
                 const int first = __builtin_ctzll(__ballot(best == most));
                 if (lane == first) {
                     places[k] = lane * held + where;
@@ -235,7 +253,7 @@ __device__ __forceinline__ void finish_row(const ScoresDev &a, int64_t r, const 
         }
         __syncthreads();
         // tokens that come into question; where more might come than there is room for, the k first of those so far are kept
-        const int size = per * kMini;
+        const int size = per * kMini, bits = 31 - __builtin_clz(size);
         uint32_t floor_key = least;
         auto sort = [&]() {  // descending, by all threads
             const int n = count;
@@ -256,6 +274,7 @@ __device__ __forceinline__ void finish_row(const ScoresDev &a, int64_t r, const 
                 }
         };
         const int step = kList / 2;
+#pragma unroll 1
         for (int e0 = 0; e0 < wanted * size; e0 += step) {
             if (wanted * size > kList && e0 > 0) {
                 __syncthreads();
@@ -270,7 +289,7 @@ __device__ __forceinline__ void finish_row(const ScoresDev &a, int64_t r, const 
                 }
             }
             for (int e = e0 + threadIdx.x; e < min(e0 + step, wanted * size); e += THREADS) {
-                const int i = places[e / size] * size + e % size;
+                const int i = (places[e >> bits] << bits) + (e & (size - 1));
                 if (i >= a.vocab) continue;
                 const uint32_t key = key_of(logit<ELT>(row, i));
                 if (key >= floor_key) list[atomicAdd(&count, 1)] = (uint64_t)key << 32 | (uint32_t)~i;
@@ -286,6 +305,7 @@ __device__ __forceinline__ void finish_row(const ScoresDev &a, int64_t r, const 
             for (int i = threadIdx.x; i < n; i += THREADS) {
                 const uint64_t x = list[i];
                 int rank = 0;
+#pragma unroll 4
                 for (int j = 0; j < n; ++j) rank += list[j] > x;
                 if (rank < a.top) put(rank, x);
             }

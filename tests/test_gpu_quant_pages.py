@@ -213,6 +213,21 @@ def test_all_or_nothing_and_reports():
         assert (got[0, :there] != 0).all() and (got[0, there:] == 0).all(), row
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_large_reads(dtype):
+    """More than half of what the caches hold: outputs go past them."""
+    heads, dim, T = 8, 128, 1100
+    t = atk.PageTables.empty(40, 32, 1, 40)
+    pools = pools_of(1, 40, 32, heads, dim, 4)
+    atk.append_quantized(t, pools, ints(0), [some((1, T, heads, dim), dtype, 0)])
+    rows, starts = torch.zeros((70,), dtype=torch.int32, device="cuda"), torch.arange(70, dtype=torch.int32, device="cuda")
+    one = atk.read_quantized(t, pools, ints(0), None, T + 70, heads, dim, dtype=dtype)[0][0]
+    got = atk.read_quantized(t, pools, rows, starts, T, heads, dim, dtype=dtype)[0]
+    for i in (0, 1, 33, 69):
+        assert torch.equal(got[i], one[i:i + T])
+    assert (got[69, T - 69:] == 0).all() and t.status.item() == 0
+
+
 def test_nothing_to_do():
     t = atk.PageTables.empty(3, 4, 3, 2)
     pools = pools_of(1, 3, 4, 1, 64, 4)
