@@ -41,7 +41,12 @@ static int check_quant(const atk_quant_attention_args *p, bool pointers) {
     return ATK_OK;
 }
 
-constexpr int64_t kSharedRows = 97, kWideParts = 16;
+// Queries of a sequence and a head of the cache from which on they share operands by way of LDS (kShared), 256 of them a workgroup: 8 sequences of 4000 to 8000 keys, 64 queries 79 us so and 56
+// with 64 of them in one wavefront, 96 queries 84 and 77, 128 88 and more.
+constexpr int64_t kSharedRows = 97;
+// Parts of a row from which on four wavefronts join them.
+constexpr int64_t kWideParts = 16;
+constexpr int64_t kScan = 8192;  // sequences up to which every workgroup looks its range up among all of them
 
 static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
     const int64_t group = p->heads / p->kv_heads, rows = p->tokens * group, all = p->row_pages * p->page_size;
@@ -49,16 +54,16 @@ static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
     pl->rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     pl->rt = std::min(pl->rt, quant_max_rt(p->dtype, pl->dp));
     const int64_t tiles = quant_ceil(all, 32);
-    // few keys: a workgroup's wavefronts share them
+    // few keys (by the rows of the table, as the host does not know the lengths): a workgroup's wavefronts share them, in one launch
     pl->mode = pl->rt == 1 && tiles <= 32 ? kJoin : kApart;
     if (rows >= kSharedRows && pl->dp <= 128) pl->mode = kShared, pl->rt = quant_shared_rt(p->dtype);
     const int block_rows = 16 * pl->rt * (pl->mode == kShared ? kSharedWaves : 1);
     pl->row_blocks = (int)quant_ceil(rows, block_rows);
     pl->team = pl->subtiles = 1, pl->row_chunks = pl->code_chunks = 0;
     const int64_t head_codes = p->dim * p->bits / 8, head_units = p->dim / kMxBlock;
-    constexpr int64_t kScan = 8192;  // sequences up to which every workgroup looks its range up among all of them
     if (pl->mode == kApart && pl->dp * p->bits / 8 < 128 && pl->rt <= 2 && p->batch <= kScan) {
-        // heads of less than a line: rows by way of LDS
+        // heads of less than a line of 128 bytes: rows by way of LDS, since loads of half a line cost as much as of a whole one (64 sequences of 4096 to 8192 keys, 8 heads of 64 bytes: the
+        // loads alone 146 us head by head, 98 by rows)
         const int64_t teams = quant_ceil(p->kv_heads, kStagedWaves);
         pl->mode = kStaged;
         pl->team = (int)quant_ceil(p->kv_heads, teams);
@@ -72,7 +77,8 @@ static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
         pl->row_chunks = pl->code_chunks + (int)units;
         if (pl->row_chunks * 32 > kStagedPieces * 64 * pl->team || quant_stage_bytes(pl->row_chunks, pl->subtiles) > kStagedLds) pl->mode = kApart, pl->team = pl->subtiles = 1;
     }
-    // ranges for wavefronts that fill the chip once, if that is more than one for each sequence
+    // ranges for wavefronts that fill the chip once, if that is more than one for each sequence; of kShared twice, as their lengths differ (2 x 512 queries over 8192 to 16384 keys: once 430 us,
+    // twice 296, three times 299)
     const int64_t per_range = (pl->mode == kStaged ? quant_ceil(p->kv_heads, pl->team) : p->kv_heads) * pl->row_blocks;
     const int64_t slots = 4 * kNumCU * quant_waves(p->dtype, pl->dp, pl->rt, pl->mode) / (pl->mode == kStaged ? pl->team * pl->subtiles : pl->mode == kShared ? kSharedWaves : 1);
     const int64_t wanted = (pl->mode == kShared ? 2 : 1) * slots / per_range, range_tiles = quant_ceil(tiles, pl->mode == kShared ? kSharedSubs : pl->subtiles);

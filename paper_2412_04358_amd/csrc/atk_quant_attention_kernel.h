@@ -169,7 +169,7 @@ constexpr int quant_waves(int elt, int dp, int rt, int mode) {
 }
 
 // Loads stay on their sides of this.  A wait for one is a number of later ones, the least over all ways to it, so page numbers, keys and values have to be asked for in one order in front of the
-// loop and in it: with page numbers last in front of it each tile waited for the next one's values (64 sequences of 4096 to 8192 keys: XXX).
+// loop and in it, or each tile waits for the next one's values.
 __device__ __forceinline__ void keep_loads() { __builtin_amdgcn_sched_barrier(0x78f); }
 
 // FULL: heads of DP elements.  Shorter ones: what lies behind them is read at their first elements, and counts as 0 in keys; of values it goes into sums that are not written.
@@ -948,7 +948,7 @@ static hipError_t launch_quant_as(const QuantAttnDev &d, hipStream_t stream) {
     const int threads = MODE == kStaged ? 64 * d.team * d.subtiles : MODE == kShared ? 64 * kSharedWaves : 64 * kQuantWaves;
     const size_t lds = MODE == kStaged ? (size_t)quant_stage_bytes(d.row_chunks, d.subtiles) : MODE == kShared ? (size_t)quant_shared_bytes(DP) : 0;
     if (lds > 65536) {
-        static const hipError_t e = hipFuncSetAttribute((const void *)&quant_attn_kernel<ELT, BITS, DP, RT, MODE, FULL>, hipFuncAttributeMaxDynamicSharedMemorySize, MODE == kShared ? quant_shared_bytes(DP) : kStagedLds);
+        const hipError_t e = hipFuncSetAttribute((const void *)&quant_attn_kernel<ELT, BITS, DP, RT, MODE, FULL>, hipFuncAttributeMaxDynamicSharedMemorySize, MODE == kShared ? quant_shared_bytes(DP) : kStagedLds);
         if (e != hipSuccess) return e;
     }
     hipLaunchKernelGGL((quant_attn_kernel<ELT, BITS, DP, RT, MODE, FULL>), dim3((uint32_t)((groups + whole - 1) / whole * whole)), dim3(threads), lds, stream, d);
