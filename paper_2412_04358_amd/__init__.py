@@ -3,7 +3,8 @@
 `approx_topk` / `exact_topk` call the hand-written HIP library through its C ABI; the
 library is loaded on first use and a missing build raises, there is no CPU fallback.
 What a decoder needs beside the selection - attention over a shared prefix, verification of
-drafted tokens, a cache's pages - is in decode.py.
+drafted tokens, a cache's pages - is in decode.py, a cache in few bits in quantized.py, and
+the scores of tokens in scores.py.
 """
 from .binding import (  # noqa: F401
     ATK_BF16,

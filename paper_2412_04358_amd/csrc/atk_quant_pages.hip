@@ -2,6 +2,8 @@
 //
 // Bound by memory: an element is read and written once, four lanes have a block of 32 (eight elements each, 16 bytes of a 16-bit type) and find its largest magnitude by two exchanges.
 // append is atk_pages.hip's append with the conversion on the way, and a sequence's tokens cut into pieces, so that one long prompt fills the chip.
+// Two prompts of 4000 tokens into 24 pools, 497 MB: about 110 us, and read back, as much again: 70; eight sequences of 8192 tokens out of two pools, 407 MB: 77 us (5.3 TB/s); four tokens into two
+// pools: 7 us, the chain of numbers, pages, values, and the tables behind them.
 #include "atk_mx.h"
 #include "atk_pages_kernel.h"
 

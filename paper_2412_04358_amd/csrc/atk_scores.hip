@@ -6,7 +6,8 @@
 // ties broken by number the k likeliest tokens lie in the k minis whose largest logits come first (a token outside of them would have k before it).  These are read
 // again, and what is not below the k-th mini's largest is ranked: hardly more than k tokens as a rule.
 //
-// Bound by memory where there are rows for the chip, by the chain of row, minis, tokens where there is one.
+// Bound by memory where there are rows for the chip, by the chain of row, minis, tokens where there is one.  64 x 5 rows of 128256 bf16, 82 MB: 25 us without likeliest tokens, 34 with five, 39 to 42 with
+// twenty (they are chosen one after the other, 0.45 us each); one row of 32000 f32 8 and 11 us; the gradient of 4096 rows of 32000 bf16, 524 MB: 102 us (5.1 TB/s).
 #include "atk_decode_common.h"
 #include "../../include/atk_scores.h"
 
