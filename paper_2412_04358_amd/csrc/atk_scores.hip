@@ -6,8 +6,8 @@
 // ties broken by number the k likeliest tokens lie in the k minis whose largest logits come first (a token outside of them would have k before it).  These are read
 // again, and what is not below the k-th mini's largest is ranked: hardly more than k tokens as a rule.
 //
-// Bound by memory where there are rows for the chip, by the chain of row, minis, tokens where there is one.  64 x 5 rows of 128256 bf16, 82 MB: 25 us without likeliest tokens, 34 with five, 39 to 42 with
-// twenty (they are chosen one after the other, 0.45 us each); one row of 32000 f32 8 and 11 us; the gradient of 4096 rows of 32000 bf16, 524 MB: 102 us (5.1 TB/s).
+// Bound by memory where there are rows for the chip, by the chain of row, minis, tokens where there is one.  64 x 5 rows of 128256 bf16, 82 MB: 25 us without likeliest tokens, 34 with five, 36 to 39 with
+// twenty; one row of 32000 f32 8 and 11 us; the gradient of 4096 rows of 32000 bf16, 524 MB: 102 us (5.1 TB/s).
 #include "atk_decode_common.h"
 #include "../../include/atk_scores.h"
 
@@ -16,6 +16,7 @@ namespace atk {
 constexpr int kMini = 128;            // elements of a mini: 16 lanes' eight
 constexpr int kChunk = 512;           // of a wavefront's step
 constexpr int kTop = 32;
+constexpr int kPlaces = 64;           // (groups of) minis whose tokens are looked at
 constexpr int kHeld = 16;             // (groups of) minis of a lane of the wavefront that chooses among them
 constexpr int kList = kTop * kMini;   // tokens that may have to be ranked
 constexpr int kSplitThreads = 256, kRowThreads = 512;  // (1024 for a row: 2048 rows of 32000 bf16 50 us, 512: 34)
@@ -207,7 +208,7 @@ __device__ __forceinline__ void finish_row(const ScoresDev &a, int64_t r, const 
         a.entropy[r] = s.z == 0.0f ? 0.0f : logf(s.z) - s.y / s.z;
     }
     if constexpr (TOP) {
-        __shared__ int places[kTop];
+        __shared__ int places[kPlaces], wanted;
         __shared__ uint32_t least;
         __shared__ int count;
         __shared__ uint64_t list[kList];
@@ -215,7 +216,7 @@ __device__ __forceinline__ void finish_row(const ScoresDev &a, int64_t r, const 
         // groups of minis, as many as one wavefront holds; groups of a lane are next to each other, so of equal ones the lowest lane's comes first
         int per = 1;
         while ((a.n_minis + per - 1) / per > 64 * kHeld) per *= 2;
-        const int groups = (a.n_minis + per - 1) / per, wanted = min(a.top, groups);
+        const int groups = (a.n_minis + per - 1) / per;
         if (threadIdx.x == 0) count = 0;
         if (threadIdx.x < 64) {
             const int held = (groups + 63) / 64;
@@ -234,22 +235,49 @@ __device__ __forceinline__ void finish_row(const ScoresDev &a, int64_t r, const 
                 key[i] = i < held && lane * held + i < groups ? key_of(most_of[i]) : 0;  // (0 is below all keys: that of -inf is 0x007fffff)
                 if (key[i] > best) best = key[i], where = i;
             }
-#pragma unroll 1
-            for (int k = 0; k < wanted; ++k) {
-                const uint32_t most = wave_max(best);
-                const int first = __builtin_ctzll(__ballot(best == most));
-                if (lane == first) {
-                    places[k] = lane * held + where;
-                    best = 0;
-                    int next = 0;
-#pragma unroll
-                    for (int i = 0; i < kHeld; ++i) {
-                        if (i == where) key[i] = 0;
-                        if (key[i] > best) best = key[i], next = i;
-                    }
-                    where = next;
+            // The `top`-th largest of the lanes' best keys is one that `top` tokens reach, so all that count are in groups that reach it: as a rule hardly more than `top` of them.  For a few tokens
+            // the groups one after the other are as fast (one row of 32000, five: 11.8 us against 13.0; 8 rows of 128256, twenty: 21.0 against 18.7).
+            int n = kPlaces + 1;
+            uint32_t reach = 0;
+            if (a.top > 8) {
+                int rank = 0;
+#pragma unroll 8
+                for (int w = 0; w < 64; ++w) {
+                    const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)best, w);
+                    rank += o > best || (o == best && w < lane);
                 }
-                if (lane == 0 && k == wanted - 1) least = a.top <= groups ? most : 0u;
+                reach = (uint32_t)__builtin_amdgcn_readlane((int)best, __builtin_ctzll(__ballot(rank == a.top - 1)));  // (0, if fewer lanes than that have a group)
+                n = 0;
+#pragma unroll
+                for (int i = 0; i < kHeld; ++i) {
+                    const bool in = key[i] > 0 && key[i] >= reach;
+                    const uint64_t all = __ballot(in);
+                    const int at = n + __popcll(all & ((uint64_t)1 << lane) - 1);
+                    if (in && at < kPlaces) places[at] = lane * held + i;
+                    n += __popcll(all);
+                }
+            }
+            if (n <= kPlaces) {
+                if (lane == 0) wanted = n, least = reach;
+            } else {
+                // a few, or many that are alike: the first `top` groups, one after the other
+                const int first_few = min(a.top, groups);
+                for (int k = 0; k < first_few; ++k) {
+                    const uint32_t most = wave_max(best);
+                    const int first = __builtin_ctzll(__ballot(best == most));
+                    if (lane == first) {
+                        places[k] = lane * held + where;
+                        best = 0;
+                        int next = 0;
+#pragma unroll
+                        for (int i = 0; i < kHeld; ++i) {
+                            if (i == where) key[i] = 0;
+                            if (key[i] > best) best = key[i], next = i;
+                        }
+                        where = next;
+                    }
+                    if (lane == 0 && k == first_few - 1) wanted = first_few, least = a.top <= groups ? most : 0u;
+                }
             }
         }
         __syncthreads();
