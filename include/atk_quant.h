@@ -40,7 +40,7 @@ int atk_read_quantized(const atk_page_tables *t, const void *const *pools, void 
 /*
  * Attention of `tokens` new tokens of each of `batch` sequences over such pools k and v.
  *   Which keys a query sees, what it gets from none, and what status reports are as for atk_shared_prefix_attention, with all keys the sequence's own.  Keys and values are
- *   those that atk_read_quantized gives in `dtype`.  (In f32 a unit that is never written, of 2^119 and more for e4m3 or 2^126 for e2m1, may give NaN in place of an infinity.)
+ *   those that atk_read_quantized gives in `dtype`.  (In f32 a unit that is never written, of 2^120 and more for e4m3 or 2^126 for e2m1, may give NaN in place of an infinity.)
  *   q, out     (batch, tokens, heads, dim) of `dtype`, dim contiguous, strides in elements for the first three (whole 16 bytes but for a single one's).
  *   k, v       n_pages * page_size rows of atk_quant_token_bytes() bytes, on 16 bytes; fewer than 2^36 bytes each.
  *   heads      a multiple of kv_heads; query head h reads head h / (heads / kv_heads).
