@@ -4,6 +4,7 @@
  *
  * Rows of logits x (batch, tokens, vocab) of `dtype`, vocab contiguous, strides in elements for the first two (rows begin where elements may):
  *   lse = log sum_i exp(x_i),   log p_i = x_i - lse,   entropy = -sum_i p_i log p_i (with 0 log 0 = 0), all f32.
+ * A log probability is as good as its size allows wherever the row lies: it is taken from a logit near the largest one, not from lse, which in f32 is off by |lse| 2^-24.
  * A logit of -inf has no probability.  A row without any (all -inf) has lse -inf, log probabilities of -inf and entropy 0; with a NaN or +inf all of these are NaN.
  */
 #ifndef ATK_SCORES_H

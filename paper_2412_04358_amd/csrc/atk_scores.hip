@@ -199,13 +199,14 @@ __device__ __forceinline__ Stats join_threads(Stats s) {
 // What a row's sums give, and its likeliest tokens.  minis: in LDS or not.
 template <int ELT, bool TOP, int THREADS>
 __device__ __forceinline__ void finish_row(const ScoresDev &a, int64_t r, const void *row, Stats s, const float *minis) {
-    const float lse = s.z == 0.0f ? -__builtin_inff() : s.r + logf(s.z);
+    // (a logit's distance from the reference is small where its probability is not, whatever its size; from lse it would be off by |lse| 2^-24, all of it in rows of the type's lowest value)
+    const float log_z = logf(s.z);
+    auto log_p = [&](float x) { return s.z == 0.0f ? -__builtin_inff() : x - s.r - log_z; };
     if (threadIdx.x == 0) {
         const int t = a.chosen[r];
-        float p = -__builtin_inff();
-        if ((unsigned)t < (unsigned)a.vocab && !(s.z == 0.0f)) p = logit<ELT>(row, t) - lse;
-        a.logprobs[r] = p, a.lse[r] = lse;
-        a.entropy[r] = s.z == 0.0f ? 0.0f : logf(s.z) - s.y / s.z;
+        a.logprobs[r] = (unsigned)t < (unsigned)a.vocab ? log_p(logit<ELT>(row, t)) : -__builtin_inff();
+        a.lse[r] = s.z == 0.0f ? -__builtin_inff() : s.r + log_z;
+        a.entropy[r] = s.z == 0.0f ? 0.0f : log_z - s.y / s.z;
     }
     if constexpr (TOP) {
         __shared__ int places[kPlaces], wanted;
@@ -328,7 +329,7 @@ __device__ __forceinline__ void finish_row(const ScoresDev &a, int64_t r, const 
         const int n = count;
         auto put = [&](int k, uint64_t x) {
             a.top_tokens[r * a.top + k] = (int)~(uint32_t)x;
-            a.top_logprobs[r * a.top + k] = s.z == 0.0f ? -__builtin_inff() : of_key((uint32_t)(x >> 32)) - lse;
+            a.top_logprobs[r * a.top + k] = log_p(of_key((uint32_t)(x >> 32)));
         };
         if (n <= 256) {
             for (int i = threadIdx.x; i < n; i += THREADS) {
