@@ -30,7 +30,8 @@ int atk_token_logprobs(const void *logits, const int64_t stride[2], const int32_
 /*
  * grad (batch, tokens, vocab) of `dtype`, strides in elements for the first two: with a = grad_logprobs and b = grad_entropy (batch, tokens) f32 (either may be NULL: 0)
  *   grad_i = a ([i = chosen] - p_i) - b p_i (log p_i + entropy),   p_i = exp(x_i - lse)
- * of the lse and the entropy that the call above gave (entropy may be NULL where grad_entropy is).  A chosen token outside 0..vocab-1 has a = 0; a row without any
+ * of the lse and the entropy that the call above gave (entropy may be NULL where grad_entropy is).  With |lse| below 1024 p is off by |lse| 2^-24 relatively, as lse itself is; from there on (a row of
+ * the type's lowest value) what lse lost in its rounding is found from the row and put in again, if it is no more than that.  A chosen token outside 0..vocab-1 has a = 0; a row without any
  * probability has gradients of 0.  Rows of grad do not overlap; it may be the logits' own memory, in the same places.
  */
 int atk_token_logprobs_grad(const void *logits, const int64_t stride[2], const int32_t *chosen, const float *lse, const float *entropy,

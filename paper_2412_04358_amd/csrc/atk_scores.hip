@@ -8,6 +8,8 @@
 //
 // Bound by memory where there are rows for the chip, by the chain of row, minis, tokens where there is one.  64 x 5 rows of 128256 bf16, 82 MB: 25 us without likeliest tokens, 34 with five, 36 to 39 with
 // twenty; one row of 32000 f32 8 and 11 us; the gradient of 4096 rows of 32000 bf16, 524 MB: 102 us (5.1 TB/s).
+#include <type_traits>
+
 #include "atk_decode_common.h"
 #include "../../include/atk_scores.h"
 
@@ -390,6 +392,10 @@ struct GradDev {
     int tokens, vocab, pieces;
 };
 constexpr int kGradThreads = 256, kGradPiece = kGradThreads * 8 * 4;
+// From here on p = e^(x - lse) is off by more than 2^-14 through lse's rounding to f32, half a step of |lse| 2^-23 (in a row of the type's lowest value it is 1 for every token).  A row with such an lse
+// is summed up first: log sum e^(x - lse) is what the rounding took, if it is no more than a rounding takes (an lse that is not these logits' own is taken as it is).  |lse| below it: 2^-24 of
+// it at most, as any function of an lse in f32.
+constexpr float kFarLse = 1024.0f;
 
 template <int ELT>
 __device__ __forceinline__ void store_logits8(void *row, int i, const float *x) {
@@ -435,30 +441,58 @@ __global__ __launch_bounds__(kGradThreads) void scores_grad_kernel(const GradDev
     const float lse = d.lse[r], b = d.b ? d.b[r] : 0.0f, h = d.b ? d.entropy[r] : 0.0f;
     const float a = d.a && (unsigned)t < (unsigned)d.vocab ? d.a[r] : 0.0f;
     const bool none = lse == -__builtin_inff();
+    const bool far = fabsf(lse) >= kFarLse && fabsf(lse) < __builtin_inff();
+    float more = 0.0f;
     auto of = [&](float x, int i) {
-        const float l = x - lse, p = __builtin_amdgcn_exp2f(l * kLog2e);
+        const float l = x - lse - more, p = __builtin_amdgcn_exp2f(l * kLog2e);
         float g = p == 0.0f ? 0.0f : -p * fmaf(b, l + h, a);  // (0 * -inf is no number)
         if (i == t) g += a;
         return none ? 0.0f : g;
     };
-    Logits8<ELT> v[kAtOnce];
+    // whole: all of the piece is in the row, so that all loads go out before the branch, which waits for lse (with lanes' conditions around each, f16 rows took 54 us for 47)
+    auto ordinary = [&](auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        Logits8<ELT> v[kAtOnce];
 #pragma unroll
-    for (int j = 0; j < kAtOnce; ++j) {
-        const int i = from + (j * kGradThreads + (int)threadIdx.x) * 8;
-        if (i + 8 <= d.vocab) v[j].load(row, i);
-    }
-#pragma unroll
-    for (int j = 0; j < kAtOnce; ++j) {
-        const int i = from + (j * kGradThreads + (int)threadIdx.x) * 8;
-        if (i + 8 <= d.vocab) {
-            float g[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) g[k] = of(v[j].get(k), i + k);
-            store_logits8<ELT>(out, i, g);
-        } else {
-            for (int k = i; k < d.vocab; ++k) store_logit<ELT>(out, k, of(logit<ELT>(row, k), k));
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int i = from + (j * kGradThreads + (int)threadIdx.x) * 8;
+            if (WHOLE || i + 8 <= d.vocab) v[j].load(row, i);
         }
-    }
+        if (far) return;
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int i = from + (j * kGradThreads + (int)threadIdx.x) * 8;
+            if (WHOLE || i + 8 <= d.vocab) {
+                float g[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) g[k] = of(v[j].get(k), i + k);
+                store_logits8<ELT>(out, i, g);
+            } else {
+                for (int k = i; k < d.vocab; ++k) store_logit<ELT>(out, k, of(logit<ELT>(row, k), k));
+            }
+        }
+    };
+    if (from + kGradPiece <= d.vocab)
+        ordinary(std::true_type{});
+    else
+        ordinary(std::false_type{});
+    // one workgroup for the whole row, which may be the gradient's own memory: all of it is read before any is written (not always the row's first one: these can all be of one XCD; 2048 rows of 32000
+    // bf16 181 us where all are like this, 47 where none is)
+    if (!far || blockIdx.x % d.pieces != r % d.pieces) return;
+    __shared__ float waves[kGradThreads / 64];
+    float z = 0.0f;
+#pragma unroll 8
+    for (int i = threadIdx.x; i < d.vocab; i += kGradThreads) z += __builtin_amdgcn_exp2f((logit<ELT>(row, i) - lse) * kLog2e);
+    for (int w = 1; w < 64; w <<= 1) z += __shfl_xor(z, w, 64);
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = z;
+    __syncthreads();
+    z = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kGradThreads / 64; ++w) z += waves[w];
+    more = logf(z);
+    if (!(fabsf(more) <= fabsf(lse) * 0x1p-23f)) more = 0.0f;
+#pragma unroll 8
+    for (int i = threadIdx.x; i < d.vocab; i += kGradThreads) store_logit<ELT>(out, i, of(logit<ELT>(row, i), i));
 }
 
 // ---------------------------------------------------------------------------------------------------------------- host
