@@ -127,12 +127,12 @@ def read_quantized(tables, pools, seqs, starts, tokens, kv_heads, dim, bits=4, d
 def quantized_attention(q, k_pages, v_pages, page_table, lens, kv_heads, bits=4, seqs=None, scale=None, out=None, return_lse=False, status=None):
     """Attention of the last T tokens of each of B sequences over quantised pools.
 
-    q (B, T, heads, dim) of float32, bfloat16 or float16, strided as it likes but for a contiguous dim; heads is a multiple of kv_heads, dim of 32, up to 256.
+    q (B, T, heads, dim) of float32, bfloat16 or float16, strided as it likes (by whole 16 bytes) but for a contiguous dim, and so is out; heads is a multiple of kv_heads, dim of 32, up to 256.
     k_pages, v_pages (pages, page_size, quantized_token_bytes(kv_heads, dim, bits)) uint8.  page_table (rows, pages per row) and lens (rows) int32: row seqs[i]
     (int32; None: i) is sequence i's, and its length counts the T tokens of this call.  Token t sees the keys before lens - (T - 1 - t).  scale: 1 / sqrt(dim) if None.
 
     Returns out (B, T, heads, dim), with return_lse also the log of the sum of exp of the scaled scores (B, T, heads) f32: what shared_prefix_attention gives on the
-    values that read_quantized gives in q's type.  A token that sees no key gets 0 and -inf."""
+    values that read_quantized gives in q's type.  A token that sees no key gets 0 and -inf.  Autograd sees none of it: results require no gradient, whatever q does."""
     if out is None:
         got = plain.call("attention", q, k_pages, v_pages, page_table, lens, kv_heads, bits, seqs, scale, return_lse, status)
         if got is not None:
@@ -183,4 +183,5 @@ def quantized_attention(q, k_pages, v_pages, page_table, lens, kv_heads, bits=4,
         binding._check(bytes_)
     work = torch.empty((bytes_,), dtype=torch.uint8, device=device)
     _call(device, _lib.atk_quant_attention, a, work.data_ptr(), bytes_)
+    torch.autograd.graph.increment_version(out)  # (autograd may have saved it)
     return (out, lse) if return_lse else out

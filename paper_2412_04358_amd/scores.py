@@ -53,7 +53,7 @@ def token_logprobs(logits, tokens, top=0):
 
     logits (B, T, vocab) of float32, bfloat16 or float16, strided as they like but for a contiguous vocab; tokens (B, T) int32, outside of the vocabulary where there is none
     (its log probability is -inf).  Returns logprobs (B, T), entropy (B, T), lse (B, T), the log of the sum of exp of the logits, top_logprobs (B, T, top), all f32, and
-    top_tokens (B, T, top) int32: the likeliest first, equally likely ones by their numbers."""
+    top_tokens (B, T, top) int32: the likeliest first, equally likely ones by their numbers.  None of these requires a gradient, also where logits do: token_logprobs_grad is theirs."""
     got = plain.call("logprobs", logits, tokens, top)
     if got is not None:
         return got
@@ -84,7 +84,7 @@ def token_logprobs_grad(logits, tokens, lse, entropy, grad_logprobs, grad_entrop
     """Gradient with respect to the logits of sum(grad_logprobs * logprobs) + sum(grad_entropy * entropy) of token_logprobs(logits, tokens).
 
     lse, entropy as that call gave them (entropy may be None where grad_entropy is), grad_logprobs (None: 0) and grad_entropy (B, T) float32.  Returns a tensor like logits, in `out` if given:
-    of their shape and type, strided as it likes but for a contiguous vocab, the logits themselves if they are not needed any more."""
+    of their shape and type, strided as it likes but for a contiguous vocab and rows that do not overlap, the logits themselves if they are not needed any more.  It is what logits.backward() takes."""
     if out is None:
         got = plain.call("grad", logits, tokens, lse, entropy, grad_logprobs, grad_entropy)
         if got is not None:
@@ -106,4 +106,5 @@ def token_logprobs_grad(logits, tokens, lse, entropy, grad_logprobs, grad_entrop
     _, out_strides = _rows(out, "out")
     if B * T * V:
         _call(device, (_lib or _library()).atk_token_logprobs_grad, logits.data_ptr(), strides, tokens.data_ptr(), *ptrs, B, T, V, code, out.data_ptr(), out_strides)
+        torch.autograd.graph.increment_version(out)  # (autograd may have saved it, the logits above all)
     return out
