@@ -49,7 +49,7 @@ __device__ __forceinline__ QuantRange quant_range(const AttnDev &a, int2 *shares
     int64_t total = 0;
     for (int b0 = 0; b0 < a.batch; b0 += 64) total += tiles_of(b0 + lane);
     for (int w = 1; w < 64; w <<= 1) total += __shfl_xor(total, w, 64);
-    const int spare = ranges - a.batch, each = (int)max((int64_t)4, (total + spare - 1) / spare);
+    const int spare = ranges - a.batch, each = (int)max((int64_t)4, spare > 0 ? (total + spare - 1) / spare : total);  // (none to spare: nothing is cut)
     QuantRange r{-1, 0, 0};
     int before = 0;
     for (int b0 = 0; b0 < a.batch && r.b < 0; b0 += 64) {

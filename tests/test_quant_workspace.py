@@ -1,0 +1,31 @@
+"""The workspace of quantized_attention against what it returns: parts of sequences that are not cut come once."""
+import ctypes
+import os
+
+import pytest
+
+import paper_2412_04358_amd as atk
+from paper_2412_04358_amd import quantized
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(atk.lib_path()):
+        import __graft_entry__
+
+        __graft_entry__.build()
+    return quantized._library()
+
+
+@pytest.mark.parametrize("batch,tokens,heads,kv_heads,dim,bits,keys", [
+    (8192, 4, 8, 1, 64, 4, 1100), (4096, 4, 8, 1, 128, 4, 1100), (3000, 1, 8, 1, 64, 4, 2000), (8000, 2, 16, 2, 64, 8, 30000), (512, 1, 8, 1, 64, 4, 1100 - 1100 % 32),
+])
+def test_uncut_sequences(lib, batch, tokens, heads, kv_heads, dim, bits, keys):
+    pages = -(-keys // 16)
+    row = heads * dim
+    a = quantized._QuantAttentionArgs(batch=batch, tokens=tokens, heads=heads, kv_heads=kv_heads, dim=dim, page_size=16, n_pages=1000, rows=batch, row_pages=pages, table_stride=pages,
+                                      q_stride=(ctypes.c_int64 * 3)(tokens * row, row, dim), out_stride=(ctypes.c_int64 * 3)(tokens * row, row, dim), scale=0.125, dtype=1, bits=bits)
+    size = lib.atk_quant_attention_workspace_bytes(a)
+    most = 2 if batch == 512 else 1     # (some hundred sequences of a few tiles may be cut in two)
+    # a part is a row in f32, its maximum and its sum; at most four tiles are taken at once
+    assert 0 < size <= most * 4 * batch * tokens * heads * (4 * dim + 8) + 8 * batch + 16
