@@ -41,9 +41,12 @@ static int check_quant(const atk_quant_attention_args *p, bool pointers) {
     return ATK_OK;
 }
 
-// Queries of a sequence and a head of the cache from which on they share operands by way of LDS (kShared), 256 of them a workgroup: 8 sequences of 4000 to 8000 keys, 64 queries 79 us so and 56
+// Queries of a sequence and a head of the cache from which on they share operands by way of LDS (kShared), 256 of them a workgroup (f32: 128): 8 sequences of 4000 to 8000 keys, 64 queries 79 us so and 56
 // with 64 of them in one wavefront, 96 queries 84 and 77, 128 88 and more.
 constexpr int64_t kSharedRows = 97;
+// A staged head is less than 128 bytes, so 64 at most, and a team's exponents are 16 bytes at most, which may lie over two pieces: what that takes of a lane's loads, and of LDS without asking for more.
+constexpr bool staged_fits(int team) { return 32 * (4 * team + 2) <= kStagedPieces * 64 * team && quant_stage_bytes(4 * team + 2, kStagedWaves / team) <= 65536; }
+static_assert(staged_fits(1) && staged_fits(2) && staged_fits(3) && staged_fits(4) && kStagedWaves == 4);
 // Parts of a row from which on four wavefronts join them.
 constexpr int64_t kWideParts = 16;
 constexpr int64_t kScan = 8192;  // sequences up to which every workgroup looks its range up among all of them
@@ -75,7 +78,6 @@ static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
             units = std::max(units, (std::min(to, p->kv_heads * head_units) + 15) / 16 - from / 16);
         }
         pl->row_chunks = pl->code_chunks + (int)units;
-        if (pl->row_chunks * 32 > kStagedPieces * 64 * pl->team || quant_stage_bytes(pl->row_chunks, pl->subtiles) > kStagedLds) pl->mode = kApart, pl->team = pl->subtiles = 1;
     }
     // ranges for wavefronts that fill the chip once, if that is more than one for each sequence; of kShared twice, as their lengths differ (2 x 512 queries over 8192 to 16384 keys: once 430 us,
     // twice 296, three times 299)

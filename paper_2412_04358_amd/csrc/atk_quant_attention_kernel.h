@@ -81,7 +81,7 @@ enum { kApart = 0,   // each has a range of its own, for a head (workgroups' wav
 };
 constexpr int kSharedWaves = 8, kSharedSubs = 4;  // of kShared: each wavefront makes keys' or values' operands of 32 of a tile's 128 keys
 constexpr int quant_shared_bytes(int dp) { return 2 * kSharedSubs * (2 * (dp / 32) + dp / 16) * 1024 + 64; }
-constexpr int kStagedWaves = 4, kStagedPieces = 3, kStagedLds = 80 * 1024;
+constexpr int kStagedWaves = 4, kStagedPieces = 3;
 constexpr int quant_stage_bytes(int row_chunks, int subtiles) { return 4 * subtiles * 32 * row_chunks * 16; }
 
 constexpr int quant_products(int elt) { return elt == ATK_F32 ? ATK_BF16 : elt; }  // type of the products' operands
@@ -952,8 +952,8 @@ static hipError_t launch_quant_as(const QuantAttnDev &d, hipStream_t stream) {
     const int64_t groups = MODE == kApart ? ((int64_t)d.units + kQuantWaves - 1) / kQuantWaves : d.units, whole = 8 * (int64_t)d.chunk;
     const int threads = MODE == kStaged ? 64 * d.team * d.subtiles : MODE == kShared ? 64 * kSharedWaves : 64 * kQuantWaves;
     const size_t lds = MODE == kStaged ? (size_t)quant_stage_bytes(d.row_chunks, d.subtiles) : MODE == kShared ? (size_t)quant_shared_bytes(DP) : 0;
-    if (lds > 65536) {
-        const hipError_t e = hipFuncSetAttribute((const void *)&quant_attn_kernel<ELT, BITS, DP, RT, MODE, FULL>, hipFuncAttributeMaxDynamicSharedMemorySize, MODE == kShared ? quant_shared_bytes(DP) : kStagedLds);
+    if (MODE == kShared) {  // (more than 64 KB)
+        const hipError_t e = hipFuncSetAttribute((const void *)&quant_attn_kernel<ELT, BITS, DP, RT, MODE, FULL>, hipFuncAttributeMaxDynamicSharedMemorySize, quant_shared_bytes(DP));
         if (e != hipSuccess) return e;
     }
     hipLaunchKernelGGL((quant_attn_kernel<ELT, BITS, DP, RT, MODE, FULL>), dim3((uint32_t)((groups + whole - 1) / whole * whole)), dim3(threads), lds, stream, d);
