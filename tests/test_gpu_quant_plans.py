@@ -118,6 +118,9 @@ def check(args, Hk, bits, widths=(0, 3000, 40000), told=0):
     (1, 300, 2, 1, 32, [260], 16),              # more new tokens than keys
     (3, 2, 20, 2, 64, [300, 0, 450], 16),       # 20, short rows of the table: several tiles at once, nothing cut
     (2, 5, 5, 1, 128, [390, 31], 16),
+    (2, 4, 5, 1, 32, [700, 45], 16),            # 20, of heads with padding
+    (2, 8, 5, 1, 96, [500, 1], 16),             # 40, of heads with padding
+    (2, 1, 4, 2, 256, [900, 40], 16),           # few, of long heads
 ], ids=str)
 def test_queries(bits, dtype, B, T, H, Hk, D, lens, ps):
     check(make(B, T, H, Hk, D, lens, ps, dtype, bits, seed=T * H + D), Hk, bits)
@@ -138,12 +141,14 @@ def test_pages_that_are_none(bits, dtype, T, Hk, D):
 
 
 @pytest.mark.parametrize("bits", [4, 8])
-@pytest.mark.parametrize("B,T,H,Hk,D", [(8200, 1, 4, 2, 64), (8200, 4, 5, 1, 64), (8200, 1, 3, 1, 128), (8200, 9, 12, 1, 32), (3000, 1, 8, 1, 64), (3000, 3, 16, 2, 64), (8000, 1, 2, 1, 128)], ids=str)
-def test_more_sequences_than_are_cut(bits, B, T, H, Hk, D):
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("B,T,H,Hk,D", [(8200, 1, 4, 2, 64), (8200, 4, 5, 1, 64), (8200, 1, 3, 1, 128), (8200, 5, 4, 1, 128), (8200, 2, 3, 1, 96), (8200, 6, 3, 1, 96), (8200, 1, 6, 3, 32),
+                                        (8200, 3, 6, 1, 32), (8200, 9, 12, 1, 32), (3000, 1, 8, 1, 64), (3000, 3, 16, 2, 64), (8000, 1, 2, 1, 128)], ids=str)
+def test_more_sequences_than_are_cut(bits, dtype, B, T, H, Hk, D):
     """Some thousand sequences, of rows that many of them share: each gets what its row's first one gets, bit for bit."""
     lens = [1, 33, 1030, 0, 200, 7, 64, 65, 300, 129]
     rows = len(lens)
-    q, k, v, table, n = make(rows, T, H, Hk, D, lens, 16, torch.bfloat16, bits, seed=T)
+    q, k, v, table, n = make(rows, T, H, Hk, D, lens, 16, dtype, bits, seed=T)
     table = wider(table, 16, 3000)
     seqs = (torch.arange(B, device="cuda") % rows).int()
     out, lse = atk.quantized_attention(q[seqs.long()], k, v, table, n, Hk, bits=bits, seqs=seqs, return_lse=True)

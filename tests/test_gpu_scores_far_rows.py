@@ -41,7 +41,7 @@ def make(kind, B, V, dtype, seed=0):
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("kind", ["lowest", "largest", "lowest but for -inf", "above", "below"])
-@pytest.mark.parametrize("B,V,top", [(1, 1, 1), (2, 300, 5), (1, 32000, 20), (2, 40000, 9), (260, 5000, 0), (1, 270000, 32)])
+@pytest.mark.parametrize("B,V,top", [(1, 1, 1), (2, 300, 5), (1, 32000, 20), (2, 40000, 9), (3, 40000, 0), (260, 5000, 0), (1, 270000, 32)])
 def test_far_rows(dtype, kind, B, V, top):
     x = make(kind, B, V, dtype, seed=V)
     tokens = torch.full((B, 1), V // 3, dtype=torch.int32, device="cuda")
