@@ -96,7 +96,7 @@ static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
     const int64_t parts = (int64_t)pl->ranges * pl->subtiles * pl->row_blocks * p->kv_heads * pl->pitch;
     pl->o_bytes = parts * p->dim * 4, pl->ml_bytes = parts * 8;
     pl->bytes = pl->o_bytes + pl->ml_bytes + (pl->ranges ? p->batch * 8 : 16);
-    const bool fit = pl->units < (INT64_C(1) << 31) && launches(quant_ceil(pl->units, per) + 8 * pl->chunk, 64 * kSharedWaves) && launches(quant_ceil(pl->rows, 4), 256);
+    const bool fit = pl->units < (INT64_C(1) << 31) && launches(quant_ceil(pl->units, per) + 8 * pl->chunk, 64 * kSharedWaves) && (pl->ranges == 0 || launches(quant_ceil(pl->rows, 4), 256));
     return fit ? ATK_OK : ATK_ERR_ARGS;
 }
 
