@@ -157,3 +157,23 @@ def test_more_sequences_than_are_cut(bits, dtype, B, T, H, Hk, D):
     live = torch.isfinite(wlse)
     assert ((out[:rows].double().cpu() - want).abs() <= tol).all()
     assert torch.equal(lse[:rows].double().cpu()[~live], wlse[~live]) and ((lse[:rows].double().cpu() - wlse).abs()[live] <= ltol[live]).all()
+
+
+@pytest.mark.parametrize("T,H,Hk,D", [(70, 8, 2, 128), (5, 8, 1, 64), (5, 8, 2, 128)], ids=str)
+def test_captured_and_replayed(T, H, Hk, D):
+    """Many queries in a graph, replayed with other inputs and lengths beside the same call outside of it."""
+    q, k, v, table, lens = make(2, T, H, Hk, D, [1300, 700], 16, torch.bfloat16, 4, seed=1)
+    table = wider(table, 16, 3000)
+    x, n = q.clone(), lens.clone()
+    atk.quantized_attention(x, k, v, table, n, Hk)     # (what loads on a first call is loaded)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = atk.quantized_attention(x, k, v, table, n, Hk, return_lse=True)
+    for step in range(4):
+        x.copy_(q.flip(0) if step % 2 else q)
+        n.copy_(lens - 37 * step)
+        graph.replay()
+        want, wlse = atk.quantized_attention(x, k, v, table, n, Hk, return_lse=True)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, wlse)
