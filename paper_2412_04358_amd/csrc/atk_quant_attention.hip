@@ -49,7 +49,11 @@ constexpr bool staged_fits(int team) { return 32 * (4 * team + 2) <= kStagedPiec
 static_assert(staged_fits(1) && staged_fits(2) && staged_fits(3) && staged_fits(4) && kStagedWaves == 4);
 // Parts of a row from which on four wavefronts join them.
 constexpr int64_t kWideParts = 16;
-constexpr int64_t kScan = 8192;  // sequences up to which every workgroup looks its range up among all of them
+// Sequences from which on wavefronts have theirs alone where workgroups would take several tiles at once.  One head of 64 in 4 bits: 8000 of 1100 keys 120 us so and 1450 by workgroups, 3500 of 8000 keys 385 and
+// 588, a tenth of them long 248 and 338, 2500 of these 231 and 201 (in f32 317 and 242), 1600 211 and 108.
+constexpr int64_t kManyParts = 3072;
+// Sequences up to which short heads go by way of LDS: 8192 of 1100 keys, 8 heads of 128 in 4 bits, 1570 us so and 2020 by wavefronts; 9000 with 32 queries of 600 keys, 4 heads of 64, 580 and 425.
+constexpr int64_t kStagedBatch = 8192;
 
 static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
     const int64_t group = p->heads / p->kv_heads, rows = p->tokens * group, all = p->row_pages * p->page_size;
@@ -64,7 +68,7 @@ static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
     pl->row_blocks = (int)quant_ceil(rows, block_rows);
     pl->team = pl->subtiles = 1, pl->row_chunks = pl->code_chunks = 0;
     const int64_t head_codes = p->dim * p->bits / 8, head_units = p->dim / kMxBlock;
-    if (pl->mode == kApart && pl->dp * p->bits / 8 < 128 && pl->rt <= 2 && p->batch <= kScan) {
+    if (pl->mode == kApart && pl->dp * p->bits / 8 < 128 && pl->rt <= 2 && p->batch <= kStagedBatch) {
         // heads of less than a line of 128 bytes: rows by way of LDS, since loads of half a line cost as much as of a whole one (64 sequences of 4096 to 8192 keys, 8 heads of 64 bytes: the
         // loads alone 146 us head by head, 98 by rows)
         const int64_t teams = quant_ceil(p->kv_heads, kStagedWaves);
@@ -81,13 +85,14 @@ static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
     }
     // ranges for wavefronts that fill the chip once, if that is more than one for each sequence; of kShared twice, as their lengths differ (2 x 512 queries over 8192 to 16384 keys: once 430 us,
     // twice 296, three times 299)
-    const int64_t per_range = (pl->mode == kStaged ? quant_ceil(p->kv_heads, pl->team) : p->kv_heads) * pl->row_blocks;
+    int64_t per_range = (pl->mode == kStaged ? quant_ceil(p->kv_heads, pl->team) : p->kv_heads) * pl->row_blocks;
     const int64_t slots = 4 * kNumCU * quant_waves(p->dtype, pl->dp, pl->rt, pl->mode) / (pl->mode == kStaged ? pl->team * pl->subtiles : pl->mode == kShared ? kSharedWaves : 1);
     const int64_t wanted = (pl->mode == kShared ? 2 : 1) * slots / per_range, range_tiles = quant_ceil(tiles, pl->mode == kShared ? kSharedSubs : pl->subtiles);
-    // where a workgroup takes several tiles at once (subtiles), its wavefronts' parts are joined by a launch of its own even if nothing is cut, of one range for each sequence: then sequences are cut as
-    // long as that may even out their lengths (1000 of up to 4000 keys, a tenth of them long: cut 55 us, not cut 68; 3000 of 2000: 239 and 153)
-    const bool cut = pl->mode != kJoin && p->batch <= kScan && range_tiles > 4 && (pl->subtiles > 1 ? 3 * wanted > 2 * p->batch : 2 * wanted >= 3 * p->batch);
-    pl->ranges = cut ? (int)std::max<int64_t>(2 * p->batch, std::min(wanted, p->batch * (1 + quant_ceil(range_tiles, 4)))) : pl->mode == kStaged && pl->subtiles > 1 ? (int)p->batch : 0;
+    // a workgroup that takes several tiles at once (subtiles) leaves as many parts for each sequence, cut or not, and a launch to join them: for some thousand sequences more than it saves
+    const bool many = pl->subtiles > 1 && p->batch >= kManyParts;
+    if (many) pl->mode = kApart, pl->team = pl->subtiles = 1, per_range = p->kv_heads * pl->row_blocks;
+    const bool cut = !many && pl->mode != kJoin && range_tiles > 4 && (pl->subtiles > 1 || 2 * wanted >= 3 * p->batch);
+    pl->ranges = cut ? (int)std::max<int64_t>(2 * p->batch, std::min(wanted, p->batch * (1 + quant_ceil(range_tiles, 4)))) : pl->subtiles > 1 ? (int)p->batch : 0;
     pl->units = pl->ranges ? pl->ranges * per_range : p->batch * per_range;
     const int64_t per = pl->mode == kApart ? kQuantWaves : 1;
     pl->chunk = (int)(pl->mode == kStaged ? std::min<int64_t>(quant_ceil(p->kv_heads, pl->team), 16) : p->kv_heads % per ? 1 : std::min<int64_t>(p->kv_heads / per, 16));

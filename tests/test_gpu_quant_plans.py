@@ -143,7 +143,7 @@ def test_pages_that_are_none(bits, dtype, T, Hk, D):
 @pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("B,T,H,Hk,D", [(8200, 1, 4, 2, 64), (8200, 4, 5, 1, 64), (8200, 1, 3, 1, 128), (8200, 5, 4, 1, 128), (8200, 2, 3, 1, 96), (8200, 6, 3, 1, 96), (8200, 1, 6, 3, 32),
-                                        (8200, 3, 6, 1, 32), (8200, 9, 12, 1, 32), (3000, 1, 8, 1, 64), (3000, 3, 16, 2, 64), (8000, 1, 2, 1, 128)], ids=str)
+                                        (8200, 3, 6, 1, 32), (8200, 1, 2, 1, 32), (8200, 9, 12, 1, 32), (9000, 1, 5, 5, 64), (9000, 3, 24, 4, 128), (3000, 1, 8, 1, 64), (3000, 3, 16, 2, 64), (8000, 1, 2, 1, 128)], ids=str)
 def test_more_sequences_than_are_cut(bits, dtype, B, T, H, Hk, D):
     """Some thousand sequences, of rows that many of them share: each gets what its row's first one gets, bit for bit."""
     lens = [1, 33, 1030, 0, 200, 7, 64, 65, 300, 129]
