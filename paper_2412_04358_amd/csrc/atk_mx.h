@@ -1,8 +1,8 @@
 // Elements of a few bits with a power of two for each 32 of them (include/atk_quant.h), both ways by the conversions of CDNA4.
 //
 // These take the unit as an f32, of which they use the exponent: byte << 23, for 0 (2^-127) and 255 (NaN) too.  Decoding is exact in f32 and bf16 (4 significant bits at most), and in f16
-// rounds what is out of its range as a conversion from f32 does; encoding rounds to the nearest, ties to even, and saturates for e2m1 but not for e4m3 (checked over all
-// exponents and codes, and 4 million values).
+// rounds what is out of its range as a conversion from f32 does; encoding rounds to the nearest, ties to even, and saturates for e2m1 but not for e4m3 (tested over all
+// exponents and codes, all numbers of 16 bits and 8 million of f32).
 #pragma once
 
 #include "atk_decode_common.h"

@@ -42,12 +42,13 @@ static int check_quant(const atk_quant_attention_args *p, bool pointers) {
 }
 
 // Queries of a sequence and a head of the cache from which on they share operands by way of LDS (kShared), 256 of them a workgroup (f32: 128): 8 sequences of 4000 to 8000 keys, 64 queries 79 us so and 56
-// with 64 of them in one wavefront, 96 queries 84 and 77, 128 88 and more.
+// with 64 of them in one wavefront, 96 queries 84 and 77, 128 88 and more.  Heads past 128 do not: their two slots of 128 keys would take 256 KB (2 x 512 queries over 4096 to 8192 keys, 16 heads on 4 of
+// 256: 319 us, 663 in f32).
 constexpr int64_t kSharedRows = 97;
 // A staged head is less than 128 bytes, so 64 at most, and a team's exponents are 16 bytes at most, which may lie over two pieces: what that takes of a lane's loads, and of LDS without asking for more.
 constexpr bool staged_fits(int team) { return 32 * (4 * team + 2) <= kStagedPieces * 64 * team && quant_stage_bytes(4 * team + 2, kStagedWaves / team) <= 65536; }
 static_assert(staged_fits(1) && staged_fits(2) && staged_fits(3) && staged_fits(4) && kStagedWaves == 4);
-// Parts of a row from which on four wavefronts join them.
+// Parts of a row from which on four wavefronts join them: 16 sequences of 8000 keys (24 parts) 36 us so and 38 by one, one of 100000 46 and 72, 32 of 8000 (12 parts) 61 and 60, 64 108 and 104.
 constexpr int64_t kWideParts = 16;
 // Sequences from which on wavefronts have theirs alone where workgroups would take several tiles at once.  One head of 64 in 4 bits: 8000 of 1100 keys 120 us so and 1450 by workgroups, 3500 of 8000 keys 385 and
 // 588, a tenth of them long 248 and 338, 2500 of these 231 and 201 (in f32 317 and 242), 1600 211 and 108.
@@ -61,7 +62,8 @@ static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
     pl->rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     pl->rt = std::min(pl->rt, quant_max_rt(p->dtype, pl->dp));
     const int64_t tiles = quant_ceil(all, 32);
-    // few keys (by the rows of the table, as the host does not know the lengths): a workgroup's wavefronts share them, in one launch
+    // few keys (by the rows of the table, as the host does not know the lengths): a workgroup's wavefronts share them, in one launch.  Two sequences, 2 heads of 64 in 4 bits: 256 keys 6.0 us so and 12.8
+    // cut, 1024 10.2 and 13.4, 2048 13.7 and 13.8, 4096 23.5 and 14.0; 64 sequences, 8 heads of 128: 1024 18 and 25, 2048 40 and 39; 256 of these: 512 43 and 49, 1024 78 and 76.
     pl->mode = pl->rt == 1 && tiles <= 32 ? kJoin : kApart;
     if (rows >= kSharedRows && pl->dp <= 128) pl->mode = kShared, pl->rt = quant_shared_rt(p->dtype);
     const int block_rows = 16 * pl->rt * (pl->mode == kShared ? kSharedWaves : 1);
@@ -83,7 +85,8 @@ static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
         }
         pl->row_chunks = pl->code_chunks + (int)units;
     }
-    // ranges for wavefronts that fill the chip once, if that is more than one for each sequence; of kShared twice, as their lengths differ (2 x 512 queries over 8192 to 16384 keys: once 430 us,
+    // ranges for wavefronts that fill the chip once, if that is more than one and a half for each sequence (8 heads of 128 in 4 bits, 6000 keys, 384 ranges: 128 sequences cut 174 us and not cut 294, 192 331
+    // and 335, 256 370 and 342, 320 463 and 426; where a tenth of them are long cutting would go on helping: 256 87 and 291, 320 101 and 305, but the host does not know); of kShared twice, as their lengths differ (2 x 512 queries over 8192 to 16384 keys: once 430 us,
     // twice 296, three times 299)
     int64_t per_range = (pl->mode == kStaged ? quant_ceil(p->kv_heads, pl->team) : p->kv_heads) * pl->row_blocks;
     const int64_t slots = 4 * kNumCU * quant_waves(p->dtype, pl->dp, pl->rt, pl->mode) / (pl->mode == kStaged ? pl->team * pl->subtiles : pl->mode == kShared ? kSharedWaves : 1);
@@ -91,6 +94,7 @@ static int plan_quant(const atk_quant_attention_args *p, QuantPlan *pl) {
     // a workgroup that takes several tiles at once (subtiles) leaves as many parts for each sequence, cut or not, and a launch to join them: for some thousand sequences more than it saves
     const bool many = pl->subtiles > 1 && p->batch >= kManyParts;
     if (many) pl->mode = kApart, pl->team = pl->subtiles = 1, per_range = p->kv_heads * pl->row_blocks;
+    // (too few tiles to cut, and several at once: one range for each sequence)
     const bool cut = !many && pl->mode != kJoin && range_tiles > 4 && (pl->subtiles > 1 || 2 * wanted >= 3 * p->batch);
     pl->ranges = cut ? (int)std::max<int64_t>(2 * p->batch, std::min(wanted, p->batch * (1 + quant_ceil(range_tiles, 4)))) : pl->subtiles > 1 ? (int)p->batch : 0;
     pl->units = pl->ranges ? pl->ranges * per_range : p->batch * per_range;

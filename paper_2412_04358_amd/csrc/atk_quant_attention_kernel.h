@@ -9,9 +9,9 @@
 // with keys and values, which are bf16 numbers, are summed up in f32.  (f32 products take eight times as long as bf16 ones.)
 //
 // How the wavefronts of a workgroup share its work goes by what bounds it (the modes below): few keys by their latency, few queries by the loads, many by vector instructions and products.
-// 64 sequences of 4096 to 8192 keys, 32 heads on 8 of 128, 4 bits, 429 MB: 107 us (4.0 TB/s), the loads alone 98, all else alone 81; 2 x 512 queries over 8192 to 16384 keys, 206
-// GFLOP: 296 to 322 us (0.64 to 0.7 PFLOP/s), the matrix units busy for 27 % and the vector unit for 40 % of the time, a SIMD's two wavefronts waiting for the same things too often;
-// two sequences of 200 keys: 5.9.
+// 64 sequences of 4096 to 8192 keys, 32 heads on 8 of 128, 4 bits, 429 MB: 107 to 109 us (4.0 TB/s) with the join's 5, 95 without what is computed, 81 without the loads; 2 x 512 queries over 8192 to
+// 16384 keys, 206 GFLOP: 295 to 322 us (0.64 to 0.7 PFLOP/s) with the join's 21, the matrix units busy for 29 % and the vector unit for 40 % of the kernel's time, a SIMD's two wavefronts waiting
+// for the same things too often; two sequences of 200 keys: 6.
 #pragma once
 
 #include "atk_attention_kernel.h"

@@ -2,8 +2,9 @@
 //
 // Bound by memory: an element is read and written once, four lanes have a block of 32 (eight elements each, 16 bytes of a 16-bit type) and find its largest magnitude by two exchanges.
 // append is atk_pages.hip's append with the conversion on the way, and a sequence's tokens cut into pieces, so that one long prompt fills the chip.
-// Two prompts of 4000 tokens into 24 pools, 497 MB: about 110 us, and read back, as much again: 70; eight sequences of 8192 tokens out of two pools, 407 MB: 77 us (5.3 TB/s); four tokens into two
-// pools: 7 us, the chain of numbers, pages, values, and the tables behind them.
+// Two prompts of 4000 tokens into 24 pools, 497 MB: 101 to 107 us, and read back, as much again, 76 to 81; eight sequences of 8192 tokens out of two pools, 407 MB: 77 us (5.3 TB/s); four tokens into
+// two pools: 7 us, the chain of numbers, pages, values, and the tables behind them.  f32, whose lanes have 32 bytes in two pieces, goes at half the rate: 4000 tokens into 12 pools and back 291 us, eight
+// sequences out of two 240.
 #include "atk_mx.h"
 #include "atk_pages_kernel.h"
 

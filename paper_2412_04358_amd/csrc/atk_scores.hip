@@ -7,7 +7,7 @@
 // again, and what is not below the k-th mini's largest is ranked: hardly more than k tokens as a rule.
 //
 // Bound by memory where there are rows for the chip, by the chain of row, minis, tokens where there is one.  64 x 5 rows of 128256 bf16, 82 MB: 25 us without likeliest tokens, 34 with five, 36 to 39 with
-// twenty; one row of 32000 f32 8 and 11 us; the gradient of 4096 rows of 32000 bf16, 524 MB: 102 us (5.1 TB/s).
+// twenty; one row of 32000 f32 9, 11 and 14 us; the gradient of 4096 rows of 32000 bf16, 524 MB: 93 to 102 us (5.1 to 5.6 TB/s).
 #include <type_traits>
 
 #include "atk_decode_common.h"
@@ -21,7 +21,8 @@ constexpr int kTop = 32;
 constexpr int kPlaces = 64;           // (groups of) minis whose tokens are looked at
 constexpr int kHeld = 16;             // (groups of) minis of a lane of the wavefront that chooses among them
 constexpr int kList = kTop * kMini;   // tokens that may have to be ranked
-constexpr int kSplitThreads = 256, kRowThreads = 512;  // (1024 for a row: 2048 rows of 32000 bf16 50 us, 512: 34)
+// (a row by 256, 512, 1024 threads, bf16: 2048 of 32000 30, 31, 47 us, with twenty likeliest 66, 58, 70; 320 of 128256 28, 25, 28 and 44, 38, 39; one of 32000 with twenty 16, 13, 13)
+constexpr int kSplitThreads = 256, kRowThreads = 512;
 constexpr int64_t kRowMinis = 2048;   // minis that a workgroup keeps in LDS
 constexpr float kReach = 4.0f;        // how far the largest logit may be above the reference: e^d is off by |d| 2^-24 and more
 constexpr float kLog2e = 1.4426950408889634f;
@@ -509,6 +510,8 @@ static int plan_scores(int64_t batch, int64_t tokens, int64_t vocab, int64_t top
     if (!launches(rows, kRowThreads)) return ATK_ERR_ARGS;
     pl->minis = scores_ceil(vocab, kMini);
     const int64_t chunks = scores_ceil(vocab, kChunk);
+    // One workgroup a row in one launch, or splits of 16 chunks at least and eight workgroups a CU at most in two.  bf16, twenty likeliest: one row of 32000 13 us by row and 15 split, of 64000 16.5 and 16, of
+    // 128256 23 and 17; 16 of 128256 24 and 18, 64 25 and 25, 128 26 and 29, 256 28 and 36, 320 38 and 42, 2048 118 and 149.  Splits of 8 chunks, or four workgroups a CU: level within 6 %.
     pl->by_row = pl->minis <= kRowMinis && (rows >= kNumCU || chunks <= 64);
     pl->splits = pl->by_row ? 1 : std::max<int64_t>(1, std::min(scores_ceil(chunks, 16), scores_ceil(8 * kNumCU, rows)));
     pl->span = scores_ceil(chunks, pl->splits) * kChunk;
