@@ -52,7 +52,7 @@ static_assert(staged_fits(1) && staged_fits(2) && staged_fits(3) && staged_fits(
 constexpr int64_t kWideParts = 16;
 // Sequences from which on wavefronts have theirs alone where workgroups would take several tiles at once.  One head of 64 in 4 bits: 8000 of 1100 keys 120 us so and 1450 by workgroups, 3500 of 8000 keys 385 and
 // 588, a tenth of them long 248 and 338, 2500 of these 231 and 201 (in f32 317 and 242), 1600 211 and 108.
-constexpr int64_t kManyParts = 3072;
+constexpr int64_t kManyParts = 3200;
 // Sequences up to which short heads go by way of LDS: 8192 of 1100 keys, 8 heads of 128 in 4 bits, 1570 us so and 2020 by wavefronts; 9000 with 32 queries of 600 keys, 4 heads of 64, 580 and 425.
 constexpr int64_t kStagedBatch = 8192;
 
